@@ -370,6 +370,112 @@ QRM_API qrm_status qrm_profile_read(qrm_ctx *ctx, int32_t kind, double *ms_total
  */
 QRM_API qrm_status qrm_profile_read_chunks(qrm_ctx *ctx, int32_t max_chunks, double *ms, int32_t *n_chunks);
 
+/*
+ * Fine-tuning (Section 4.2: the image decoder is taught to write the key, with a message loss on the extractor's logits and some hundred
+ * AdamW steps).  The calls below are the parts of such a step that are not matrix products; they take any context, whatever it was
+ * created with, unless stated.  Types of tensors: */
+typedef enum { QRM_F32 = 0, QRM_BF16 = 1, QRM_F16 = 2 } qrm_type;
+typedef enum { QRM_ACT_NONE = 0, QRM_ACT_RELU = 1, QRM_ACT_SILU = 2 } qrm_act;
+
+/*
+ * Group norm with an activation, channels last.  x [N,P,C]: N images of P pixels of C channels; group g is the C / groups channels
+ * from g * C / groups on.  Over the M = P * C / groups values of a group in one image
+ *   mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps),  z = gamma[c] (x - mean) rstd + beta[c],  y = act(z)
+ * with act z, max(z, 0) or z / (1 + exp(-z)); sums and all that follows in 32 bits, y rounded once to its type.
+ * Neighbouring channels lie side by side; pixels and images may lie further apart than C and P * C (the map is a part of a wider
+ * buffer): strides in elements, 0 = dense.  y has strides of its own, dy those of y, dx those of x.
+ * d_gamma, d_beta f32 [C] or NULL (ones, zeros); d_mean, d_rstd f32 [N,groups], what the backward pass needs, or NULL both.
+ * d_y may be d_x, and d_dx may be d_dy, where the strides of x and y are equal; outputs overlap nothing else.
+ *
+ * Backward: with h = (x - mean) rstd and dz = dy act'(z) (0 for a ReLU at z <= 0)
+ *   dbeta[c] = sum dz,  dgamma[c] = sum dz h  (over images and pixels),
+ *   dx = rstd (gamma dz - sum_group(gamma dz) / M - h sum_group(gamma dz h) / M).
+ * d_dx, d_dgamma, d_dbeta: any of them may be NULL (not wanted).  With N = 0 the last two are set to zeros.
+ * The same bits from call to call.  A value that is not finite reaches the outputs of its group in its image and dgamma, dbeta of that
+ * group's channels, no others.
+ * Errors: QRM_E_INVALID (NULL pointer, N < 0, P < 1, groups that do not divide C, an unknown type or activation, eps not above
+ * zero, strides under C or (P-1) * pixel + C, a pointer not aligned to its elements, one of d_mean and d_rstd alone),
+ * QRM_E_UNSUPPORTED (C above 65536, a group of more than 1024 pieces of what the alignment allows to read at once, up to 16 bytes;
+ * N or P of 2^31 and more), QRM_E_NOMEM.
+ */
+typedef struct {
+    int64_t N, P;
+    int32_t C, groups;
+    int32_t type; /* qrm_type of x, y, dx, dy */
+    int32_t act;  /* qrm_act */
+    float eps;
+    int64_t x_pixel, x_image; /* distance of neighbouring pixels / images of x and dx, in elements */
+    int64_t y_pixel, y_image; /* .. of y and dy */
+} qrm_group_norm_desc;
+QRM_API qrm_status qrm_group_norm(qrm_ctx *ctx, const qrm_group_norm_desc *desc, const void *d_x, const float *d_gamma, const float *d_beta,
+                                  void *d_y, float *d_mean, float *d_rstd, void *stream);
+QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_desc *desc, const void *d_x, const void *d_dy,
+                                           const float *d_gamma, const float *d_beta, const float *d_mean, const float *d_rstd,
+                                           void *d_dx, float *d_dgamma, float *d_dbeta, void *stream);
+
+/*
+ * AdamW over all tensors of a network in one call.  A plan (qrm_adamw) holds the addresses and sizes of the parameters and moments, which
+ * stay the caller's and have to stay where they are while the plan is used; gradients are named at every step.  For each element
+ *   g = grad * grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in 32 bits, lr = the step's times the tensor's lr_scale; p is rounded to its type, and once more, from the 32 bits, to d_copy (the
+ * parameters the next forward pass reads in 16 bits).
+ * Moments in 32 bits: f32 [n].  Moments in 8 bits: one code an element and one f32 scale for QRM_MOMENT_BLOCK elements in a
+ * row (the last block of a tensor may be shorter); they are decoded, updated in 32 bits and rounded to the nearest code again:
+ *   m = scale c |c| / 127^2, c int8 (scale: the largest |m| of the block),
+ *   sqrt(v) = scale c^2 / 255^2, c uint8 (scale: the largest sqrt(v)); where v > 0 the code is at least 1, so no root falls to zero.
+ * Zeros (codes and scales) are moments of zero.  A gradient that is not finite spoils its element and, in 8 bits, its block.
+ *
+ * qrm_adamw_create: h_tensors HOST [n_tensors], read during the call.  qrm_adamw_step: h_grads HOST [n_tensors] of device pointers of
+ * grad_type, read during the call; NULL = the tensor has no gradient at this step and stays as it is, moments included.  step counts from
+ * 1.  d_grad_scale f32 [1] on the device, read by the kernels (a clipping factor, the inverse of a loss scale), or NULL = 1.
+ * A launch takes the gradients of several hundred tensors.  qrm_adamw_destroy waits for the device; NULL is ignored.
+ * Errors: QRM_E_INVALID (NULL pointer, n < 0, unknown type, state_bits not 8 or 32, a copy of other than 16 bits or beside parameters that are
+ * not f32, a pointer not aligned to its elements, step < 1, lr, weight_decay, lr_scale or eps negative or not finite, a beta outside [0, 1), a plan of
+ * another device), QRM_E_NOMEM, QRM_E_UNSUPPORTED (a plan of 2^31 and more pieces of 4096 elements).
+ *
+ * qrm_unpack_moment: the values that 8-bit codes stand for, f32 or bf16 [n]: moment 0 = m, 1 = v.
+ */
+#define QRM_MOMENT_BLOCK 256
+typedef struct qrm_adamw qrm_adamw; /* opaque, library-owned */
+typedef struct {
+    int64_t n;               /* elements; 0 is a tensor nothing is done for */
+    void *d_param;           /* param_type [n] */
+    void *d_m, *d_v;         /* f32 [n], or codes [n] */
+    float *d_m_scale, *d_v_scale; /* f32 [(n + 255) / 256] for 8-bit moments, else NULL */
+    void *d_copy;            /* copy_type [n] or NULL */
+    float weight_decay, lr_scale;
+} qrm_adamw_tensor;
+typedef struct {
+    int32_t n_tensors;
+    int32_t param_type, grad_type, copy_type; /* qrm_type; copy_type is read only where a tensor has d_copy */
+    int32_t state_bits;                       /* 32 or 8 */
+} qrm_adamw_desc;
+QRM_API qrm_status qrm_adamw_create(qrm_ctx *ctx, const qrm_adamw_desc *desc, const qrm_adamw_tensor *h_tensors, qrm_adamw **out);
+QRM_API void qrm_adamw_destroy(qrm_adamw *opt);
+QRM_API qrm_status qrm_adamw_step(qrm_ctx *ctx, qrm_adamw *opt, const void *const *h_grads, int64_t step, double lr, double beta1, double beta2,
+                                  double eps, const float *d_grad_scale, void *stream);
+QRM_API qrm_status qrm_unpack_moment(qrm_ctx *ctx, int32_t moment, const void *d_codes, const float *d_scales, int64_t n, int32_t out_type,
+                                     void *d_out, void *stream);
+
+/*
+ * Message loss with its gradient (Section 4.1: binary cross-entropy of the logits against the message, and a penalty for more errors than
+ * the Reed-Solomon code corrects).  With s = +1 / -1 for a target bit of 1 / 0 and x = s * logit
+ *   L = 1/(N n_bits) sum log(1 + exp(-x)) + rs_weight / N sum_images max(0, E - t)^2,
+ *   E = sum over the image's symbols of 1 - prod over the symbol's bits of 1 / (1 + exp(-x)): the expected number of wrong symbols
+ *   when a logit's sigmoid is the chance of a one; t = (n - k) / 2 symbols are corrected; symbol j = bits j*m .. j*m+m-1.
+ * (The paper's E counts wrong bits, which has no gradient and is not what t counts.)
+ * d_logits f32 [N,n_bits]; d_target u8 [N,n_bits] or, with target_rows 1, [n_bits] for all images, any value but 0 is a one;
+ * d_loss f32 [1]; d_grad f32 [N,n_bits] = dL / dlogit, or NULL; d_bit_errors, d_symbol_errors i32 [N], or NULL: hard bits (logit > 0)
+ * and symbols that differ from the target.  The same bits from call to call.  N = 0: the loss is set to 0.
+ * A context without a code takes any n_bits, rs_weight 0 and no d_symbol_errors.
+ * Errors: QRM_E_INVALID (NULL pointer, N < 0, target_rows not 1 or N, n_bits not n * m or outside 1..2040, rs_weight negative or not finite, or
+ * needing a code that is not there), QRM_E_UNSUPPORTED (N of 2^31 / 64 and more), QRM_E_NOMEM.
+ */
+QRM_API qrm_status qrm_message_loss(qrm_ctx *ctx, const float *d_logits, const uint8_t *d_target, int64_t target_rows, int64_t N,
+                                    int32_t n_bits, float rs_weight, float *d_loss, float *d_grad, int32_t *d_bit_errors,
+                                    int32_t *d_symbol_errors, void *stream);
+
 /* Library version string, e.g. "qrm 0.1 gfx950". */
 QRM_API const char *qrm_version(void);
 

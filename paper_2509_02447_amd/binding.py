@@ -37,16 +37,37 @@ class _RsDesc(C.Structure):
     _fields_ = [("m", C.c_int32), ("prim_poly", C.c_uint32), ("n", C.c_int32), ("k", C.c_int32), ("fcr", C.c_int32)]
 
 
+class _GroupNormDesc(C.Structure):
+    _fields_ = [("N", C.c_int64), ("P", C.c_int64), ("C", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32), ("act", C.c_int32),
+                ("eps", C.c_float), ("x_pixel", C.c_int64), ("x_image", C.c_int64), ("y_pixel", C.c_int64), ("y_image", C.c_int64)]
+
+
+class _AdamwTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d_param", C.c_void_p), ("d_m", C.c_void_p), ("d_v", C.c_void_p), ("d_m_scale", C.c_void_p),
+                ("d_v_scale", C.c_void_p), ("d_copy", C.c_void_p), ("weight_decay", C.c_float), ("lr_scale", C.c_float)]
+
+
+class _AdamwDesc(C.Structure):
+    _fields_ = [("n_tensors", C.c_int32), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32),
+                ("state_bits", C.c_int32)]
+
+
 EXPORTS = ["qrm_create", "qrm_destroy", "qrm_last_error", "qrm_set_micro_batch", "qrm_workspace_bytes",
            "qrm_extract_tiles", "qrm_preprocess", "qrm_select_tiles_variance", "qrm_extractor_forward", "qrm_extractor_blocks", "qrm_rs_decode", "qrm_detect",
            "qrm_detect_host", "qrm_plan_streams", "qrm_key_threshold", "qrm_set_key", "qrm_verify_key", "qrm_detect_verify",
-           "qrm_profile_enable", "qrm_profile_read", "qrm_profile_read_chunks", "qrm_release_stream", "qrm_detect_static", "qrm_version"]
+           "qrm_profile_enable", "qrm_profile_read", "qrm_profile_read_chunks", "qrm_release_stream", "qrm_detect_static", "qrm_version",
+           "qrm_group_norm", "qrm_group_norm_backward", "qrm_adamw_create", "qrm_adamw_destroy", "qrm_adamw_step", "qrm_unpack_moment",
+           "qrm_message_loss"]
 DIAG_EXPORTS = ["qrm_diag_set_flags", "qrm_diag_matrix_rate", "qrm_diag_pair_split",
                 "qrm_diag_wide_schedule", "qrm_diag_last_lines", "qrm_diag_host_plan",
                 "qrm_diag_preprocess_strips", "qrm_diag_rs_lanes", "qrm_diag_chain_patience", "qrm_diag_chain_count",
                 "qrm_diag_chain_left_over", "qrm_diag_chain_rule"]   # include/qrm_diag.h: bench and test tooling
 
 QRM_MAX_STREAMS = 8   # include/qrm.h
+QRM_F32, QRM_BF16, QRM_F16 = 0, 1, 2
+QRM_ACT_NONE, QRM_ACT_RELU, QRM_ACT_SILU = 0, 1, 2
+QRM_MOMENT_BLOCK = 256
+ACTIVATIONS = {"none": QRM_ACT_NONE, "relu": QRM_ACT_RELU, "silu": QRM_ACT_SILU}
 QRM_DIAG_NO_FUSED_PAIRS, QRM_DIAG_POISON_WORKSPACE, QRM_DIAG_FUSE_ALWAYS, QRM_DIAG_CHAIN_ALWAYS, QRM_DIAG_NO_CHAIN = 1, 2, 4, 8, 16
 (QRM_PROFILE_PAIR_FIRST, QRM_PROFILE_PAIR_MID, QRM_PROFILE_PAIR_LAST, QRM_PROFILE_BLOCK_FIRST, QRM_PROFILE_BLOCK_MID,
  QRM_PROFILE_BLOCK_LAST, QRM_PROFILE_HEAD, QRM_PROFILE_RS_DECODE, QRM_PROFILE_CHAIN, QRM_PROFILE_KINDS) = range(10)
@@ -139,6 +160,20 @@ def load_library():
     lib.qrm_diag_chain_left_over.restype = C.c_int
     lib.qrm_diag_chain_rule.argtypes = [i32] * 6 + [C.POINTER(i32)] * 2
     lib.qrm_diag_chain_rule.restype = C.c_int
+    lib.qrm_group_norm.argtypes = [vp, C.POINTER(_GroupNormDesc)] + [vp] * 7
+    lib.qrm_group_norm.restype = C.c_int
+    lib.qrm_group_norm_backward.argtypes = [vp, C.POINTER(_GroupNormDesc)] + [vp] * 10
+    lib.qrm_group_norm_backward.restype = C.c_int
+    lib.qrm_adamw_create.argtypes = [vp, C.POINTER(_AdamwDesc), C.POINTER(_AdamwTensor), C.POINTER(vp)]
+    lib.qrm_adamw_create.restype = C.c_int
+    lib.qrm_adamw_destroy.argtypes = [vp]
+    lib.qrm_adamw_destroy.restype = None
+    lib.qrm_adamw_step.argtypes = [vp, vp, C.POINTER(vp), i64, C.c_double, C.c_double, C.c_double, C.c_double, vp, vp]
+    lib.qrm_adamw_step.restype = C.c_int
+    lib.qrm_unpack_moment.argtypes = [vp, i32, vp, vp, i64, i32, vp, vp]
+    lib.qrm_unpack_moment.restype = C.c_int
+    lib.qrm_message_loss.argtypes = [vp, vp, vp, i64, i64, i32, C.c_float, vp, vp, vp, vp, vp]
+    lib.qrm_message_loss.restype = C.c_int
     lib.qrm_version.argtypes = []
     lib.qrm_version.restype = C.c_char_p
     _lib = lib
@@ -176,6 +211,27 @@ def _dptr(t) -> Optional[int]:
         return None
     assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous and on the GPU"
     return t.data_ptr()
+
+
+def _dptr_map(t) -> Optional[int]:
+    """Device pointer of a map [..., C] whose pixels may lie further apart than C elements (or None)."""
+    if t is None:
+        return None
+    assert t.is_cuda and (t.shape[-1] == 1 or t.stride(-1) == 1), "channels must lie side by side, on the GPU"
+    return t.data_ptr()
+
+
+def type_code(dtype) -> int:
+    """qrm_type of a torch dtype."""
+    import torch
+    return {torch.float32: QRM_F32, torch.bfloat16: QRM_BF16, torch.float16: QRM_F16}[dtype]
+
+
+def group_norm_desc(N: int, P: int, C: int, groups: int, dtype, act: str = "none", eps: float = 1e-6, x_pixel: int = 0,
+                    x_image: int = 0, y_pixel: int = 0, y_image: int = 0):
+    """The qrm_group_norm_desc of maps [N,P,C] of `dtype`; act is "none", "relu" or "silu"; strides in elements, 0 = dense."""
+    return _GroupNormDesc(int(N), int(P), int(C), int(groups), type_code(dtype), ACTIVATIONS[act], float(eps), int(x_pixel),
+                          int(x_image), int(y_pixel), int(y_image))
 
 
 def _hptr(t) -> Optional[int]:
@@ -366,3 +422,77 @@ class Context:
                                                 int(tile), _dptr(d_logits), _dptr(d_bits), _dptr(d_msg),
                                                 _dptr(d_codeword), _dptr(d_nerr), _dptr(d_matches), _dptr(d_detected),
                                                 _stream_handle(stream)))
+
+    def qrm_group_norm(self, desc, d_x, d_gamma, d_beta, d_y, d_mean=None, d_rstd=None, stream=None):
+        self._check(self._lib.qrm_group_norm(self._h, C.byref(desc), _dptr_map(d_x), _dptr(d_gamma), _dptr(d_beta), _dptr_map(d_y),
+                                             _dptr(d_mean), _dptr(d_rstd), _stream_handle(stream)))
+
+    def qrm_group_norm_backward(self, desc, d_x, d_dy, d_gamma, d_beta, d_mean, d_rstd, d_dx, d_dgamma=None, d_dbeta=None,
+                                stream=None):
+        self._check(self._lib.qrm_group_norm_backward(self._h, C.byref(desc), _dptr_map(d_x), _dptr_map(d_dy), _dptr(d_gamma),
+                                                      _dptr(d_beta), _dptr(d_mean), _dptr(d_rstd), _dptr_map(d_dx),
+                                                      _dptr(d_dgamma), _dptr(d_dbeta), _stream_handle(stream)))
+
+    def qrm_unpack_moment(self, moment: int, d_codes, d_scales, n, d_out, stream=None):
+        self._check(self._lib.qrm_unpack_moment(self._h, int(moment), _dptr(d_codes), _dptr(d_scales), int(n), type_code(d_out.dtype),
+                                                _dptr(d_out), _stream_handle(stream)))
+
+    def qrm_message_loss(self, d_logits, d_target, target_rows, N, n_bits, rs_weight, d_loss, d_grad=None, d_bit_errors=None,
+                         d_symbol_errors=None, stream=None):
+        self._check(self._lib.qrm_message_loss(self._h, _dptr(d_logits), _dptr(d_target), int(target_rows), int(N), int(n_bits),
+                                               float(rs_weight), _dptr(d_loss), _dptr(d_grad), _dptr(d_bit_errors),
+                                               _dptr(d_symbol_errors), _stream_handle(stream)))
+
+
+class AdamW:
+    """Owns one qrm_adamw.  `tensors`: a list of dict(param=, m=, v=, and as needed m_scale=, v_scale=, copy=, weight_decay=0.0,
+    lr_scale=1.0) of device tensors, all parameters of one type; moments are f32, or int8 (m) and uint8 (v) codes with f32 scales,
+    one for QRM_MOMENT_BLOCK elements.  The object keeps the tensors alive, and `ctx`, which reports its errors."""
+
+    def __init__(self, ctx: Context, tensors, grad_type):
+        self._h = C.c_void_p()
+        self._ctx, self._keep = ctx, list(tensors)
+        self._lib = ctx._lib
+        n = len(self._keep)
+        rows = (_AdamwTensor * max(1, n))()
+        for r, t in zip(rows, self._keep):
+            r.n = t["param"].numel()
+            r.d_param, r.d_m, r.d_v = _dptr(t["param"]), _dptr(t["m"]), _dptr(t["v"])
+            r.d_m_scale, r.d_v_scale, r.d_copy = _dptr(t.get("m_scale")), _dptr(t.get("v_scale")), _dptr(t.get("copy"))
+            r.weight_decay, r.lr_scale = float(t.get("weight_decay", 0.0)), float(t.get("lr_scale", 1.0))
+        one = lambda types, what: (types.pop() if len(types) == 1 else self._mixed(what)) if types else None
+        import torch
+        param = one({t["param"].dtype for t in self._keep}, "parameters") or torch.float32
+        moment = one({t["m"].dtype for t in self._keep}, "moments") or torch.float32
+        copy = one({t["copy"].dtype for t in self._keep if t.get("copy") is not None}, "copies")
+        desc = _AdamwDesc(n, type_code(param), type_code(grad_type), QRM_BF16 if copy is None else type_code(copy),
+                          {torch.float32: 32, torch.int8: 8}[moment])
+        ctx._check(self._lib.qrm_adamw_create(ctx._h, C.byref(desc), rows, C.byref(self._h)))
+        self._n, self._grad_type, self._sizes = n, grad_type, [t["param"].numel() for t in self._keep]
+
+    @staticmethod
+    def _mixed(what):
+        raise ValueError(f"all {what} of a plan have one type")
+
+    def qrm_adamw_step(self, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                       d_grad_scale=None, stream=None):
+        """grads: one device tensor of grad_type for each tensor of the plan, or None where it has no gradient."""
+        assert len(grads) == self._n, "one gradient (or None) for each tensor"
+        ptrs = (C.c_void_p * max(1, self._n))()
+        for i, g in enumerate(grads):
+            if g is not None:
+                assert g.dtype == self._grad_type and g.numel() == self._sizes[i], "a gradient has the wrong type or size"
+                ptrs[i] = _dptr(g)
+        self._ctx._check(self._lib.qrm_adamw_step(self._ctx._h, self._h, ptrs, int(step), float(lr), float(beta1), float(beta2),
+                                                  float(eps), _dptr(d_grad_scale), _stream_handle(stream)))
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h:
+            self._lib.qrm_adamw_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -1,0 +1,263 @@
+// One AdamW step over many tensors (qrm_adamw_step) and the values of 8-bit moments (qrm_unpack_moment).
+//
+// A workgroup takes a piece of 4096 elements of one tensor; which one, a table of the plan says.  Every element is read and written once;
+// nothing is shared between elements but a block's scale of 8-bit moments, which is the largest of 256 neighbours: four to a lane, one
+// block to a wavefront.  Bound by memory: 28 bytes an element in 32 bits, 14 with 8-bit moments, 16-bit gradients and a 16-bit copy.
+#include "qrm_train.h"
+
+#include <type_traits>
+
+namespace qrm {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <int COUNT> struct Grads {
+    const void *p[COUNT];
+};
+
+struct Rates { // of a tensor, in a step
+    float beta1, rest1, beta2, rest2, eps, keep, rate, root, scale;
+};
+
+__device__ __forceinline__ Rates rates_of(const AdamwStep &s, const AdamwTensor &t)
+{
+    return Rates{s.beta1, s.rest1, s.beta2, s.rest2, s.eps, 1.f - s.lr * t.lr_scale * t.weight_decay, s.rate * t.lr_scale, s.root, s.grad_scale ? *s.grad_scale : 1.f};
+}
+
+__device__ __forceinline__ void update(const Rates &r, float g, float &p, float &m, float &v, float &u)
+{
+    g *= r.scale;
+    m = m * r.beta1 + g * r.rest1;
+    v = v * r.beta2 + g * g * r.rest2;
+    u = sqrtf(v);
+    p = p * r.keep - r.rate * (m / (u * r.root + r.eps));
+}
+
+template <int V> __device__ __forceinline__ void store_copy(void *copy, int type, int64_t i, const float (&p)[V])
+{
+    if (type == QRM_BF16) {
+        Pack<bf16_t, V> c;
+#pragma unroll
+        for (int k = 0; k < V; ++k) c.e[k] = (bf16_t)p[k];
+        store_pack<bf16_t, V>((bf16_t *)copy + i, c);
+    } else {
+        Pack<f16_t, V> c;
+#pragma unroll
+        for (int k = 0; k < V; ++k) c.e[k] = (f16_t)p[k];
+        store_pack<f16_t, V>((f16_t *)copy + i, c);
+    }
+}
+
+template <typename TP, typename TG, int V> __device__ __forceinline__ void step_f32(const AdamwTensor &t, const TG *grad, const Rates &r, int copy_type, int64_t i)
+{
+    const Pack<TP, V> p = load_pack<TP, V>((const TP *)t.p + i);
+    const Pack<TG, V> g = load_pack<TG, V>(grad + i);
+    Pack<float, V> m = load_pack<float, V>((const float *)t.m + i), v = load_pack<float, V>((const float *)t.v + i);
+    Pack<TP, V> q;
+    float w[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        float u;
+        w[k] = (float)p.e[k];
+        update(r, (float)g.e[k], w[k], m.e[k], v.e[k], u);
+        q.e[k] = (TP)w[k];
+    }
+    store_pack<TP, V>((TP *)t.p + i, q);
+    store_pack<float, V>((float *)t.m + i, m);
+    store_pack<float, V>((float *)t.v + i, v);
+    if (t.copy) store_copy<V>(t.copy, copy_type, i, w);
+}
+
+__device__ __forceinline__ bool aligned(const void *p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// A multiple of four elements of every array lies on a boundary that one load or store needs.
+template <typename TP, typename TG, typename TM> __device__ __forceinline__ bool wide_ok(const AdamwTensor &t, const TG *grad)
+{
+    return aligned(t.p, 4 * sizeof(TP)) && aligned(grad, 4 * sizeof(TG)) && aligned(t.m, 4 * sizeof(TM)) && aligned(t.v, 4 * sizeof(TM)) &&
+           aligned(t.copy, 8);
+}
+
+template <typename TP, typename TG, int COUNT>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTensor *tensors, const uint2 *pieces, uint32_t t0, Grads<COUNT> grads, AdamwStep s, int copy_type)
+{
+    const uint2 piece = pieces[blockIdx.x];
+    const AdamwTensor t = tensors[piece.x];
+    const TG *grad = (const TG *)grads.p[piece.x - t0];
+    if (!grad) return;
+    const Rates r = rates_of(s, t);
+    const int64_t first = (int64_t)piece.y * kAdamwPiece, last = min(first + kAdamwPiece, t.n);
+    if (wide_ok<TP, TG, float>(t, grad)) {
+        int64_t i = first + threadIdx.x * 4;
+#pragma unroll 4
+        for (; i + 4 <= last; i += kThreads * 4) step_f32<TP, TG, 4>(t, grad, r, copy_type, i);
+        for (; i < last; ++i) step_f32<TP, TG, 1>(t, grad, r, copy_type, i); // (one thread, up to three elements)
+    } else {
+        for (int64_t i = first + threadIdx.x; i < last; i += kThreads) step_f32<TP, TG, 1>(t, grad, r, copy_type, i);
+    }
+}
+
+// ---------------------------------------------------------------- moments in 8 bits
+
+__device__ __forceinline__ float decode_m(int c, float scale) { return scale * ((float)(c * abs(c)) * (1.f / 16129.f)); }
+__device__ __forceinline__ float decode_u(uint32_t c, float scale) { return scale * ((float)(c * c) * (1.f / 65025.f)); }
+
+// The largest of a wavefront's values >= 0; a NaN counts as larger than all (the order of the bits).
+__device__ __forceinline__ float wave_max(float v)
+{
+    int b = __float_as_int(v);
+    for (int o = 32; o; o /= 2) b = max(b, __shfl_xor(b, o));
+    return __int_as_float(b);
+}
+
+// 1 / scale for values up to `scale`, times `up`; tiny scales, whose inverse is past the largest number, are lifted first.
+__device__ __forceinline__ float inverse(float scale, float &up)
+{
+    up = scale < 0x1p-100f ? 0x1p100f : 1.f;
+    return scale > 0.f ? 1.f / (scale * up) : 0.f;
+}
+
+template <typename TP, typename TG, int COUNT>
+__global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *tensors, const uint2 *pieces, uint32_t t0, Grads<COUNT> grads, AdamwStep s, int copy_type)
+{
+    const uint2 piece = pieces[blockIdx.x];
+    const AdamwTensor t = tensors[piece.x];
+    const TG *grad = (const TG *)grads.p[piece.x - t0];
+    if (!grad) return;
+    const Rates r = rates_of(s, t);
+    const int64_t first = (int64_t)piece.y * kAdamwPiece, last = min(first + kAdamwPiece, t.n);
+    const bool wide = wide_ok<TP, TG, uint8_t>(t, grad);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+#pragma unroll 2
+    for (int64_t b = first + wave * QRM_MOMENT_BLOCK; b < last; b += kThreads / 64 * QRM_MOMENT_BLOCK) {
+        const float sm = t.m_scale[b / QRM_MOMENT_BLOCK], su = t.v_scale[b / QRM_MOMENT_BLOCK];
+        const int64_t i = b + lane * 4;
+        Pack<TP, 4> p{};
+        Pack<TG, 4> g{};
+        Pack<int8_t, 4> cm{};
+        Pack<uint8_t, 4> cu{};
+        const bool whole = wide && b + QRM_MOMENT_BLOCK <= last;
+        if (whole) {
+            p = load_pack<TP, 4>((const TP *)t.p + i);
+            g = load_pack<TG, 4>(grad + i);
+            cm = load_pack<int8_t, 4>((const int8_t *)t.m + i);
+            cu = load_pack<uint8_t, 4>((const uint8_t *)t.v + i);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < last) {
+                    p.e[k] = ((const TP *)t.p)[i + k];
+                    g.e[k] = grad[i + k];
+                    cm.e[k] = ((const int8_t *)t.m)[i + k];
+                    cu.e[k] = ((const uint8_t *)t.v)[i + k];
+                }
+        }
+        float w[4], m[4], u[4], top_m = 0.f, top_u = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            w[k] = (float)p.e[k];
+            m[k] = decode_m(cm.e[k], sm);
+            const float root = decode_u(cu.e[k], su);
+            float v = root * root;
+            update(r, (float)g.e[k], w[k], m[k], v, u[k]);
+            p.e[k] = (TP)w[k];
+            if (i + k >= last) m[k] = u[k] = 0.f; // (an element that is not there: of weight nothing in the largest)
+            top_m = __int_as_float(max(__float_as_int(top_m), __float_as_int(fabsf(m[k]))));
+            top_u = __int_as_float(max(__float_as_int(top_u), __float_as_int(u[k])));
+        }
+        top_m = wave_max(top_m);
+        top_u = wave_max(top_u);
+        float up_m, up_u;
+        const float inv_m = inverse(top_m, up_m), inv_u = inverse(top_u, up_u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int am = (int)rintf(127.f * sqrtf(fabsf(m[k]) * up_m * inv_m));
+            cm.e[k] = (int8_t)(m[k] < 0.f ? -am : am);
+            const int au = (int)rintf(255.f * sqrtf(u[k] * up_u * inv_u));
+            cu.e[k] = (uint8_t)(u[k] > 0.f ? max(au, 1) : au);
+        }
+        if (whole) {
+            store_pack<TP, 4>((TP *)t.p + i, p);
+            store_pack<int8_t, 4>((int8_t *)t.m + i, cm);
+            store_pack<uint8_t, 4>((uint8_t *)t.v + i, cu);
+            if (t.copy) store_copy<4>(t.copy, copy_type, i, w);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < last) {
+                    ((TP *)t.p)[i + k] = p.e[k];
+                    ((int8_t *)t.m)[i + k] = cm.e[k];
+                    ((uint8_t *)t.v)[i + k] = cu.e[k];
+                    const float one[1] = {w[k]};
+                    if (t.copy) store_copy<1>(t.copy, copy_type, i + k, one);
+                }
+        }
+        if (lane == 0) {
+            t.m_scale[b / QRM_MOMENT_BLOCK] = top_m;
+            t.v_scale[b / QRM_MOMENT_BLOCK] = top_u;
+        }
+    }
+}
+
+// Four codes a thread, 1024 elements a workgroup.
+template <typename T> __global__ __launch_bounds__(kThreads) void unpack_moment_kernel(int moment, const uint8_t *codes, const float *scales, int64_t n, T *out)
+{
+    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
+    if (i >= n) return;
+    const float scale = scales[i / QRM_MOMENT_BLOCK];
+    auto value = [&](uint8_t c) {
+        if (moment == 0) return (T)decode_m((int8_t)c, scale);
+        const float u = decode_u(c, scale);
+        return (T)(u * u);
+    };
+    if (i + 4 <= n && aligned(codes, 4) && aligned(out, 4 * sizeof(T))) {
+        const Pack<uint8_t, 4> c = load_pack<uint8_t, 4>(codes + i);
+        Pack<T, 4> v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v.e[k] = value(c.e[k]);
+        store_pack<T, 4>(out + i, v);
+    } else {
+        for (int k = 0; k < 4 && i + k < n; ++k) out[i + k] = value(codes[i + k]);
+    }
+}
+
+template <int COUNT>
+hipError_t launch_counted(const AdamwTypes &t, const AdamwTensor *tensors, const uint2 *pieces, uint32_t count, uint32_t t0, const void *const *grads, int n_grads,
+                          const AdamwStep &step, hipStream_t s)
+{
+    Grads<COUNT> g;
+    for (int i = 0; i < COUNT; ++i) g.p[i] = i < n_grads ? grads[i] : nullptr;
+    return with_type(t.param, [&](auto *np) {
+        return with_type(t.grad, [&](auto *ng) {
+            using TP = std::remove_pointer_t<decltype(np)>;
+            using TG = std::remove_pointer_t<decltype(ng)>;
+            if (t.bits == 32)
+                hipLaunchKernelGGL((adamw_kernel<TP, TG, COUNT>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
+            else
+                hipLaunchKernelGGL((adamw8_kernel<TP, TG, COUNT>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
+            return hipGetLastError();
+        });
+    });
+}
+
+} // namespace
+
+hipError_t launch_adamw(const AdamwTypes &t, const AdamwTensor *tensors, const uint2 *pieces, uint32_t first, uint32_t count, uint32_t t0,
+                        const void *const *grads, int n_grads, const AdamwStep &step, hipStream_t s)
+{
+    // (arguments are copied at every launch: short lists take short ones)
+    return n_grads <= 32 ? launch_counted<32>(t, tensors, pieces + first, count, t0, grads, n_grads, step, s)
+                         : launch_counted<kAdamwGrads>(t, tensors, pieces + first, count, t0, grads, n_grads, step, s);
+}
+
+hipError_t launch_unpack_moment(int moment, const void *codes, const float *scales, int64_t n, int out_type, void *out, int, hipStream_t s)
+{
+    const dim3 grid((uint32_t)((n + 4 * kThreads - 1) / (4 * kThreads)));
+    if (out_type == QRM_F32)
+        hipLaunchKernelGGL(unpack_moment_kernel<float>, grid, dim3(kThreads), 0, s, moment, (const uint8_t *)codes, scales, n, (float *)out);
+    else
+        hipLaunchKernelGGL(unpack_moment_kernel<bf16_t>, grid, dim3(kThreads), 0, s, moment, (const uint8_t *)codes, scales, n, (bf16_t *)out);
+    return hipGetLastError();
+}
+
+} // namespace qrm

@@ -368,10 +368,6 @@ WsLayout ws_layout(const qrm_ctx *c, int64_t N, int h, int w, bool want_symbols,
     return L;
 }
 
-} // namespace qrm
-
-namespace {
-
 // Hands the caller's stream its workspace of at least `bytes` bytes.  A stream keeps its workspace from call
 // to call.  A stream not seen before takes a free one, or - when all are taken - the one whose last call lies
 // furthest back: the new stream is then made to wait (on the device) for that call to finish, so nothing is
@@ -436,6 +432,10 @@ qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s)
     if (e != hipSuccess) return hip_fail(c, e, "hipEventRecord");
     return QRM_OK;
 }
+
+} // namespace qrm
+
+namespace {
 
 // Event pair around one launch while profiling is on (null otherwise).
 qrm_ctx::Timed *time_begin(qrm_ctx *c, bool may_time, int kind, double flops, hipStream_t s)

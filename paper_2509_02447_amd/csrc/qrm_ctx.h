@@ -110,6 +110,10 @@ qrm_status run_extractor(qrm_ctx *c, uint8_t *base, ChainMemory &chain_memory, c
                          float *d_logits, uint8_t *d_bits, uint8_t *d_symbols, int m_sym, const WordArgs &word, float *d_act,
                          bool may_time, hipStream_t s);
 
+// The workspace of at least `bytes` bytes of the caller's stream, and what goes behind the last kernel that uses it.
+qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out);
+qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s);
+
 // QRM_E_DEVICE, once, if an earlier call's launch has lost images.
 qrm_status report_lost(qrm_ctx *c);
 
