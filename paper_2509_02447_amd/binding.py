@@ -469,20 +469,22 @@ class AdamW:
                           {torch.float32: 32, torch.int8: 8}[moment])
         ctx._check(self._lib.qrm_adamw_create(ctx._h, C.byref(desc), rows, C.byref(self._h)))
         self._n, self._grad_type, self._sizes = n, grad_type, [t["param"].numel() for t in self._keep]
+        self._array = C.c_void_p * max(1, n)
 
     @staticmethod
     def _mixed(what):
         raise ValueError(f"all {what} of a plan have one type")
 
+    def _grad(self, g, n):
+        assert g.dtype is self._grad_type and g.numel() == n, "a gradient has the wrong type or size"
+        assert g.is_cuda and g.is_contiguous(), "device tensors must be contiguous and on the GPU"
+        return g.data_ptr()
+
     def qrm_adamw_step(self, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                        d_grad_scale=None, stream=None):
         """grads: one device tensor of grad_type for each tensor of the plan, or None where it has no gradient."""
         assert len(grads) == self._n, "one gradient (or None) for each tensor"
-        ptrs = (C.c_void_p * max(1, self._n))()
-        for i, g in enumerate(grads):
-            if g is not None:
-                assert g.dtype == self._grad_type and g.numel() == self._sizes[i], "a gradient has the wrong type or size"
-                ptrs[i] = _dptr(g)
+        ptrs = self._array(*[None if g is None else self._grad(g, n) for g, n in zip(grads, self._sizes)])
         self._ctx._check(self._lib.qrm_adamw_step(self._ctx._h, self._h, ptrs, int(step), float(lr), float(beta1), float(beta2),
                                                   float(eps), _dptr(d_grad_scale), _stream_handle(stream)))
 

@@ -25,13 +25,11 @@ __device__ __forceinline__ Rates rates_of(const AdamwStep &s, const AdamwTensor 
     return Rates{s.beta1, s.rest1, s.beta2, s.rest2, s.eps, 1.f - s.lr * t.lr_scale * t.weight_decay, s.rate * t.lr_scale, s.root, s.grad_scale ? *s.grad_scale : 1.f};
 }
 
-__device__ __forceinline__ void update(const Rates &r, float g, float &p, float &m, float &v, float &u)
+__device__ __forceinline__ void moments(const Rates &r, float g, float &m, float &v)
 {
     g *= r.scale;
     m = m * r.beta1 + g * r.rest1;
     v = v * r.beta2 + g * g * r.rest2;
-    u = sqrtf(v);
-    p = p * r.keep - r.rate * (m / (u * r.root + r.eps));
 }
 
 template <int V> __device__ __forceinline__ void store_copy(void *copy, int type, int64_t i, const float (&p)[V])
@@ -58,9 +56,8 @@ template <typename TP, typename TG, int V> __device__ __forceinline__ void step_
     float w[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        float u;
-        w[k] = (float)p.e[k];
-        update(r, (float)g.e[k], w[k], m.e[k], v.e[k], u);
+        moments(r, (float)g.e[k], m.e[k], v.e[k]);
+        w[k] = (float)p.e[k] * r.keep - r.rate * (m.e[k] / (sqrtf(v.e[k]) * r.root + r.eps));
         q.e[k] = (TP)w[k];
     }
     store_pack<TP, V>((TP *)t.p + i, q);
@@ -110,11 +107,17 @@ __device__ __forceinline__ float wave_max(float v)
     return __int_as_float(b);
 }
 
-// 1 / scale for values up to `scale`, times `up`; tiny scales, whose inverse is past the largest number, are lifted first.
+// Here and below the hardware's roots and inverses are taken as they are (1 ulp): rounded exactly, they would make this kernel's arithmetic as long
+// as its memory's time.  They know no numbers below 2^-126, so what may be there is lifted first.
+__device__ __forceinline__ float root_of(float v)
+{
+    return v >= 0x1p-100f ? __builtin_amdgcn_sqrtf(v) : sqrtf(v);
+}
+// 1 / scale / up for values up to `scale`, which are multiplied by `up` first.
 __device__ __forceinline__ float inverse(float scale, float &up)
 {
     up = scale < 0x1p-100f ? 0x1p100f : 1.f;
-    return scale > 0.f ? 1.f / (scale * up) : 0.f;
+    return scale > 0.f ? __builtin_amdgcn_rcpf(scale * up) : 0.f;
 }
 
 template <typename TP, typename TG, int COUNT>
@@ -128,7 +131,6 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
     const int64_t first = (int64_t)piece.y * kAdamwPiece, last = min(first + kAdamwPiece, t.n);
     const bool wide = wide_ok<TP, TG, uint8_t>(t, grad);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-#pragma unroll 2
     for (int64_t b = first + wave * QRM_MOMENT_BLOCK; b < last; b += kThreads / 64 * QRM_MOMENT_BLOCK) {
         const float sm = t.m_scale[b / QRM_MOMENT_BLOCK], su = t.v_scale[b / QRM_MOMENT_BLOCK];
         const int64_t i = b + lane * 4;
@@ -159,7 +161,9 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
             m[k] = decode_m(cm.e[k], sm);
             const float root = decode_u(cu.e[k], su);
             float v = root * root;
-            update(r, (float)g.e[k], w[k], m[k], v, u[k]);
+            moments(r, (float)g.e[k], m[k], v);
+            u[k] = root_of(v);
+            w[k] = w[k] * r.keep - r.rate * (m[k] * __builtin_amdgcn_rcpf(u[k] * r.root + r.eps));
             p.e[k] = (TP)w[k];
             if (i + k >= last) m[k] = u[k] = 0.f; // (an element that is not there: of weight nothing in the largest)
             top_m = __int_as_float(max(__float_as_int(top_m), __float_as_int(fabsf(m[k]))));
@@ -171,9 +175,9 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
         const float inv_m = inverse(top_m, up_m), inv_u = inverse(top_u, up_u);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int am = (int)rintf(127.f * sqrtf(fabsf(m[k]) * up_m * inv_m));
+            const int am = (int)rintf(127.f * __builtin_amdgcn_sqrtf(fabsf(m[k]) * up_m * inv_m));
             cm.e[k] = (int8_t)(m[k] < 0.f ? -am : am);
-            const int au = (int)rintf(255.f * sqrtf(u[k] * up_u * inv_u));
+            const int au = (int)rintf(255.f * __builtin_amdgcn_sqrtf(u[k] * up_u * inv_u));
             cu.e[k] = (uint8_t)(u[k] > 0.f ? max(au, 1) : au);
         }
         if (whole) {
@@ -199,10 +203,11 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
     }
 }
 
-// Four codes a thread, 1024 elements a workgroup.
+// Sixteen codes a thread, 4096 a workgroup.
+constexpr int kUnpack = 16;
 template <typename T> __global__ __launch_bounds__(kThreads) void unpack_moment_kernel(int moment, const uint8_t *codes, const float *scales, int64_t n, T *out)
 {
-    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
+    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kUnpack;
     if (i >= n) return;
     const float scale = scales[i / QRM_MOMENT_BLOCK];
     auto value = [&](uint8_t c) {
@@ -210,14 +215,18 @@ template <typename T> __global__ __launch_bounds__(kThreads) void unpack_moment_
         const float u = decode_u(c, scale);
         return (T)(u * u);
     };
-    if (i + 4 <= n && aligned(codes, 4) && aligned(out, 4 * sizeof(T))) {
-        const Pack<uint8_t, 4> c = load_pack<uint8_t, 4>(codes + i);
-        Pack<T, 4> v;
+    if (i + kUnpack <= n && aligned(codes, kUnpack) && aligned(out, 16)) {
+        constexpr int V = 16 / sizeof(T);
+        const Pack<uint8_t, kUnpack> c = load_pack<uint8_t, kUnpack>(codes + i);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v.e[k] = value(c.e[k]);
-        store_pack<T, 4>(out + i, v);
+        for (int j = 0; j < kUnpack; j += V) {
+            Pack<T, V> v;
+#pragma unroll
+            for (int k = 0; k < V; ++k) v.e[k] = value(c.e[j + k]);
+            store_pack<T, V>(out + i + j, v);
+        }
     } else {
-        for (int k = 0; k < 4 && i + k < n; ++k) out[i + k] = value(codes[i + k]);
+        for (int k = 0; k < kUnpack && i + k < n; ++k) out[i + k] = value(codes[i + k]);
     }
 }
 
@@ -252,7 +261,7 @@ hipError_t launch_adamw(const AdamwTypes &t, const AdamwTensor *tensors, const u
 
 hipError_t launch_unpack_moment(int moment, const void *codes, const float *scales, int64_t n, int out_type, void *out, int, hipStream_t s)
 {
-    const dim3 grid((uint32_t)((n + 4 * kThreads - 1) / (4 * kThreads)));
+    const dim3 grid((uint32_t)((n + kUnpack * kThreads - 1) / (kUnpack * kThreads)));
     if (out_type == QRM_F32)
         hipLaunchKernelGGL(unpack_moment_kernel<float>, grid, dim3(kThreads), 0, s, moment, (const uint8_t *)codes, scales, n, (float *)out);
     else

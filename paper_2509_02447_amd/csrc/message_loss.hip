@@ -1,7 +1,8 @@
 // Message loss with its gradient (qrm_message_loss).
 //
 // A lane takes a symbol, 2^k lanes an image: the image's expected number of wrong symbols, which every bit's gradient depends on, is a sum over
-// neighbouring lanes.  Bound by launch latency up to thousands of images, by memory beyond (9 bytes a bit).
+// neighbouring lanes.  Workgroups leave their part of the loss in 64 bits; the last one that is done adds them up, in their order.  Bound by launch
+// latency up to thousands of images, by memory beyond (9 bytes a bit).
 #include "qrm_train.h"
 
 #include <algorithm>
@@ -10,7 +11,8 @@
 namespace qrm {
 namespace {
 
-constexpr int kThreads = 256, kSmallThreads = 1024;
+constexpr int kThreads = 1024;
+constexpr int kVm0 = (7 << 4) | (15 << 8); // s_waitcnt vmcnt(0) alone
 
 struct LossArgs {
     const float *logits;
@@ -20,11 +22,13 @@ struct LossArgs {
     float weight, per_bit, per_image; // 1 / (N n_bits), weight / N
     float *loss, *grad;
     int32_t *bit_errors, *symbol_errors;
-    double *partial; // [workgroups], or null: one workgroup, which writes the loss
+    bool wide;       // logits and gradients lie on 16-byte boundaries
+    double *partial; // [workgroups], unless there is only one
+    uint32_t *done;  // workgroups that are; 0 between calls
 };
 
 template <int M> struct Symbol {
-    float x[M];        // logits, turned so that the right side is above zero
+    float miss[M];     // chance that a bit is wrong
     uint32_t ones;     // target bits
     int wrong;         // hard bits that differ
     float bce, right;  // sum of -log sigmoid(x); chance that all bits are right
@@ -32,33 +36,60 @@ template <int M> struct Symbol {
 
 template <int M> __device__ __forceinline__ Symbol<M> read_symbol(const LossArgs &a, int64_t image, int j)
 {
+    constexpr int V = M % 4 == 0 ? 4 : 1;
     Symbol<M> s;
     const float *z = a.logits + image * a.n_bits + j * M;
     const uint8_t *target = a.target + image * a.target_stride + j * M;
+    float v[M];
+#pragma unroll
+    for (int b = 0; b < M; b += V) {
+        if (V == 4 && a.wide) {
+            const Pack<float, V> p = load_pack<float, V>(z + b);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[b + k] = p.e[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[b + k] = z[b + k];
+        }
+    }
     s.ones = 0;
     s.wrong = 0;
     s.bce = 0.f;
+    s.right = 1.f;
 #pragma unroll
     for (int b = 0; b < M; ++b) {
         const bool one = target[b] != 0;
-        const float v = z[b];
         s.ones |= (uint32_t)one << b;
-        s.wrong += (v > 0.f) != one;
-        s.x[b] = one ? v : -v;
-        s.bce += (s.x[b] > 0.f ? 0.f : -s.x[b]) + log1pf(expf(-fabsf(s.x[b])));
+        s.wrong += (v[b] > 0.f) != one;
+        // x = s * logit; sigmoid(x) and sigmoid(-x) from e = exp(-|x|) <= 1.  The hardware's functions are within 1 ulp, but know no numbers below 2^-126.
+        const float x = one ? v[b] : -v[b], far = fabsf(x);
+        const float e = far < 80.f ? __builtin_amdgcn_exp2f(far * -1.44269504f) : expf(-far), w = 1.f + e, r = __builtin_amdgcn_rcpf(w);
+        const bool good = x >= 0.f;
+        s.miss[b] = good ? e * r : r;
+        s.right *= good ? r : e * r;
+        // log(1 + e): the logarithm of the rounded sum and, to first order, of what the rounding left out
+        const float rest = e - (w - 1.f), log1 = fmaf(rest, r, __builtin_amdgcn_logf(w) * 0.693147181f);
+        s.bce += (x > 0.f ? 0.f : -x) + log1; // (a NaN stays one)
     }
-    s.right = expf(-s.bce);
     return s;
 }
 
 template <int M> __device__ __forceinline__ void write_grad(const LossArgs &a, int64_t image, int j, const Symbol<M> &s, float over)
 {
+    constexpr int V = M % 4 == 0 ? 4 : 1;
     float *g = a.grad + image * a.n_bits + j * M;
     const float pull = a.per_bit + 2.f * a.per_image * over * s.right;
 #pragma unroll
-    for (int b = 0; b < M; ++b) {
-        const float e = expf(-fabsf(s.x[b])), miss = (s.x[b] >= 0.f ? e : 1.f) / (1.f + e);
-        g[b] = (s.ones >> b & 1 ? -miss : miss) * pull;
+    for (int b = 0; b < M; b += V) {
+        Pack<float, V> p;
+#pragma unroll
+        for (int k = 0; k < V; ++k) p.e[k] = (s.ones >> (b + k) & 1 ? -pull : pull) * s.miss[b + k];
+        if (V == 4 && a.wide) {
+            store_pack<float, V>(g + b, p);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) g[b + k] = p.e[k];
+        }
     }
 }
 
@@ -69,9 +100,10 @@ template <typename T> __device__ __forceinline__ T lanes_sum(T v, int lanes)
     return v;
 }
 
-template <int M> __global__ __launch_bounds__(kSmallThreads) void message_loss_kernel(LossArgs a)
+template <int M> __global__ __launch_bounds__(kThreads) void message_loss_kernel(LossArgs a)
 {
-    __shared__ double sums[kSmallThreads / 64];
+    __shared__ double sums[kThreads / 64];
+    __shared__ bool last;
     const int lane = threadIdx.x & (a.lanes - 1), per = blockDim.x / a.lanes;
     double total = 0.0;
     // the loop is the same for all lanes of a wavefront: those of images past the last one compute nothing
@@ -104,25 +136,32 @@ template <int M> __global__ __launch_bounds__(kSmallThreads) void message_loss_k
             total += (double)bce * a.per_bit + (double)over * over * a.per_image;
         }
     }
-    total = lanes_sum(total, 64);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < blockDim.x / 64; ++w) total += sums[w];
-        if (a.partial) a.partial[blockIdx.x] = total;
-        else *a.loss = (float)total;
+    auto add_up = [&](double v) { // over the workgroup; thread 0 has the sum
+        v = lanes_sum(v, 64);
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = v;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            for (int w = 1; w < (int)blockDim.x / 64; ++w) v += sums[w];
+        return v;
+    };
+    total = add_up(total);
+    if (gridDim.x == 1) {
+        if (threadIdx.x == 0) *a.loss = (float)total;
+        return;
     }
-}
-
-__global__ __launch_bounds__(256) void loss_sum_kernel(const double *partial, int count, float *loss)
-{
-    __shared__ double sums[4];
-    double s = 0.0;
-    for (int i = threadIdx.x; i < count; i += 256) s += partial[i];
-    s = lanes_sum(s, 64);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = s;
+    // parts and count are stored past the L2s; a part has arrived before its workgroup is counted
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(a.partial + blockIdx.x, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __builtin_amdgcn_s_waitcnt(kVm0);
+        last = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
+        if (last) __hip_atomic_store(a.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     __syncthreads();
-    if (threadIdx.x == 0) *loss = (float)(sums[0] + sums[1] + sums[2] + sums[3]);
+    if (!last) return;
+    total = 0.0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += blockDim.x) total += __hip_atomic_load(a.partial + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    total = add_up(total);
+    if (threadIdx.x == 0) *a.loss = (float)total;
 }
 
 int lanes_of(int n)
@@ -134,21 +173,22 @@ int lanes_of(int n)
 
 } // namespace
 
-// Workgroups of a call; one of 1024 threads up to four images a lane group, then no second launch is needed.
+// Workgroups of a call: one for up to four images a lane group of 1024 threads, else at most 256, whose counting takes a microsecond.
 int64_t loss_blocks(int64_t N, int n)
 {
-    const int lanes = lanes_of(n);
-    if (N <= 4 * (kSmallThreads / lanes)) return 1;
-    return std::min<int64_t>((N + kThreads / lanes - 1) / (kThreads / lanes), 2048);
+    const int64_t per = kThreads / lanes_of(n);
+    return N <= 4 * per ? 1 : std::min<int64_t>((N + per - 1) / per, 256);
 }
 
-hipError_t launch_message_loss(const LossCall &c, double *partial, hipStream_t s)
+hipError_t launch_message_loss(const LossCall &c, double *partial, uint32_t *done, hipStream_t s)
 {
     const int64_t blocks = loss_blocks(c.N, c.n);
     const double images = c.N ? (double)c.N : 1.0;
-    LossArgs a{c.logits, c.target, c.target_stride, c.N, c.n_bits, c.n, c.t, lanes_of(c.n), c.weight, (float)(1.0 / (images * c.n_bits)),
-               (float)(c.weight / images), c.loss, c.grad, c.bit_errors, c.symbol_errors, blocks > 1 ? partial : nullptr};
-    const dim3 grid((uint32_t)blocks), block(blocks > 1 ? kThreads : kSmallThreads);
+    const int lanes = lanes_of(c.n);
+    const bool wide = ((uintptr_t)c.logits | (uintptr_t)c.grad) % 16 == 0;
+    LossArgs a{c.logits, c.target, c.target_stride, c.N, c.n_bits, c.n, c.t, lanes, c.weight, (float)(1.0 / (images * c.n_bits)),
+               (float)(c.weight / images), c.loss, c.grad, c.bit_errors, c.symbol_errors, wide, partial, done};
+    const dim3 grid((uint32_t)blocks), block(blocks > 1 ? kThreads : (int)std::min<int64_t>(kThreads, std::max<int64_t>(1, (c.N * lanes + 63) / 64) * 64));
     auto run = [&](auto m) { hipLaunchKernelGGL((message_loss_kernel<decltype(m)::value>), grid, block, 0, s, a); };
     switch (c.m) {
     case 1: run(std::integral_constant<int, 1>()); break;
@@ -160,9 +200,6 @@ hipError_t launch_message_loss(const LossCall &c, double *partial, hipStream_t s
     case 7: run(std::integral_constant<int, 7>()); break;
     default: run(std::integral_constant<int, 8>()); break;
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || blocks == 1) return e;
-    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(256), 0, s, partial, (int)blocks, c.loss);
     return hipGetLastError();
 }
 

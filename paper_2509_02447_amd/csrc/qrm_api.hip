@@ -383,7 +383,12 @@ qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
         if (!slot)
             for (auto &sl : c->slots)
                 if (!slot || sl.last_use < slot->last_use) slot = &sl;
-        if (slot->done && slot->last_use) {
+        if (slot->unmarked) {
+            // (its stream may be gone: there is nothing else to wait for)
+            hipError_t e = hipDeviceSynchronize();
+            if (e != hipSuccess) return hip_fail(c, e, "hipDeviceSynchronize(workspace hand-over)");
+            slot->unmarked = false;
+        } else if (slot->done && slot->last_use) {
             hipError_t e = hipStreamWaitEvent(s, slot->done, 0);
             if (e != hipSuccess) return hip_fail(c, e, "hipStreamWaitEvent(workspace hand-over)");
         }
@@ -425,11 +430,29 @@ qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
     return QRM_OK;
 }
 
+qrm_status get_counters(qrm_ctx *c, hipStream_t s, QrmSlot *slot)
+{
+    if (slot->counters) return QRM_OK;
+    void *p = nullptr;
+    if (hipMalloc(&p, kSlotCounters * sizeof(uint32_t)) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(c, QRM_E_NOMEM, "no device memory for a workspace's counters");
+    }
+    const hipError_t e = hipMemsetAsync(p, 0, kSlotCounters * sizeof(uint32_t), s); // (never in a graph: nothing can be allocated while one is recorded)
+    if (e != hipSuccess) {
+        (void)hipFree(p);
+        return hip_fail(c, e, "hipMemsetAsync(counters)");
+    }
+    slot->counters = (uint32_t *)p;
+    return QRM_OK;
+}
+
 // behind the last kernel of a call: whoever takes the workspace over waits for this
 qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s)
 {
     hipError_t e = hipEventRecord(slot->done, s);
     if (e != hipSuccess) return hip_fail(c, e, "hipEventRecord");
+    slot->unmarked = false; // (short calls before this one are on the same stream)
     return QRM_OK;
 }
 
@@ -790,11 +813,13 @@ void qrm_destroy(qrm_ctx *c)
     (void)hipSetDevice(c->device);
     for (auto &sl : c->slots) {
         // the caller's stream may be gone by now: the event behind the workspace's last call is what is waited for
+        if (sl.unmarked) (void)hipDeviceSynchronize();
         if (sl.done) {
             if (sl.last_use) (void)hipEventSynchronize(sl.done);
             (void)hipEventDestroy(sl.done);
         }
         if (sl.ws) (void)hipFree(sl.ws);
+        if (sl.counters) (void)hipFree(sl.counters);
     }
     for (auto &t : c->timed) {
         (void)hipEventDestroy(t.start);
@@ -830,6 +855,11 @@ qrm_status qrm_release_stream(qrm_ctx *c, void *stream)
             if (sl.done && sl.last_use) {
                 e = hipEventSynchronize(sl.done);
                 if (e != hipSuccess) return hip_fail(c, e, "hipEventSynchronize");
+            }
+            if (sl.unmarked) {
+                e = hipStreamSynchronize(sl.stream);
+                if (e != hipSuccess) return hip_fail(c, e, "hipStreamSynchronize");
+                sl.unmarked = false;
             }
             sl.used = false;
             sl.stream = nullptr;

@@ -17,6 +17,8 @@ struct ChainMemory {
     bool dirty = false;
 };
 
+constexpr int kSlotCounters = 1024;
+
 // A workspace of the context: the device memory the kernels of one caller stream work in.
 struct QrmSlot {
     bool used = false;
@@ -24,7 +26,9 @@ struct QrmSlot {
     void *ws = nullptr;
     size_t bytes = 0;
     ChainMemory chain;            // its own, for as long as the context lives
+    uint32_t *counters = nullptr; // kSlotCounters, all zero between calls: how many workgroups of a launch are done (get_counters)
     hipEvent_t done = nullptr;    // recorded behind the last kernel of every call that used the workspace
+    bool unmarked = false;        // .. but for those of short calls, for which recording an event would cost as much as a launch (slot_used)
     uint64_t last_use = 0;        // value of the context's call counter at that call
 };
 
@@ -113,6 +117,10 @@ qrm_status run_extractor(qrm_ctx *c, uint8_t *base, ChainMemory &chain_memory, c
 // The workspace of at least `bytes` bytes of the caller's stream, and what goes behind the last kernel that uses it.
 qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out);
 qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s);
+// The counters of a slot, allocated at their first use.
+qrm_status get_counters(qrm_ctx *c, hipStream_t s, QrmSlot *slot);
+// .. of a short call: nothing is recorded, and who takes the workspace over, frees or gives it back waits for the device or the stream instead.
+inline void slot_used(QrmSlot *slot) { slot->unmarked = true; }
 
 // QRM_E_DEVICE, once, if an earlier call's launch has lost images.
 qrm_status report_lost(qrm_ctx *c);

@@ -64,11 +64,11 @@ qrm_status start(qrm_ctx *c)
     return e == hipSuccess ? QRM_OK : hip_fail(c, e, "hipSetDevice");
 }
 
-qrm_status plan(qrm_ctx *c, const qrm_group_norm_desc &d, int align, bool backward, NormPlan *p)
+qrm_status plan(qrm_ctx *c, const qrm_group_norm_desc &d, int align, bool backward, bool channels, NormPlan *p)
 {
-    if (!plan_norm(d, align, backward, c->num_cu, p))
+    if (!plan_norm(d, align, backward, channels, c->num_cu, p))
         return fail(c, QRM_E_UNSUPPORTED, "a group has more than 1024 pieces of what the alignment allows to read at once");
-    if ((double)d.N * p->tiles * p->chunks > 2e9) return fail(c, QRM_E_UNSUPPORTED, "more than 2^31 tiles");
+    if ((double)d.N * p->first.tiles * p->first.chunks > 2e9 || (!p->whole && (double)d.N * p->second.tiles * p->second.chunks > 2e9)) return fail(c, QRM_E_UNSUPPORTED, "more than 2^31 tiles");
     return QRM_OK;
 }
 
@@ -90,13 +90,14 @@ qrm_status qrm_group_norm(qrm_ctx *c, const qrm_group_norm_desc *desc, const voi
     if (align < type_bytes(call.d.type) || !aligned_to(d_gamma, 4) || !aligned_to(d_beta, 4) || !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4))
         return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
     NormPlan p;
-    if ((st = plan(c, call.d, align, false, &p)) != QRM_OK || (st = start(c)) != QRM_OK) return st;
+    if ((st = plan(c, call.d, align, false, false, &p)) != QRM_OK || (st = start(c)) != QRM_OK) return st;
     call.x = d_x; call.y = d_y; call.gamma = d_gamma; call.beta = d_beta; call.mean = d_mean; call.rstd = d_rstd;
-    QrmSlot *slot;
-    if ((st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
-    hipError_t e = launch_norm_forward(call, p, slot->ws, (hipStream_t)stream);
+    QrmSlot *slot = nullptr;
+    if (p.bytes && (st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
+    hipError_t e = launch_norm_forward(call, p, slot ? slot->ws : nullptr, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(c, e, "group_norm launch");
-    return slot_done(c, slot, (hipStream_t)stream);
+    if (slot) slot_used(slot);
+    return QRM_OK;
 }
 
 qrm_status qrm_group_norm_backward(qrm_ctx *c, const qrm_group_norm_desc *desc, const void *d_x, const void *d_dy, const float *d_gamma,
@@ -123,12 +124,13 @@ qrm_status qrm_group_norm_backward(qrm_ctx *c, const qrm_group_norm_desc *desc, 
         hipError_t e = launch_norm_backward(call, p, nullptr, (hipStream_t)stream);
         return e == hipSuccess ? QRM_OK : hip_fail(c, e, "group_norm_backward launch");
     }
-    if ((st = plan(c, call.d, align, true, &p)) != QRM_OK || (st = start(c)) != QRM_OK) return st;
-    QrmSlot *slot;
-    if ((st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
-    hipError_t e = launch_norm_backward(call, p, slot->ws, (hipStream_t)stream);
+    if ((st = plan(c, call.d, align, true, d_dgamma || d_dbeta, &p)) != QRM_OK || (st = start(c)) != QRM_OK) return st;
+    QrmSlot *slot = nullptr;
+    if (p.bytes && (st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
+    hipError_t e = launch_norm_backward(call, p, slot ? slot->ws : nullptr, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(c, e, "group_norm_backward launch");
-    return slot_done(c, slot, (hipStream_t)stream);
+    if (slot) slot_used(slot);
+    return QRM_OK;
 }
 
 qrm_status qrm_adamw_create(qrm_ctx *c, const qrm_adamw_desc *desc, const qrm_adamw_tensor *h_tensors, qrm_adamw **out)
@@ -281,10 +283,13 @@ qrm_status qrm_message_loss(qrm_ctx *c, const float *d_logits, const uint8_t *d_
                   c->has_rs ? c->rs.two_t / 2 : 0, rs_weight, d_loss, d_grad, d_bit_errors, d_symbol_errors};
     const int64_t blocks = loss_blocks(N, call.n);
     QrmSlot *slot = nullptr;
-    if (blocks > 1 && (st = get_slot(c, (hipStream_t)stream, (size_t)blocks * sizeof(double), &slot)) != QRM_OK) return st;
-    hipError_t e = launch_message_loss(call, slot ? (double *)slot->ws : nullptr, (hipStream_t)stream);
+    if (blocks > 1 && ((st = get_slot(c, (hipStream_t)stream, (size_t)blocks * sizeof(double), &slot)) != QRM_OK ||
+                       (st = get_counters(c, (hipStream_t)stream, slot)) != QRM_OK))
+        return st;
+    hipError_t e = launch_message_loss(call, slot ? (double *)slot->ws : nullptr, slot ? slot->counters : nullptr, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(c, e, "message_loss launch");
-    return slot ? slot_done(c, slot, (hipStream_t)stream) : QRM_OK;
+    if (slot) slot_used(slot);
+    return QRM_OK;
 }
 
 } // extern "C"
