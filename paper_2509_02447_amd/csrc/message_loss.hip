@@ -34,6 +34,23 @@ template <int M> struct Symbol {
     float bce, right;  // sum of -log sigmoid(x); chance that all bits are right
 };
 
+// sigmoid(x) and sigmoid(-x) of a symbol's bits from e = exp(-|x|) <= 1.
+template <int M, bool FAR> __device__ __forceinline__ void chances(Symbol<M> &s, const float (&x)[M])
+{
+    s.bce = 0.f;
+    s.right = 1.f;
+#pragma unroll
+    for (int b = 0; b < M; ++b) {
+        const float e = FAR ? expf(-fabsf(x[b])) : __builtin_amdgcn_exp2f(fabsf(x[b]) * -1.44269504f), w = 1.f + e, r = __builtin_amdgcn_rcpf(w);
+        const bool good = x[b] >= 0.f;
+        const float q = e * r;
+        s.miss[b] = good ? q : r;
+        s.right *= good ? r : q;
+        // log(1 + e): the logarithm of the rounded sum and, to first order, of what the rounding left out
+        s.bce += fmaf(e - (w - 1.f), r, __builtin_amdgcn_logf(w) * 0.693147181f) + (x[b] > 0.f ? 0.f : -x[b]); // (a NaN stays one)
+    }
+}
+
 template <int M> __device__ __forceinline__ Symbol<M> read_symbol(const LossArgs &a, int64_t image, int j)
 {
     constexpr int V = M % 4 == 0 ? 4 : 1;
@@ -54,23 +71,18 @@ template <int M> __device__ __forceinline__ Symbol<M> read_symbol(const LossArgs
     }
     s.ones = 0;
     s.wrong = 0;
-    s.bce = 0.f;
-    s.right = 1.f;
+    float farthest = 0.f;
 #pragma unroll
     for (int b = 0; b < M; ++b) {
         const bool one = target[b] != 0;
         s.ones |= (uint32_t)one << b;
         s.wrong += (v[b] > 0.f) != one;
-        // x = s * logit; sigmoid(x) and sigmoid(-x) from e = exp(-|x|) <= 1.  The hardware's functions are within 1 ulp, but know no numbers below 2^-126.
-        const float x = one ? v[b] : -v[b], far = fabsf(x);
-        const float e = far < 80.f ? __builtin_amdgcn_exp2f(far * -1.44269504f) : expf(-far), w = 1.f + e, r = __builtin_amdgcn_rcpf(w);
-        const bool good = x >= 0.f;
-        s.miss[b] = good ? e * r : r;
-        s.right *= good ? r : e * r;
-        // log(1 + e): the logarithm of the rounded sum and, to first order, of what the rounding left out
-        const float rest = e - (w - 1.f), log1 = fmaf(rest, r, __builtin_amdgcn_logf(w) * 0.693147181f);
-        s.bce += (x > 0.f ? 0.f : -x) + log1; // (a NaN stays one)
+        v[b] = one ? v[b] : -v[b]; // x = s * logit
+        farthest = fmaxf(farthest, fabsf(v[b]));
     }
+    // The hardware's functions are within 1 ulp, but know no numbers below 2^-126: symbols with a logit that far off take the library's.
+    if (farthest < 80.f) chances<M, false>(s, v);
+    else chances<M, true>(s, v);
     return s;
 }
 
@@ -93,11 +105,28 @@ template <int M> __device__ __forceinline__ void write_grad(const LossArgs &a, i
     }
 }
 
-// Sum over `lanes` neighbouring lanes, the same bits in each.
+// v plus that of another lane of the row of 16, which CTRL picks.
+template <int CTRL, typename T> __device__ __forceinline__ T add_lane(T v)
+{
+    return v + __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// Sum over `lanes` neighbouring lanes, the same bits in each: pairs, fours, halves of a row and rows by lane moves in the vector unit.
 template <typename T> __device__ __forceinline__ T lanes_sum(T v, int lanes)
 {
-    for (int o = lanes / 2; o; o /= 2) v += __shfl_xor(v, o, 64);
+    if (lanes > 1) v = add_lane<0xB1>(v);   // quad_perm [1,0,3,2]
+    if (lanes > 2) v = add_lane<0x4E>(v);   // quad_perm [2,3,0,1]
+    if (lanes > 4) v = add_lane<0x141>(v);  // row_half_mirror
+    if (lanes > 8) v = add_lane<0x140>(v);  // row_mirror
+    if (lanes > 16) v += __shfl_xor(v, 16);
+    if (lanes > 32) v += __shfl_xor(v, 32);
     return v;
+}
+// A barrier for shared memory alone: stores to memory may be under way.
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 template <int M> __global__ __launch_bounds__(kThreads) void message_loss_kernel(LossArgs a)
@@ -106,47 +135,52 @@ template <int M> __global__ __launch_bounds__(kThreads) void message_loss_kernel
     __shared__ bool last;
     const int lane = threadIdx.x & (a.lanes - 1), per = blockDim.x / a.lanes;
     double total = 0.0;
+    Symbol<M> mine; // this lane's first symbol stays, further ones (n > 64) are read again for the gradient
+    float over = 0.f;
+    int64_t image = a.N;
+    auto write_image = [&] {
+        if (a.grad && image < a.N)
+            for (int j = lane; j < a.n; j += a.lanes) write_grad<M>(a, image, j, j == lane ? mine : read_symbol<M>(a, image, j), over);
+    };
     // the loop is the same for all lanes of a wavefront: those of images past the last one compute nothing
     for (int64_t first = (int64_t)blockIdx.x * per; first < a.N; first += (int64_t)gridDim.x * per) {
-        const int64_t image = first + threadIdx.x / a.lanes;
+        write_image(); // the last round's: this round's waits until the part of the loss is on its way
+        image = first + threadIdx.x / a.lanes;
         const bool here = image < a.N;
-        Symbol<M> mine; // this lane's first symbol stays, further ones (n > 64) are read again for the gradient
         float wrong = 0.f, bce = 0.f;
-        int bits = 0, symbols = 0;
+        int errors = 0; // bits, and in the upper half symbols
         if (here)
             for (int j = lane; j < a.n; j += a.lanes) {
                 const Symbol<M> s = read_symbol<M>(a, image, j);
                 if (j == lane) mine = s;
                 wrong += 1.f - s.right;
                 bce += s.bce;
-                bits += s.wrong;
-                symbols += s.wrong != 0;
+                errors += s.wrong + (s.wrong ? 0x10000 : 0);
             }
         wrong = lanes_sum(wrong, a.lanes);
         bce = lanes_sum(bce, a.lanes);
-        bits = lanes_sum(bits, a.lanes);
-        symbols = lanes_sum(symbols, a.lanes);
-        const float excess = wrong - (float)a.t, over = a.weight > 0.f && !(excess <= 0.f) ? excess : 0.f;
-        if (!here) continue;
-        if (a.grad)
-            for (int j = lane; j < a.n; j += a.lanes) write_grad<M>(a, image, j, j == lane ? mine : read_symbol<M>(a, image, j), over);
-        if (lane == 0) {
-            if (a.bit_errors) a.bit_errors[image] = bits;
-            if (a.symbol_errors) a.symbol_errors[image] = symbols;
+        errors = lanes_sum(errors, a.lanes);
+        const float excess = wrong - (float)a.t;
+        over = a.weight > 0.f && !(excess <= 0.f) ? excess : 0.f;
+        if (here && lane == 0) {
+            if (a.bit_errors) a.bit_errors[image] = errors & 0xffff;
+            if (a.symbol_errors) a.symbol_errors[image] = errors >> 16;
             total += (double)bce * a.per_bit + (double)over * over * a.per_image;
         }
     }
-    auto add_up = [&](double v) { // over the workgroup; thread 0 has the sum
-        v = lanes_sum(v, 64);
+    auto add_up = [&](double v, int apart) { // over the workgroup, of lanes `apart`; thread 0 has the sum
+        for (int o = 32; o >= apart; o /= 2) v += __shfl_down(v, o);
+        if (blockDim.x == 64) return v;
         if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = v;
-        __syncthreads();
+        lds_barrier();
         if (threadIdx.x == 0)
             for (int w = 1; w < (int)blockDim.x / 64; ++w) v += sums[w];
         return v;
     };
-    total = add_up(total);
+    total = add_up(total, a.lanes);
     if (gridDim.x == 1) {
         if (threadIdx.x == 0) *a.loss = (float)total;
+        write_image();
         return;
     }
     // parts and count are stored past the L2s; a part has arrived before its workgroup is counted
@@ -156,11 +190,12 @@ template <int M> __global__ __launch_bounds__(kThreads) void message_loss_kernel
         last = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
         if (last) __hip_atomic_store(a.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    __syncthreads();
+    write_image();
+    lds_barrier();
     if (!last) return;
     total = 0.0;
     for (int i = threadIdx.x; i < (int)gridDim.x; i += blockDim.x) total += __hip_atomic_load(a.partial + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    total = add_up(total);
+    total = add_up(total, 1);
     if (threadIdx.x == 0) *a.loss = (float)total;
 }
 
