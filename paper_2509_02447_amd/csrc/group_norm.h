@@ -104,19 +104,30 @@ __device__ __forceinline__ float2 *part_at(const NormArgs &a, const Tile &t, int
 {
     return a.part + ((size_t)t.n * a.G + t.g0 + g) * a.parts + s;
 }
-// Up to K parts of the lane's share of a group, several on their way at a time: use(part, its index), in order.
-template <typename F> __device__ __forceinline__ void each_part(const float2 *part, int parts, int lane, int lanes, F use)
-{
-    constexpr int K = 4;
-    for (int s = lane; s < parts; s += K * lanes) {
-        float2 v[K];
+// A lane's share of a group's parts (every `lanes`-th from `lane` on), several on their way at a time.  The first are asked for before the pixels are:
+// what is waited for first has to be asked for first.
+struct Parts {
+    static constexpr int K = 4;
+    const float2 *part;
+    int parts, lane, lanes;
+    float2 v[K];
+    __device__ __forceinline__ void ask(int s)
+    {
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] = part[min(s + k * lanes, parts - 1)];
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (s + k * lanes < parts) use(v[k], s + k * lanes);
     }
-}
+    __device__ __forceinline__ Parts(const float2 *p, int count, int l, int n) : part(p), parts(count), lane(l), lanes(n) { ask(l); }
+    template <typename F> __device__ __forceinline__ void each(F use) // use(part, its index), in order
+    {
+        for (int s = lane; s < parts;) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (s + k * lanes < parts) use(v[k], s + k * lanes);
+            s += K * lanes;
+            if (s < parts) ask(s);
+        }
+    }
+};
 // How many lanes join a group of the tile: all threads have a part in it where they can.
 __device__ __forceinline__ int lanes_for(int groups)
 {
@@ -342,7 +353,7 @@ template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__
     for (int i = 0; i < R; ++i)
         if (i < pixels) {
             x[i].pin();
-            store_words<T, V>(q + i * ys, f.template apply<ACT>(x[i], a.act));
+            store_words<false, T, V>(q + i * ys, f.template apply<ACT>(x[i], a.act));
         }
 }
 
@@ -373,12 +384,14 @@ template <typename T, int V, int W> __global__ __launch_bounds__(kMaxThreads) vo
 }
 
 // .. the second: joins the chunks' parts and writes the outputs.
-template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxThreads) void norm_apply_kernel(NormArgs a)
+template <typename T, int V, int W, int ACT, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_apply_kernel(NormArgs a)
 {
     constexpr int R = 4;
     extern __shared__ float2 lds[]; // mean, rstd of the tile's groups
     float *stats = (float *)lds;
     const Tile t = find_tile<V>(a);
+    const int lanes = lanes_for(t.groups), lane = threadIdx.x & (lanes - 1), first = threadIdx.x / lanes;
+    Parts parts(part_at(a, t, min(first, t.groups - 1), 0), a.parts, lane, lanes);
     // from the last pixels on, which the first launch has read last and the caches may still hold; the first of them are on their way while the
     // parts are joined
     int left = t.r < t.rpar ? pixels_at(t, t.r) : 0;
@@ -387,14 +400,14 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
     Words<T, V> x[R], next[R];
     if (t.r < t.rpar) fetch<T, V, R, true>(p, xs, left, left, x);
     Affine<V, W> f(a, t);
-    const int lanes = lanes_for(t.groups), lane = threadIdx.x & (lanes - 1);
-    for (int g = threadIdx.x / lanes; g < t.groups; g += blockDim.x / lanes) {
+    for (int g = first; g < t.groups; g += blockDim.x / lanes) {
+        if (g != first) parts = Parts(part_at(a, t, g, 0), a.parts, lane, lanes);
         float mean = 0.f, m2 = 0.f, count = 0.f;
         // pixels of chunk s: its share of every round, and what the last round leaves for it
         const int64_t round = (int64_t)a.parts * a.parts_rpar;
         const float share = (float)(a.P / round) * a.parts_rpar;
         const int rest = (int)(a.P % round);
-        each_part(part_at(a, t, g, 0), a.parts, lane, lanes, [&](float2 v, int s) {
+        parts.each([&](float2 v, int s) {
             join_spread(mean, m2, count, v.x, v.y, (share + (float)max(0, min(a.parts_rpar, rest - s * a.parts_rpar))) * (float)a.D);
         });
         for (int o = lanes / 2; o; o /= 2) {
@@ -411,7 +424,7 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
         if (left > R) fetch<T, V, R, true>(p, xs, left - R, left, next);
 #pragma unroll
         for (int i = 0; i < R; ++i)
-            if (i < left) store_words<T, V>(q + (left - 1 - i) * ys, f.template apply<ACT>(x[i], a.act));
+            if (i < left) store_words<STREAM, T, V>(q + (left - 1 - i) * ys, f.template apply<ACT>(x[i], a.act));
 #pragma unroll
         for (int i = 0; i < R; ++i) x[i] = next[i];
     }
@@ -625,7 +638,7 @@ template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__
             for (int v = 0; v < V; ++v) d[v] = f.dx(v, x[i].get(v) - c.mean[v * W / V], dz[i][v]);
             Words<T, V> out;
             out.set(d);
-            store_words<T, V>(q + i * xs, out);
+            store_words<false, T, V>(q + i * xs, out);
         }
 }
 
@@ -673,7 +686,7 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
 }
 
 // .. the second: dx, and in the workgroups behind those dgamma and dbeta of 16 channels each.
-template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxThreads) void norm_grad_apply_kernel(NormArgs a, uint32_t apply_blocks)
+template <typename T, int V, int W, int ACT, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_grad_apply_kernel(NormArgs a, uint32_t apply_blocks)
 {
     constexpr int R = 2;
     extern __shared__ float2 lds[];
@@ -683,6 +696,8 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
     }
     float *sums = (float *)lds;
     const Tile t = find_tile<V>(a);
+    const int lanes = lanes_for(t.groups), lane = threadIdx.x & (lanes - 1), first = threadIdx.x / lanes;
+    Parts parts(part_at(a, t, min(first, t.groups - 1), 0), a.parts, lane, lanes);
     int left = t.r < t.rpar ? pixels_at(t, t.r) : 0; // (from the last pixels on, as above)
     const T *p = x_at<T, V>(a, t, left ? t.r : 0);
     const T *q = (const T *)a.dy + y_offset<V>(a, t, left ? t.r : 0);
@@ -694,10 +709,10 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
     }
     const Slopes<V, W, ACT> c(a, t);
     const float inv = 1.f / ((float)a.P * (float)a.D);
-    const int lanes = lanes_for(t.groups), lane = threadIdx.x & (lanes - 1);
-    for (int k = threadIdx.x / lanes; k < t.groups; k += blockDim.x / lanes) {
+    for (int k = first; k < t.groups; k += blockDim.x / lanes) {
+        if (k != first) parts = Parts(part_at(a, t, k, 0), a.parts, lane, lanes);
         float2 v = make_float2(0.f, 0.f);
-        each_part(part_at(a, t, k, 0), a.parts, lane, lanes, [&](float2 p, int) {
+        parts.each([&](float2 p, int) {
             v.x += p.x;
             v.y += p.y;
         });
@@ -727,7 +742,7 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
                 }
                 Words<T, V> r;
                 r.set(out);
-                store_words<T, V>(w + (left - 1 - i) * xs, r);
+                store_words<STREAM, T, V>(w + (left - 1 - i) * xs, r);
             }
 #pragma unroll
         for (int i = 0; i < R; ++i) x[i] = next_x[i], dy[i] = next_dy[i];
@@ -796,8 +811,11 @@ template <typename T> hipError_t norm_forward(const NormCall &c, const NormPlan 
         hipLaunchKernelGGL((norm_stats_kernel<T, V, W>), grid, block, join, s, a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((norm_apply_kernel<T, V, W, ACT>), dim3(p.second.blocks(c.d.N)), dim3(p.second.threads), 2 * (p.second.ct / a.D) * sizeof(float), s,
-                           norm_args(c, p, p.second, ws));
+        auto apply = [&](auto stream) {
+            hipLaunchKernelGGL((norm_apply_kernel<T, V, W, ACT, decltype(stream)::value>), dim3(p.second.blocks(c.d.N)), dim3(p.second.threads),
+                               2 * (p.second.ct / a.D) * sizeof(float), s, norm_args(c, p, p.second, ws));
+        };
+        p.stream ? apply(std::true_type()) : apply(std::false_type());
         return hipGetLastError();
     });
 }
@@ -824,7 +842,11 @@ template <typename T> hipError_t norm_backward(const NormCall &c, const NormPlan
         if (e != hipSuccess) return e;
         const uint32_t apply = c.dx ? p.second.blocks(c.d.N) : 0;
         const size_t own = std::max(2 * (p.second.ct / a.D) * sizeof(float), p.second.threads / 4 * sizeof(float2));
-        hipLaunchKernelGGL((norm_grad_apply_kernel<T, V, W, ACT>), dim3(apply + extra), dim3(p.second.threads), own, s, norm_args(c, p, p.second, ws), apply);
+        auto launch = [&](auto stream) {
+            hipLaunchKernelGGL((norm_grad_apply_kernel<T, V, W, ACT, decltype(stream)::value>), dim3(apply + extra), dim3(p.second.threads), own, s,
+                               norm_args(c, p, p.second, ws), apply);
+        };
+        p.stream ? launch(std::true_type()) : launch(std::false_type());
         return hipGetLastError();
     });
 }

@@ -68,6 +68,10 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
         deal(p.second, backward ? 2 : 4);
         p.part_words = (size_t)d.N * d.groups * p.first.chunks;
     }
+    // Outputs larger than all L2s (8 x 4 MiB) are written past the caches: who reads them next finds little of them there, and what they would push out of the memory-side
+    // cache is written to memory while the next launch reads.  4 images of 256 x 256 pixels, 128 channels, bf16 (64 MiB): 43.6 us without, 38.6 with;
+    // backward 72.0 and 62.4.
+    p.stream = (double)d.N * d.P * d.C * size > 32.0 * (1 << 20);
     p.channels = backward && channels && !(p.whole && d.N == 1);
     p.bytes = (p.part_words + (p.channels ? (size_t)d.N * p.first.chunks * d.C : 0)) * sizeof(float2);
     *out = p;

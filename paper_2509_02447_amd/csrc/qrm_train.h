@@ -64,7 +64,8 @@ template <typename T, int V> __device__ __forceinline__ Words<T, V> load_words(c
     }
     return r;
 }
-template <typename T, int V> __device__ __forceinline__ void store_words(T *p, const Words<T, V> &r)
+// STREAM: past the caches, for what will not be read from them.
+template <bool STREAM, typename T, int V> __device__ __forceinline__ void store_words(T *p, const Words<T, V> &r)
 {
     if constexpr (V * sizeof(T) == 2) {
         *(uint16_t *)p = (uint16_t)r.w[0];
@@ -73,7 +74,8 @@ template <typename T, int V> __device__ __forceinline__ void store_words(T *p, c
         vec v;
 #pragma unroll
         for (int i = 0; i < Words<T, V>::N; ++i) v[i] = r.w[i];
-        *(vec *)p = v;
+        if (STREAM) __builtin_nontemporal_store(v, (vec *)p);
+        else *(vec *)p = v;
     }
 }
 
@@ -104,6 +106,7 @@ struct NormPlan {
     NormCut first, second;
     bool whole;        // one launch (`first`): a workgroup holds a whole tile of an image, up to `pixels` pieces a thread
     int pixels;
+    bool stream;       // two launches: outputs past the caches
     bool channels;     // sums of the channels go through the workspace
     size_t part_words; // of the chunks' groups in the workspace, before the channels' sums
     size_t bytes;      // of workspace
