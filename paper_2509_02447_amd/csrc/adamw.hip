@@ -32,26 +32,26 @@ __device__ __forceinline__ void moments(const Rates &r, float g, float &m, float
     v = v * r.beta2 + g * g * r.rest2;
 }
 
-template <int V> __device__ __forceinline__ void store_copy(void *copy, int type, int64_t i, const float (&p)[V])
+template <int V, bool STREAM = false> __device__ __forceinline__ void store_copy(void *copy, int type, int64_t i, const float (&p)[V])
 {
     if (type == QRM_BF16) {
         Pack<bf16_t, V> c;
 #pragma unroll
         for (int k = 0; k < V; ++k) c.e[k] = (bf16_t)p[k];
-        store_pack<bf16_t, V>((bf16_t *)copy + i, c);
+        store_pack<bf16_t, V, STREAM>((bf16_t *)copy + i, c);
     } else {
         Pack<f16_t, V> c;
 #pragma unroll
         for (int k = 0; k < V; ++k) c.e[k] = (f16_t)p[k];
-        store_pack<f16_t, V>((f16_t *)copy + i, c);
+        store_pack<f16_t, V, STREAM>((f16_t *)copy + i, c);
     }
 }
 
-template <typename TP, typename TG, int V> __device__ __forceinline__ void step_f32(const AdamwTensor &t, const TG *grad, const Rates &r, int copy_type, int64_t i)
+template <typename TP, typename TG, int V, bool STREAM> __device__ __forceinline__ void step_f32(const AdamwTensor &t, const TG *grad, const Rates &r, int copy_type, int64_t i)
 {
-    const Pack<TP, V> p = load_pack<TP, V>((const TP *)t.p + i);
-    const Pack<TG, V> g = load_pack<TG, V>(grad + i);
-    Pack<float, V> m = load_pack<float, V>((const float *)t.m + i), v = load_pack<float, V>((const float *)t.v + i);
+    const Pack<TP, V> p = load_pack<TP, V, STREAM>((const TP *)t.p + i);
+    const Pack<TG, V> g = load_pack<TG, V, STREAM>(grad + i);
+    Pack<float, V> m = load_pack<float, V, STREAM>((const float *)t.m + i), v = load_pack<float, V, STREAM>((const float *)t.v + i);
     Pack<TP, V> q;
     float w[V];
 #pragma unroll
@@ -60,10 +60,10 @@ template <typename TP, typename TG, int V> __device__ __forceinline__ void step_
         w[k] = (float)p.e[k] * r.keep - r.rate * (m.e[k] / (sqrtf(v.e[k]) * r.root + r.eps));
         q.e[k] = (TP)w[k];
     }
-    store_pack<TP, V>((TP *)t.p + i, q);
-    store_pack<float, V>((float *)t.m + i, m);
-    store_pack<float, V>((float *)t.v + i, v);
-    if (t.copy) store_copy<V>(t.copy, copy_type, i, w);
+    store_pack<TP, V, STREAM>((TP *)t.p + i, q);
+    store_pack<float, V, STREAM>((float *)t.m + i, m);
+    store_pack<float, V, STREAM>((float *)t.v + i, v);
+    if (t.copy) store_copy<V, STREAM>(t.copy, copy_type, i, w);
 }
 
 __device__ __forceinline__ bool aligned(const void *p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
@@ -75,7 +75,7 @@ template <typename TP, typename TG, typename TM> __device__ __forceinline__ bool
            aligned(t.copy, 8);
 }
 
-template <typename TP, typename TG, int COUNT>
+template <typename TP, typename TG, int COUNT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTensor *tensors, const uint2 *pieces, uint32_t t0, Grads<COUNT> grads, AdamwStep s, int copy_type)
 {
     const uint2 piece = pieces[blockIdx.x];
@@ -87,39 +87,35 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTensor *tens
     if (wide_ok<TP, TG, float>(t, grad)) {
         int64_t i = first + threadIdx.x * 4;
 #pragma unroll 4
-        for (; i + 4 <= last; i += kThreads * 4) step_f32<TP, TG, 4>(t, grad, r, copy_type, i);
-        for (; i < last; ++i) step_f32<TP, TG, 1>(t, grad, r, copy_type, i); // (one thread, up to three elements)
+        for (; i + 4 <= last; i += kThreads * 4) step_f32<TP, TG, 4, STREAM>(t, grad, r, copy_type, i);
+        for (; i < last; ++i) step_f32<TP, TG, 1, false>(t, grad, r, copy_type, i); // (one thread, up to three elements)
     } else {
-        for (int64_t i = first + threadIdx.x; i < last; i += kThreads) step_f32<TP, TG, 1>(t, grad, r, copy_type, i);
+        for (int64_t i = first + threadIdx.x; i < last; i += kThreads) step_f32<TP, TG, 1, false>(t, grad, r, copy_type, i);
     }
 }
 
 // ---------------------------------------------------------------- moments in 8 bits
 
-__device__ __forceinline__ float decode_m(int c, float scale) { return scale * ((float)(c * abs(c)) * (1.f / 16129.f)); }
-__device__ __forceinline__ float decode_u(uint32_t c, float scale) { return scale * ((float)(c * c) * (1.f / 65025.f)); }
+// Codes as numbers, before the block's scale.
+__device__ __forceinline__ float square_m(int8_t c) { return (float)c * fabsf((float)c); }
+__device__ __forceinline__ float square_u(uint8_t c) { return (float)c * (float)c; }
+constexpr float kStepM = 1.f / 16129.f, kStepU = 1.f / 65025.f; // 1 / 127^2, 1 / 255^2
 
-// The largest of a wavefront's values >= 0; a NaN counts as larger than all (the order of the bits).
-__device__ __forceinline__ float wave_max(float v)
+// The larger of v and another lane's, of numbers >= 0 by their bits: a NaN counts as larger than all.
+template <int CTRL> __device__ __forceinline__ int max_lane(int v) { return max(v, __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float wave_max(int v)
 {
-    int b = __float_as_int(v);
-    for (int o = 32; o; o /= 2) b = max(b, __shfl_xor(b, o));
-    return __int_as_float(b);
+    v = max_lane<0xB1>(v);  // pairs, fours, halves of a row of 16, rows
+    v = max_lane<0x4E>(v);
+    v = max_lane<0x141>(v);
+    v = max_lane<0x140>(v);
+    v = max(v, __shfl_xor(v, 16));
+    return __int_as_float(max(v, __shfl_xor(v, 32)));
 }
+__device__ __forceinline__ int magnitude(float v) { return __float_as_int(v) & 0x7fffffff; }
 
-// Here and below the hardware's roots and inverses are taken as they are (1 ulp): rounded exactly, they would make this kernel's arithmetic as long
-// as its memory's time.  They know no numbers below 2^-126, so what may be there is lifted first.
-__device__ __forceinline__ float root_of(float v)
-{
-    return v >= 0x1p-100f ? __builtin_amdgcn_sqrtf(v) : sqrtf(v);
-}
-// 1 / scale / up for values up to `scale`, which are multiplied by `up` first.
-__device__ __forceinline__ float inverse(float scale, float &up)
-{
-    up = scale < 0x1p-100f ? 0x1p100f : 1.f;
-    return scale > 0.f ? __builtin_amdgcn_rcpf(scale * up) : 0.f;
-}
-
+// The arithmetic takes the hardware's roots and inverses as they are (1 ulp): rounded exactly, they would take longer than the memory does.  They know no numbers
+// below 2^-126: blocks with such a v take the library's root, moments of a tiny scale are lifted first.
 template <typename TP, typename TG, int COUNT>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *tensors, const uint2 *pieces, uint32_t t0, Grads<COUNT> grads, AdamwStep s, int copy_type)
 {
@@ -132,7 +128,8 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
     const bool wide = wide_ok<TP, TG, uint8_t>(t, grad);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     for (int64_t b = first + wave * QRM_MOMENT_BLOCK; b < last; b += kThreads / 64 * QRM_MOMENT_BLOCK) {
-        const float sm = t.m_scale[b / QRM_MOMENT_BLOCK], su = t.v_scale[b / QRM_MOMENT_BLOCK];
+        float *const at_m = t.m_scale + b / QRM_MOMENT_BLOCK, *const at_u = t.v_scale + b / QRM_MOMENT_BLOCK;
+        const float sm = *at_m * kStepM, su = *at_u * kStepU;
         const int64_t i = b + lane * 4;
         Pack<TP, 4> p{};
         Pack<TG, 4> g{};
@@ -144,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
             g = load_pack<TG, 4>(grad + i);
             cm = load_pack<int8_t, 4>((const int8_t *)t.m + i);
             cu = load_pack<uint8_t, 4>((const uint8_t *)t.v + i);
-        } else {
+        } else { // (elements that are not there: zeros, of no weight in the largest)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (i + k < last) {
@@ -154,31 +151,40 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
                     cu.e[k] = ((const uint8_t *)t.v)[i + k];
                 }
         }
-        float w[4], m[4], u[4], top_m = 0.f, top_u = 0.f;
+        float w[4], m[4], v[4], u[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            w[k] = (float)p.e[k];
-            m[k] = decode_m(cm.e[k], sm);
-            const float root = decode_u(cu.e[k], su);
-            float v = root * root;
-            moments(r, (float)g.e[k], m[k], v);
-            u[k] = root_of(v);
-            w[k] = w[k] * r.keep - r.rate * (m[k] * __builtin_amdgcn_rcpf(u[k] * r.root + r.eps));
-            p.e[k] = (TP)w[k];
-            if (i + k >= last) m[k] = u[k] = 0.f; // (an element that is not there: of weight nothing in the largest)
-            top_m = __int_as_float(max(__float_as_int(top_m), __float_as_int(fabsf(m[k]))));
-            top_u = __int_as_float(max(__float_as_int(top_u), __float_as_int(u[k])));
+            m[k] = square_m(cm.e[k]) * sm;
+            const float root = square_u(cu.e[k]) * su;
+            v[k] = root * root;
+            moments(r, (float)g.e[k], m[k], v[k]);
+            u[k] = __builtin_amdgcn_sqrtf(v[k]);
         }
-        top_m = wave_max(top_m);
-        top_u = wave_max(top_u);
-        float up_m, up_u;
-        const float inv_m = inverse(top_m, up_m), inv_u = inverse(top_u, up_u);
+        if (__any(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < 0x1p-100f)) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = sqrtf(v[k]);
+        }
+        int top_m = 0, top_u = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int am = (int)rintf(127.f * __builtin_amdgcn_sqrtf(fabsf(m[k]) * up_m * inv_m));
-            cm.e[k] = (int8_t)(m[k] < 0.f ? -am : am);
-            const int au = (int)rintf(255.f * __builtin_amdgcn_sqrtf(u[k] * up_u * inv_u));
-            cu.e[k] = (uint8_t)(u[k] > 0.f ? max(au, 1) : au);
+            w[k] = (float)p.e[k] * r.keep - r.rate * (m[k] * __builtin_amdgcn_rcpf(u[k] * r.root + r.eps));
+            p.e[k] = (TP)w[k];
+            top_m = max(top_m, magnitude(m[k]));
+            top_u = max(top_u, magnitude(u[k]));
+        }
+        const float scale_m = wave_max(top_m), scale_u = wave_max(top_u);
+        float of_m = scale_m;
+        if (scale_m < 0x1p-100f) { // (the same in all lanes)
+            of_m *= 0x1p100f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) m[k] *= 0x1p100f;
+        }
+        const float inv_m = of_m > 0.f ? 16129.f * __builtin_amdgcn_rcpf(of_m) : 0.f, inv_u = scale_u > 0.f ? 65025.f * __builtin_amdgcn_rcpf(scale_u) : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            cm.e[k] = (int8_t)(int)copysignf(rintf(__builtin_amdgcn_sqrtf(fabsf(m[k]) * inv_m)), m[k]);
+            const float y = rintf(__builtin_amdgcn_sqrtf(u[k] * inv_u));
+            cu.e[k] = (uint8_t)(int)(u[k] > 0.f ? fmaxf(y, 1.f) : 0.f);
         }
         if (whole) {
             store_pack<TP, 4>((TP *)t.p + i, p);
@@ -197,8 +203,8 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
                 }
         }
         if (lane == 0) {
-            t.m_scale[b / QRM_MOMENT_BLOCK] = top_m;
-            t.v_scale[b / QRM_MOMENT_BLOCK] = top_u;
+            *at_m = scale_m;
+            *at_u = scale_u;
         }
     }
 }
@@ -209,10 +215,10 @@ template <typename T> __global__ __launch_bounds__(kThreads) void unpack_moment_
 {
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kUnpack;
     if (i >= n) return;
-    const float scale = scales[i / QRM_MOMENT_BLOCK];
+    const float scale = scales[i / QRM_MOMENT_BLOCK] * (moment ? kStepU : kStepM);
     auto value = [&](uint8_t c) {
-        if (moment == 0) return (T)decode_m((int8_t)c, scale);
-        const float u = decode_u(c, scale);
+        if (moment == 0) return (T)(square_m((int8_t)c) * scale);
+        const float u = square_u(c) * scale;
         return (T)(u * u);
     };
     if (i + kUnpack <= n && aligned(codes, kUnpack) && aligned(out, 16)) {
@@ -240,8 +246,10 @@ hipError_t launch_counted(const AdamwTypes &t, const AdamwTensor *tensors, const
         return with_type(t.grad, [&](auto *ng) {
             using TP = std::remove_pointer_t<decltype(np)>;
             using TG = std::remove_pointer_t<decltype(ng)>;
-            if (t.bits == 32)
-                hipLaunchKernelGGL((adamw_kernel<TP, TG, COUNT>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
+            if (t.bits == 32 && t.stream)
+                hipLaunchKernelGGL((adamw_kernel<TP, TG, COUNT, true>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
+            else if (t.bits == 32)
+                hipLaunchKernelGGL((adamw_kernel<TP, TG, COUNT, false>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
             else
                 hipLaunchKernelGGL((adamw8_kernel<TP, TG, COUNT>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
             return hipGetLastError();

@@ -10,12 +10,28 @@ namespace qrm {
 
 typedef _Float16 f16_t;
 
-// V neighbouring elements as one load or store of up to 16 bytes.
+// V neighbouring elements as one load or store of up to 16 bytes.  STREAM: past the caches, for what will not be read from them.
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack {
     T e[V];
 };
-template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const T *p) { return *(const Pack<T, V> *)p; }
-template <typename T, int V> __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &v) { *(Pack<T, V> *)p = v; }
+template <int BYTES> struct Raw {
+    typedef uint32_t type __attribute__((ext_vector_type(BYTES / 4)));
+};
+template <> struct Raw<4> { typedef uint32_t type; };
+template <> struct Raw<2> { typedef uint16_t type; };
+template <> struct Raw<1> { typedef uint8_t type; };
+template <typename T, int V, bool STREAM = false> __device__ __forceinline__ Pack<T, V> load_pack(const T *p)
+{
+    typedef typename Raw<sizeof(T) * V>::type R;
+    typedef Pack<T, V> P;
+    return __builtin_bit_cast(P, STREAM ? __builtin_nontemporal_load((const R *)p) : *(const R *)p);
+}
+template <typename T, int V, bool STREAM = false> __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &v)
+{
+    typedef typename Raw<sizeof(T) * V>::type R;
+    if (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(R, v), (R *)p);
+    else *(R *)p = __builtin_bit_cast(R, v);
+}
 
 // The same as the 32-bit registers that they were loaded into: elements are widened where they are used and, behind a pin(), widened again
 // there instead of being kept as 32-bit numbers in between.
@@ -140,6 +156,7 @@ struct AdamwStep {
 };
 struct AdamwTypes {
     int param, grad, copy, bits;
+    bool stream; // 32-bit moments: a step passes more bytes than the caches hold
 };
 // Pieces first .. first + count - 1 of the plan, which belong to tensors t0 .. t0 + grads - 1.
 hipError_t launch_adamw(const AdamwTypes &t, const AdamwTensor *tensors, const uint2 *pieces, uint32_t first, uint32_t count, uint32_t t0,
