@@ -114,98 +114,118 @@ __device__ __forceinline__ float wave_max(int v)
 }
 __device__ __forceinline__ int magnitude(float v) { return __float_as_int(v) & 0x7fffffff; }
 
-// The arithmetic takes the hardware's roots and inverses as they are (1 ulp): rounded exactly, they would take longer than the memory does.  They know no numbers
-// below 2^-126: blocks with such a v take the library's root, moments of a tiny scale are lifted first.
+// What a lane holds of a block: four neighbouring elements.
+template <typename TP, typename TG> struct Quad {
+    Pack<TP, 4> p;
+    Pack<TG, 4> g;
+    Pack<int8_t, 4> m;
+    Pack<uint8_t, 4> u;
+    float scale_m, scale_u;
+};
+
+// One step of a wavefront's block; the scales come back the same in all lanes, w the parameters in 32 bits.  The arithmetic takes the hardware's roots and
+// inverses as they are (1 ulp): rounded exactly, they would take longer than the memory does.  They know no numbers below 2^-126: blocks with such a v take
+// the library's root, moments of a tiny scale are lifted first.
+template <typename TP, typename TG> __device__ __forceinline__ void step_block(const Rates &r, Quad<TP, TG> &q, float (&w)[4])
+{
+    const float sm = q.scale_m * kStepM, su = q.scale_u * kStepU;
+    float m[4], v[4], u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        m[k] = square_m(q.m.e[k]) * sm;
+        const float root = square_u(q.u.e[k]) * su;
+        v[k] = root * root;
+        moments(r, (float)q.g.e[k], m[k], v[k]);
+        u[k] = __builtin_amdgcn_sqrtf(v[k]);
+    }
+    if (__any(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < 0x1p-100f)) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = sqrtf(v[k]);
+    }
+    int top_m = 0, top_u = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        w[k] = (float)q.p.e[k] * r.keep - r.rate * (m[k] * __builtin_amdgcn_rcpf(u[k] * r.root + r.eps));
+        q.p.e[k] = (TP)w[k];
+        top_m = max(top_m, magnitude(m[k]));
+        top_u = max(top_u, magnitude(u[k]));
+    }
+    q.scale_m = wave_max(top_m);
+    q.scale_u = wave_max(top_u);
+    float of_m = q.scale_m;
+    if (of_m < 0x1p-100f) {
+        of_m *= 0x1p100f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m[k] *= 0x1p100f;
+    }
+    const float inv_m = of_m > 0.f ? 16129.f * __builtin_amdgcn_rcpf(of_m) : 0.f, inv_u = q.scale_u > 0.f ? 65025.f * __builtin_amdgcn_rcpf(q.scale_u) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        q.m.e[k] = (int8_t)(int)copysignf(rintf(__builtin_amdgcn_sqrtf(fabsf(m[k]) * inv_m)), m[k]);
+        const float y = rintf(__builtin_amdgcn_sqrtf(u[k] * inv_u));
+        q.u.e[k] = (uint8_t)(int)(u[k] > 0.f ? fmaxf(y, 1.f) : 0.f);
+    }
+}
+
 template <typename TP, typename TG, int COUNT>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *tensors, const uint2 *pieces, uint32_t t0, Grads<COUNT> grads, AdamwStep s, int copy_type)
 {
+    constexpr int kBlocks = kAdamwPiece / (kThreads / 64) / QRM_MOMENT_BLOCK; // of a wavefront, side by side
     const uint2 piece = pieces[blockIdx.x];
     const AdamwTensor t = tensors[piece.x];
     const TG *grad = (const TG *)grads.p[piece.x - t0];
     if (!grad) return;
     const Rates r = rates_of(s, t);
-    const int64_t first = (int64_t)piece.y * kAdamwPiece, last = min(first + kAdamwPiece, t.n);
-    const bool wide = wide_ok<TP, TG, uint8_t>(t, grad);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    for (int64_t b = first + wave * QRM_MOMENT_BLOCK; b < last; b += kThreads / 64 * QRM_MOMENT_BLOCK) {
-        float *const at_m = t.m_scale + b / QRM_MOMENT_BLOCK, *const at_u = t.v_scale + b / QRM_MOMENT_BLOCK;
-        const float sm = *at_m * kStepM, su = *at_u * kStepU;
-        const int64_t i = b + lane * 4;
-        Pack<TP, 4> p{};
-        Pack<TG, 4> g{};
-        Pack<int8_t, 4> cm{};
-        Pack<uint8_t, 4> cu{};
-        const bool whole = wide && b + QRM_MOMENT_BLOCK <= last;
-        if (whole) {
-            p = load_pack<TP, 4>((const TP *)t.p + i);
-            g = load_pack<TG, 4>(grad + i);
-            cm = load_pack<int8_t, 4>((const int8_t *)t.m + i);
-            cu = load_pack<uint8_t, 4>((const uint8_t *)t.v + i);
-        } else { // (elements that are not there: zeros, of no weight in the largest)
+    const int64_t first = (int64_t)piece.y * kAdamwPiece + wave * (kBlocks * QRM_MOMENT_BLOCK), last = min((int64_t)(piece.y + 1) * kAdamwPiece, t.n);
+    float *const scales_m = t.m_scale + first / QRM_MOMENT_BLOCK, *const scales_u = t.v_scale + first / QRM_MOMENT_BLOCK;
+    TP *const p = (TP *)t.p + first;
+    const TG *const g = grad + first;
+    int8_t *const m = (int8_t *)t.m + first;
+    uint8_t *const u = (uint8_t *)t.v + first;
+    if (first + kBlocks * QRM_MOMENT_BLOCK <= last && wide_ok<TP, TG, uint8_t>(t, grad)) {
+        Quad<TP, TG> q[kBlocks]; // all on their way before the first is used
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + k < last) {
-                    p.e[k] = ((const TP *)t.p)[i + k];
-                    g.e[k] = grad[i + k];
-                    cm.e[k] = ((const int8_t *)t.m)[i + k];
-                    cu.e[k] = ((const uint8_t *)t.v)[i + k];
-                }
+        for (int b = 0; b < kBlocks; ++b) {
+            const int i = b * QRM_MOMENT_BLOCK + lane * 4;
+            q[b].scale_m = scales_m[b];
+            q[b].scale_u = scales_u[b];
+            q[b].p = load_pack<TP, 4>(p + i);
+            q[b].g = load_pack<TG, 4>(g + i);
+            q[b].m = load_pack<int8_t, 4>(m + i);
+            q[b].u = load_pack<uint8_t, 4>(u + i);
         }
-        float w[4], m[4], v[4], u[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            m[k] = square_m(cm.e[k]) * sm;
-            const float root = square_u(cu.e[k]) * su;
-            v[k] = root * root;
-            moments(r, (float)g.e[k], m[k], v[k]);
-            u[k] = __builtin_amdgcn_sqrtf(v[k]);
+        for (int b = 0; b < kBlocks; ++b) {
+            const int i = b * QRM_MOMENT_BLOCK + lane * 4;
+            float w[4];
+            step_block<TP, TG>(r, q[b], w);
+            store_pack<TP, 4>(p + i, q[b].p);
+            store_pack<int8_t, 4>(m + i, q[b].m);
+            store_pack<uint8_t, 4>(u + i, q[b].u);
+            if (t.copy) store_copy<4>(t.copy, copy_type, first + i, w);
+            if (lane == 0) scales_m[b] = q[b].scale_m, scales_u[b] = q[b].scale_u;
         }
-        if (__any(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < 0x1p-100f)) {
+        return;
+    }
+    for (int b = 0; b < kBlocks && first + b * QRM_MOMENT_BLOCK < last; ++b) {
+        const int i = b * QRM_MOMENT_BLOCK + lane * 4, here = (int)max((int64_t)0, min((int64_t)4, last - first - i));
+        Quad<TP, TG> q{}; // (elements that are not there: zeros, of no weight in the largest)
+        q.scale_m = scales_m[b];
+        q.scale_u = scales_u[b];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = sqrtf(v[k]);
-        }
-        int top_m = 0, top_u = 0;
+        for (int k = 0; k < 4; ++k)
+            if (k < here) q.p.e[k] = p[i + k], q.g.e[k] = g[i + k], q.m.e[k] = m[i + k], q.u.e[k] = u[i + k];
+        float w[4];
+        step_block<TP, TG>(r, q, w);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            w[k] = (float)p.e[k] * r.keep - r.rate * (m[k] * __builtin_amdgcn_rcpf(u[k] * r.root + r.eps));
-            p.e[k] = (TP)w[k];
-            top_m = max(top_m, magnitude(m[k]));
-            top_u = max(top_u, magnitude(u[k]));
-        }
-        const float scale_m = wave_max(top_m), scale_u = wave_max(top_u);
-        float of_m = scale_m;
-        if (scale_m < 0x1p-100f) { // (the same in all lanes)
-            of_m *= 0x1p100f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) m[k] *= 0x1p100f;
-        }
-        const float inv_m = of_m > 0.f ? 16129.f * __builtin_amdgcn_rcpf(of_m) : 0.f, inv_u = scale_u > 0.f ? 65025.f * __builtin_amdgcn_rcpf(scale_u) : 0.f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            cm.e[k] = (int8_t)(int)copysignf(rintf(__builtin_amdgcn_sqrtf(fabsf(m[k]) * inv_m)), m[k]);
-            const float y = rintf(__builtin_amdgcn_sqrtf(u[k] * inv_u));
-            cu.e[k] = (uint8_t)(int)(u[k] > 0.f ? fmaxf(y, 1.f) : 0.f);
-        }
-        if (whole) {
-            store_pack<TP, 4>((TP *)t.p + i, p);
-            store_pack<int8_t, 4>((int8_t *)t.m + i, cm);
-            store_pack<uint8_t, 4>((uint8_t *)t.v + i, cu);
-            if (t.copy) store_copy<4>(t.copy, copy_type, i, w);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + k < last) {
-                    ((TP *)t.p)[i + k] = p.e[k];
-                    ((int8_t *)t.m)[i + k] = cm.e[k];
-                    ((uint8_t *)t.v)[i + k] = cu.e[k];
-                    const float one[1] = {w[k]};
-                    if (t.copy) store_copy<1>(t.copy, copy_type, i + k, one);
-                }
-        }
-        if (lane == 0) {
-            *at_m = scale_m;
-            *at_u = scale_u;
-        }
+        for (int k = 0; k < 4; ++k)
+            if (k < here) {
+                p[i + k] = q.p.e[k], m[i + k] = q.m.e[k], u[i + k] = q.u.e[k];
+                const float one[1] = {w[k]};
+                if (t.copy) store_copy<1>(t.copy, copy_type, first + i + k, one);
+            }
+        if (lane == 0) scales_m[b] = q.scale_m, scales_u[b] = q.scale_u;
     }
 }
 
