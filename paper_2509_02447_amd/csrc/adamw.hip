@@ -167,7 +167,7 @@ template <typename TP, typename TG> __device__ __forceinline__ void step_block(c
     }
 }
 
-template <typename TP, typename TG, int COUNT>
+template <typename TP, typename TG, int COUNT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *tensors, const uint2 *pieces, uint32_t t0, Grads<COUNT> grads, AdamwStep s, int copy_type)
 {
     constexpr int kBlocks = kAdamwPiece / (kThreads / 64) / QRM_MOMENT_BLOCK; // of a wavefront, side by side
@@ -190,8 +190,8 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
             const int i = b * QRM_MOMENT_BLOCK + lane * 4;
             q[b].scale_m = scales_m[b];
             q[b].scale_u = scales_u[b];
-            q[b].p = load_pack<TP, 4>(p + i);
-            q[b].g = load_pack<TG, 4>(g + i);
+            q[b].p = load_pack<TP, 4, STREAM>(p + i);
+            q[b].g = load_pack<TG, 4, STREAM>(g + i);
             q[b].m = load_pack<int8_t, 4>(m + i);
             q[b].u = load_pack<uint8_t, 4>(u + i);
         }
@@ -200,10 +200,10 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const AdamwTensor *ten
             const int i = b * QRM_MOMENT_BLOCK + lane * 4;
             float w[4];
             step_block<TP, TG>(r, q[b], w);
-            store_pack<TP, 4>(p + i, q[b].p);
+            store_pack<TP, 4, STREAM>(p + i, q[b].p);
             store_pack<int8_t, 4>(m + i, q[b].m);
             store_pack<uint8_t, 4>(u + i, q[b].u);
-            if (t.copy) store_copy<4>(t.copy, copy_type, first + i, w);
+            if (t.copy) store_copy<4, STREAM>(t.copy, copy_type, first + i, w);
             if (lane == 0) scales_m[b] = q[b].scale_m, scales_u[b] = q[b].scale_u;
         }
         return;
@@ -266,12 +266,14 @@ hipError_t launch_counted(const AdamwTypes &t, const AdamwTensor *tensors, const
         return with_type(t.grad, [&](auto *ng) {
             using TP = std::remove_pointer_t<decltype(np)>;
             using TG = std::remove_pointer_t<decltype(ng)>;
-            if (t.bits == 32 && t.stream)
-                hipLaunchKernelGGL((adamw_kernel<TP, TG, COUNT, true>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
-            else if (t.bits == 32)
-                hipLaunchKernelGGL((adamw_kernel<TP, TG, COUNT, false>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
-            else
-                hipLaunchKernelGGL((adamw8_kernel<TP, TG, COUNT>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
+            auto launch = [&](auto stream) {
+                constexpr bool STREAM = decltype(stream)::value;
+                if (t.bits == 32)
+                    hipLaunchKernelGGL((adamw_kernel<TP, TG, COUNT, STREAM>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
+                else
+                    hipLaunchKernelGGL((adamw8_kernel<TP, TG, COUNT, STREAM>), dim3(count), dim3(kThreads), 0, s, tensors, pieces, t0, g, step, t.copy);
+            };
+            t.stream ? launch(std::true_type()) : launch(std::false_type());
             return hipGetLastError();
         });
     });

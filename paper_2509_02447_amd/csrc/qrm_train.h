@@ -156,7 +156,7 @@ struct AdamwStep {
 };
 struct AdamwTypes {
     int param, grad, copy, bits;
-    bool stream; // 32-bit moments: a step passes more bytes than the caches hold
+    bool stream; // a step passes more bytes than the caches hold
 };
 // Pieces first .. first + count - 1 of the plan, which belong to tensors t0 .. t0 + grads - 1.
 hipError_t launch_adamw(const AdamwTypes &t, const AdamwTensor *tensors, const uint2 *pieces, uint32_t first, uint32_t count, uint32_t t0,

@@ -184,9 +184,10 @@ qrm_status qrm_adamw_create(qrm_ctx *c, const qrm_adamw_desc *desc, const qrm_ad
     qrm_adamw *o = new (std::nothrow) qrm_adamw();
     if (!o) return fail(c, QRM_E_NOMEM, "no host memory for the plan");
     o->device = c->device;
-    // Past the caches where a step's moments alone are more than the memory-side cache (256 MiB): the next step finds nothing of them there.  50 million
-    // parameters with a 16-bit copy 278 us without, 266 with; 200 million in 32 bits 1107 and 1065.
-    o->types = AdamwTypes{desc->param_type, desc->grad_type, desc->copy_type, desc->state_bits, elements * 8 > ((uint64_t)256 << 20)};
+    // Past the caches (8-bit moments excepted) where a step passes more than the memory-side cache holds (256 MiB): the next step finds nothing of it there.  50
+    // million parameters with 16-bit gradients and a copy 278 us without, 266 with, with 8-bit moments 151 and 144; 200 million in 32 bits 1107 and 1053.
+    const uint64_t each = 2 * pb + type_bytes(desc->grad_type) + 4 * mb; // bytes an element
+    o->types = AdamwTypes{desc->param_type, desc->grad_type, desc->copy_type, desc->state_bits, elements * each > ((uint64_t)256 << 20)};
     o->first_piece = std::move(first);
     if (!pieces.empty()) {
         const size_t at = (tensors.size() * sizeof(AdamwTensor) + 255) / 256 * 256;
