@@ -475,16 +475,14 @@ class AdamW:
     def _mixed(what):
         raise ValueError(f"all {what} of a plan have one type")
 
-    def _grad(self, g, n):
-        assert g.dtype is self._grad_type and g.numel() == n, "a gradient has the wrong type or size"
-        assert g.is_cuda and g.is_contiguous(), "device tensors must be contiguous and on the GPU"
-        return g.data_ptr()
-
     def qrm_adamw_step(self, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                        d_grad_scale=None, stream=None):
         """grads: one device tensor of grad_type for each tensor of the plan, or None where it has no gradient."""
         assert len(grads) == self._n, "one gradient (or None) for each tensor"
-        ptrs = self._array(*[None if g is None else self._grad(g, n) for g, n in zip(grads, self._sizes)])
+        t = self._grad_type
+        assert all([g is None or (g.dtype is t and g.numel() == n and g.is_cuda and g.is_contiguous()) for g, n in zip(grads, self._sizes)]), \
+            "gradients must have the plan's type and sizes, be contiguous and on the GPU"
+        ptrs = self._array(*[None if g is None else g.data_ptr() for g in grads])
         self._ctx._check(self._lib.qrm_adamw_step(self._ctx._h, self._h, ptrs, int(step), float(lr), float(beta1), float(beta2),
                                                   float(eps), _dptr(d_grad_scale), _stream_handle(stream)))
 

@@ -47,22 +47,29 @@ template <int V, bool STREAM = false> __device__ __forceinline__ void store_copy
     }
 }
 
-template <typename TP, typename TG, int V, bool STREAM> __device__ __forceinline__ void step_f32(const AdamwTensor &t, const TG *grad, const Rates &r, int copy_type, int64_t i)
+// What a thread holds of a piece: V neighbouring elements.
+template <typename TP, typename TG, int V> struct Some {
+    Pack<TP, V> p;
+    Pack<TG, V> g;
+    Pack<float, V> m, v;
+};
+template <typename TP, typename TG, int V, bool STREAM> __device__ __forceinline__ Some<TP, TG, V> load_some(const AdamwTensor &t, const TG *grad, int64_t i)
 {
-    const Pack<TP, V> p = load_pack<TP, V, STREAM>((const TP *)t.p + i);
-    const Pack<TG, V> g = load_pack<TG, V, STREAM>(grad + i);
-    Pack<float, V> m = load_pack<float, V, STREAM>((const float *)t.m + i), v = load_pack<float, V, STREAM>((const float *)t.v + i);
-    Pack<TP, V> q;
+    return Some<TP, TG, V>{load_pack<TP, V, STREAM>((const TP *)t.p + i), load_pack<TG, V, STREAM>(grad + i), load_pack<float, V, STREAM>((const float *)t.m + i),
+                           load_pack<float, V, STREAM>((const float *)t.v + i)};
+}
+template <typename TP, typename TG, int V, bool STREAM> __device__ __forceinline__ void step_some(const AdamwTensor &t, const Rates &r, int copy_type, int64_t i, Some<TP, TG, V> e)
+{
     float w[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        moments(r, (float)g.e[k], m.e[k], v.e[k]);
-        w[k] = (float)p.e[k] * r.keep - r.rate * (m.e[k] / (sqrtf(v.e[k]) * r.root + r.eps));
-        q.e[k] = (TP)w[k];
+        moments(r, (float)e.g.e[k], e.m.e[k], e.v.e[k]);
+        w[k] = (float)e.p.e[k] * r.keep - r.rate * (e.m.e[k] / (sqrtf(e.v.e[k]) * r.root + r.eps));
+        e.p.e[k] = (TP)w[k];
     }
-    store_pack<TP, V, STREAM>((TP *)t.p + i, q);
-    store_pack<float, V, STREAM>((float *)t.m + i, m);
-    store_pack<float, V, STREAM>((float *)t.v + i, v);
+    store_pack<TP, V, STREAM>((TP *)t.p + i, e.p);
+    store_pack<float, V, STREAM>((float *)t.m + i, e.m);
+    store_pack<float, V, STREAM>((float *)t.v + i, e.v);
     if (t.copy) store_copy<V, STREAM>(t.copy, copy_type, i, w);
 }
 
@@ -84,14 +91,24 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwTensor *tens
     if (!grad) return;
     const Rates r = rates_of(s, t);
     const int64_t first = (int64_t)piece.y * kAdamwPiece, last = min(first + kAdamwPiece, t.n);
-    if (wide_ok<TP, TG, float>(t, grad)) {
-        int64_t i = first + threadIdx.x * 4;
-#pragma unroll 4
-        for (; i + 4 <= last; i += kThreads * 4) step_f32<TP, TG, 4, STREAM>(t, grad, r, copy_type, i);
-        for (; i < last; ++i) step_f32<TP, TG, 1, false>(t, grad, r, copy_type, i); // (one thread, up to three elements)
-    } else {
-        for (int64_t i = first + threadIdx.x; i < last; i += kThreads) step_f32<TP, TG, 1, false>(t, grad, r, copy_type, i);
+    constexpr int kTimes = kAdamwPiece / (kThreads * 4);
+    if (!wide_ok<TP, TG, float>(t, grad)) {
+        for (int64_t i = first + threadIdx.x; i < last; i += kThreads) step_some<TP, TG, 1, false>(t, r, copy_type, i, load_some<TP, TG, 1, false>(t, grad, i));
+        return;
     }
+    // all on their way before the first is used; what is behind the end is the last four elements' that are there
+    const int64_t quads = first + (last - first) / 4 * 4;
+    if (quads > first) {
+        Some<TP, TG, 4> e[kTimes];
+#pragma unroll
+        for (int j = 0; j < kTimes; ++j) e[j] = load_some<TP, TG, 4, STREAM>(t, grad, min(first + (j * kThreads + threadIdx.x) * 4, quads - 4));
+#pragma unroll
+        for (int j = 0; j < kTimes; ++j) {
+            const int64_t i = first + (j * kThreads + threadIdx.x) * 4;
+            if (i < quads) step_some<TP, TG, 4, STREAM>(t, r, copy_type, i, e[j]);
+        }
+    }
+    if (quads + threadIdx.x < last) step_some<TP, TG, 1, false>(t, r, copy_type, quads + threadIdx.x, load_some<TP, TG, 1, false>(t, grad, quads + threadIdx.x));
 }
 
 // ---------------------------------------------------------------- moments in 8 bits
