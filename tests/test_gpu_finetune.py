@@ -292,6 +292,60 @@ def test_group_norm_same_bits_again_on_other_streams_and_beside_other_work(ctx, 
     assert all(torch.equal(a, b) for out in got for a, b in zip(first, out))
 
 
+@pytest.mark.parametrize("c,groups,dtype", [(8192, 1, torch.bfloat16), (8192, 2, torch.float32), (1024, 1, torch.float32), (6144, 1, torch.float16), (513, 1, torch.float32)])
+def test_group_norm_wide_groups(ctx, qrm, c, groups, dtype):
+    for p in (5, 64, 700):
+        check_backward(ctx, qrm, 2, p, c, groups, dtype, "silu", seed=c + p)
+
+
+@pytest.mark.parametrize("n,p,c,groups", [(300, 40, 64, 8), (64, 512, 256, 32), (33, 2048, 512, 32), (2000, 1, 32, 32), (1, 65, 512, 32), (7, 1025, 128, 32)])
+def test_group_norm_between_one_launch_and_two(ctx, qrm, n, p, c, groups):
+    """Sizes on both sides of the rules that give a tile to one workgroup, and tiles of half a line to few images."""
+    if n * p * c < 5_000_000:
+        check_backward(ctx, qrm, n, p, c, groups, torch.bfloat16, "silu", seed=n + p)
+    else:                                                    # too large for the 64-bit oracle in a test: image by image the same bits
+        g = torch.Generator().manual_seed(n)
+        x, dy = (torch.randn((n, p, c), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+        y, dx, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty((n, groups), device="cuda"), torch.empty((n, groups), device="cuda")
+        d = qrm.group_norm_desc(n, p, c, groups, x.dtype, "silu")
+        ctx.qrm_group_norm(d, x, None, None, y, mean, rstd)
+        ctx.qrm_group_norm_backward(d, x, dy, None, None, mean, rstd, dx)
+        torch.cuda.synchronize()
+        for i in (0, n // 2, n - 1):
+            ry, rm, rr = ft.group_norm(f64(x[i:i + 1]), None, None, groups, "silu", EPS)
+            rdx = ft.group_norm_backward(f64(x[i:i + 1]), f64(dy[i:i + 1]), None, None, rm, rr, groups, "silu")[0]
+            # a group's mean and spread are near 0 and 1 here: the errors of check_norm and check_backward, at their largest
+            assert (np.abs(f64(y[i]) - ry[0]) <= HALF[x.dtype] * np.abs(ry[0]) + 1000 * U).all()
+            assert (np.abs(f64(dx[i]) - rdx[0]) <= HALF[x.dtype] * np.abs(rdx[0]) + 4000 * U).all()
+
+
+def test_more_streams_than_workspaces(ctx, qrm):
+    """A stream not seen before takes over a workspace that a call has just used on another one."""
+    n, p, c, groups = 2, 9000, 64, 8
+    g = torch.Generator().manual_seed(12)
+    maps = [torch.randn((n, p, c), generator=g).to(torch.bfloat16).cuda() for _ in range(4)]
+    d = qrm.group_norm_desc(n, p, c, groups, torch.bfloat16, "silu")
+
+    def once(x):
+        y, mean, rstd = torch.empty_like(x), torch.empty((n, groups), device="cuda"), torch.empty((n, groups), device="cuda")
+        dx, dgamma = torch.empty_like(x), torch.empty(c, device="cuda")
+        ctx.qrm_group_norm(d, x, None, None, y, mean, rstd)
+        ctx.qrm_group_norm_backward(d, x, y, None, None, mean, rstd, dx, dgamma)
+        return y, mean, rstd, dx, dgamma
+
+    expected = [once(x) for x in maps]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2 * qrm.QRM_MAX_STREAMS + 3)], []
+    for i in range(3 * len(streams)):
+        with torch.cuda.stream(streams[i % len(streams)]):
+            got.append(once(maps[i % 4]))
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(expected[i % 4], out)), i
+    for s in streams:
+        ctx.qrm_release_stream(s)
+
+
 def test_group_norm_no_images(ctx, qrm):
     x = torch.empty((0, 10, 8), device="cuda")
     d = qrm.group_norm_desc(0, 10, 8, 2, x.dtype)
@@ -676,3 +730,48 @@ def test_message_loss_same_bits_again(ctx):
             ctx.qrm_message_loss(z, target, n, n, 48, 1.0, loss, dz)
             outs.append((loss, dz))
         assert all(torch.equal(a, b) for o in outs for a, b in zip(o, outs[0]))
+
+
+def test_a_recorded_step_gives_the_eager_step_at_every_replay(ctx, qrm):
+    """Norm, its backward pass, the loss and AdamW in one graph, replayed with eager work of the same context in between."""
+    n, p, c, groups, bits = 3, 9000, 64, 8, 48
+    g = torch.Generator().manual_seed(21)
+    x, dy = (torch.randn((n, p, c), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    logits, target = torch.randn((6000, bits), generator=g).cuda(), torch.randint(0, 2, (bits,), generator=g, dtype=torch.uint8).cuda()
+    grad = torch.randn(5000, generator=g).cuda()
+    d = qrm.group_norm_desc(n, p, c, groups, x.dtype, "silu")
+
+    def state():
+        o = dict(y=torch.empty_like(x), mean=torch.empty((n, groups), device="cuda"), rstd=torch.empty((n, groups), device="cuda"), dx=torch.empty_like(x),
+                 dgamma=torch.empty(c, device="cuda"), dbeta=torch.empty(c, device="cuda"), loss=torch.empty(1, device="cuda"), dz=torch.empty_like(logits),
+                 p=torch.ones(5000, device="cuda"), m=torch.zeros(5000, dtype=torch.int8, device="cuda"), v=torch.zeros(5000, dtype=torch.uint8, device="cuda"),
+                 ms=torch.zeros(20, device="cuda"), vs=torch.zeros(20, device="cuda"))
+        return o, qrm.AdamW(ctx, [dict(param=o["p"], m=o["m"], v=o["v"], m_scale=o["ms"], v_scale=o["vs"])], torch.float32)
+
+    def step(o, opt):
+        ctx.qrm_group_norm(d, x, None, None, o["y"], o["mean"], o["rstd"])
+        ctx.qrm_group_norm_backward(d, x, dy, None, None, o["mean"], o["rstd"], o["dx"], o["dgamma"], o["dbeta"])
+        ctx.qrm_message_loss(logits, target, 1, 6000, bits, 1.0, o["loss"], o["dz"])
+        opt.qrm_adamw_step([grad], 3, 1e-3)
+
+    (eager, eager_opt), (seen, seen_opt) = state(), state()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):                          # the stream's workspace is there before the recording
+        step(seen, seen_opt)
+    step(eager, eager_opt)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step(seen, seen_opt)
+    for _ in range(4):
+        for k in ("y", "mean", "dx", "dgamma", "loss", "dz"):
+            seen[k].fill_(5)
+        with torch.cuda.stream(stream):
+            graph.replay()
+        step(eager, eager_opt)
+        torch.cuda.synchronize()
+        for k in eager:
+            assert torch.equal(eager[k], seen[k]), k
+        logits.mul_(0.9), x.mul_(1.25)                       # other inputs at the same addresses
+        torch.cuda.synchronize()
+    ctx.qrm_release_stream(stream)
