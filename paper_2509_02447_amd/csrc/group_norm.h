@@ -330,7 +330,7 @@ template <int V, int W> struct Affine {
 // One launch: R pixels a thread, a whole tile a workgroup.
 template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__(kMaxThreads) void norm_whole_kernel(NormArgs a)
 {
-    extern __shared__ float2 lds[];
+    extern __shared__ __align__(16) float2 lds[];
     float *stats = (float *)(lds + join_floats2(blockDim.x, W, a.rpar)); // mean, rstd of the tile's groups
     const Tile t = find_tile<V>(a);
     const bool active = t.r < t.rpar;
@@ -361,7 +361,7 @@ template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__
 template <typename T, int V, int W> __global__ __launch_bounds__(kMaxThreads) void norm_stats_kernel(NormArgs a)
 {
     constexpr int R = 8;
-    extern __shared__ float2 lds[];
+    extern __shared__ __align__(16) float2 lds[];
     const Tile t = find_tile<V>(a);
     Spread<W> mine;
 #pragma unroll
@@ -387,7 +387,7 @@ template <typename T, int V, int W> __global__ __launch_bounds__(kMaxThreads) vo
 template <typename T, int V, int W, int ACT, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_apply_kernel(NormArgs a)
 {
     constexpr int R = 4;
-    extern __shared__ float2 lds[]; // mean, rstd of the tile's groups
+    extern __shared__ __align__(16) float2 lds[]; // mean, rstd of the tile's groups
     float *stats = (float *)lds;
     const Tile t = find_tile<V>(a);
     const int lanes = lanes_for(t.groups), lane = threadIdx.x & (lanes - 1), first = threadIdx.x / lanes;
@@ -522,12 +522,13 @@ __device__ __forceinline__ void sum_chunk(const NormArgs &a, const Tile &t, cons
     float2 *total = parts < t.rpar || t.rpar == 1 ? lds : second;
 #pragma unroll 1
     for (int j = threadIdx.x; j < nch; j += threads) {
-        float2 s = make_float2(0.f, 0.f);
+        double sb = 0.0, sg = 0.0; // (few channels have many parts)
 #pragma unroll 2
         for (int q = 0; q < parts; ++q) {
-            s.x += sums[q * nch + j].x;
-            s.y += sums[q * nch + j].y;
+            sb += sums[q * nch + j].x;
+            sg += sums[q * nch + j].y;
         }
+        const float2 s = make_float2((float)sb, (float)sg);
         by_channel(j, s.x, s.y);
         const float w = a.gamma ? a.gamma[t.c0 + j] : 1.f;
         total[j] = make_float2(s.x * w, s.y * w);
@@ -550,45 +551,47 @@ __device__ __forceinline__ void sum_chunk(const NormArgs &a, const Tile &t, cons
     }
 }
 
-// dgamma, dbeta of up to 16 channels from c0 on: `terms` sums of each, added in a fixed order by a workgroup.
+// dgamma, dbeta of up to 16 channels from c0 on: `terms` sums of each, added in a fixed order by a workgroup, in 64 bits: they may cancel, and are few.
+// lds: blockDim.x / 2 float2s.
 __device__ __forceinline__ void channel_grads(const NormArgs &a, int64_t terms, int c0, float2 *lds)
 {
     const int c = c0 + threadIdx.x % 16, r = threadIdx.x / 16, rows = blockDim.x / 16;
-    float2 s = make_float2(0.f, 0.f);
+    double b = 0.0, g = 0.0;
     if (c < a.C) {
 #pragma unroll 8
         for (int64_t k = r; k < terms; k += rows) {
             const float2 v = a.chan[k * a.C + c];
-            s.x += v.x;
-            s.y += v.y;
+            b += v.x;
+            g += v.y;
         }
     }
     // lanes 16 apart hold the same channel
     for (int o = 32; o >= 16; o /= 2) {
-        s.x += __shfl_down(s.x, o);
-        s.y += __shfl_down(s.y, o);
+        b += __shfl_down(b, o);
+        g += __shfl_down(g, o);
     }
-    if ((threadIdx.x & 63) < 16) lds[threadIdx.x / 64 * 16 + threadIdx.x % 16] = s;
+    double2 *sums = (double2 *)lds;
+    if ((threadIdx.x & 63) < 16) sums[threadIdx.x / 64 * 16 + threadIdx.x % 16] = make_double2(b, g);
     __syncthreads();
     if (threadIdx.x < 16 && c < a.C) {
         for (int k = 1; k < (int)blockDim.x / 64; ++k) {
-            s.x += lds[k * 16 + threadIdx.x].x;
-            s.y += lds[k * 16 + threadIdx.x].y;
+            b += sums[k * 16 + threadIdx.x].x;
+            g += sums[k * 16 + threadIdx.x].y;
         }
-        if (a.dbeta) a.dbeta[c] = s.x;
-        if (a.dgamma) a.dgamma[c] = s.y;
+        if (a.dbeta) a.dbeta[c] = (float)b;
+        if (a.dgamma) a.dgamma[c] = (float)g;
     }
 }
 __global__ __launch_bounds__(kThreads) void norm_channels_kernel(NormArgs a)
 {
-    __shared__ float2 lds[kThreads / 4];
+    __shared__ __align__(16) float2 lds[kThreads / 2];
     channel_grads(a, a.N * a.parts, blockIdx.x * 16, lds);
 }
 
 // One launch (and one for the channels of several images): R pixels a thread, a whole tile a workgroup.  dz stays in registers beside the input.
 template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__(kMaxThreads / 2) void norm_grad_whole_kernel(NormArgs a)
 {
-    extern __shared__ float2 lds[];
+    extern __shared__ __align__(16) float2 lds[];
     float *sums = (float *)(lds + sum_floats2(blockDim.x, V, a.rpar)); // A, B of the tile's groups
     const Tile t = find_tile<V>(a);
     const int64_t xs = t.step * a.xp, ys = t.step * a.yp;
@@ -646,7 +649,7 @@ template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__
 template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxThreads) void norm_grad_sums_kernel(NormArgs a)
 {
     constexpr int R = 3;
-    extern __shared__ float2 lds[];
+    extern __shared__ __align__(16) float2 lds[];
     const Tile t = find_tile<V>(a);
     const int pixels = t.r < t.rpar ? pixels_at(t, t.r) : 0;
     const T *p = x_at<T, V>(a, t, pixels ? t.r : 0);
@@ -689,7 +692,7 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
 template <typename T, int V, int W, int ACT, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_grad_apply_kernel(NormArgs a, uint32_t apply_blocks)
 {
     constexpr int R = 2;
-    extern __shared__ float2 lds[];
+    extern __shared__ __align__(16) float2 lds[];
     if (blockIdx.x >= apply_blocks) {
         channel_grads(a, a.N * a.parts, (blockIdx.x - apply_blocks) * 16, lds);
         return;
@@ -841,7 +844,7 @@ template <typename T> hipError_t norm_backward(const NormCall &c, const NormPlan
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const uint32_t apply = c.dx ? p.second.blocks(c.d.N) : 0;
-        const size_t own = std::max(2 * (p.second.ct / a.D) * sizeof(float), p.second.threads / 4 * sizeof(float2));
+        const size_t own = std::max(2 * (p.second.ct / a.D) * sizeof(float), p.second.threads / 2 * sizeof(float2));
         auto launch = [&](auto stream) {
             hipLaunchKernelGGL((norm_grad_apply_kernel<T, V, W, ACT, decltype(stream)::value>), dim3(apply + extra), dim3(p.second.threads), own, s,
                                norm_args(c, p, p.second, ws), apply);
