@@ -46,18 +46,25 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
     };
 
     // One launch where a tile of an image fits a workgroup, if that is over before a second launch would have begun or keeps all compute units
-    // busy.  Tiles of 64 bytes where there are few, of a line else.  Measured with silu, one launch / two, us: bf16, 4 images of 512 channels, 16 / 256 /
-    // 1024 / 2048 pixels 5.6 / 9.0, 6.0 / 10.0, 9.6 / 13.9, 13.5 / 12.7; 32 of 2048 pixels 27.7 / 38.5; backward, 4 images, 256 / 512 / 1024 pixels
-    // 9.8 / 11.7, 12.1 / 13.8, 18.3 / 13.8; 32 of 512 19.2 / 21.2.
+    // busy.  Where tiles of a line leave compute units idle, they are half a line wide, and a quarter where there are very few (narrow ones share their lines
+    // with other dies' caches).  Measured with silu and bf16, one launch / two, us: 1 image of 512 channels, 64 / 256 / 1024 / 2048 pixels 5.7 / 9.3,
+    // 5.7 / 9.7, 7.4 / 9.8, 10.1 / 9.9; 4 images of 256 / 1024 / 2048 pixels 6.0 / 9.9, 9.6 / 10.3, 13.4 / 12.3; 16 of 1024 13.6 / 16.4; 32 of 2048
+    // 27.7 / 38.5; backward, 1 image, 256 / 1024 / 2048 pixels 7.0 / 11.5, 11.1 / 11.6, 18.7 / 11.8; 4 of 256 / 512 / 1024 9.6 / 11.7, 11.7 / 11.8, 18.0 / 12.3.
     const int most_threads = p.W > 2 ? 256 : backward ? kNormMaxThreads / 2 : kNormMaxThreads;
     p.first = cut(128, 64);
     const bool many_tiles = d.N * p.first.tiles >= num_cu;
-    if (!many_tiles) p.first = cut(64, 64);
+    if (!many_tiles) {
+        const NormCut half = cut(64, 64), quarter = cut(32, 64);
+        if (d.N * quarter.tiles <= num_cu / 4) p.first = quarter;
+        else if (d.N * half.tiles <= num_cu) p.first = half;
+    }
+    const int64_t most = backward || p.first.ct * size < 64 ? 16384 : 32768; // elements of a tile
     const int cols = p.first.ct / p.V;
     auto threads_for = [&](int pixels) { return std::min<int64_t>(INT32_MAX, ((d.P + pixels - 1) / pixels * cols + 255) / 256 * 256); };
     p.pixels = threads_for(kNormFew) <= most_threads ? kNormFew : norm_many(backward, p.W);
     const int64_t threads = threads_for(p.pixels);
-    p.whole = threads <= most_threads && d.P <= p.pixels * (threads / cols) && (many_tiles || d.P * p.first.ct <= (backward ? 16384 : 32768));
+    p.whole = threads <= most_threads && d.P <= p.pixels * (threads / cols) &&
+              (many_tiles || (d.P * p.first.ct <= most && !(backward && d.N > 1 && d.P > 512)));
     if (p.whole) {
         p.first.threads = (int)threads;
         p.part_words = 0;
