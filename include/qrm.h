@@ -36,7 +36,9 @@
  *     call.  When more streams than that have been used, a stream not seen
  *     before takes over the workspace whose last call lies furthest back; its
  *     work is ordered (on the device) behind that call, so results stay
- *     correct, and streams that no longer exist cost nothing.
+ *     correct, and streams that no longer exist cost nothing.  (Where that
+ *     last call was one of the fine-tuning calls, the host waits for the
+ *     device instead: those calls leave no event behind.)
  *     qrm_release_stream hands a stream's workspace back explicitly.
  */
 #ifndef QRM_H

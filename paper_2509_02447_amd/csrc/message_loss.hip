@@ -1,8 +1,9 @@
 // Message loss with its gradient (qrm_message_loss).
 //
 // A lane takes a symbol, 2^k lanes an image: the image's expected number of wrong symbols, which every bit's gradient depends on, is a sum over
-// neighbouring lanes.  Workgroups leave their part of the loss in 64 bits; the last one that is done adds them up, in their order.  Bound by launch
-// latency up to thousands of images, by memory beyond (9 bytes a bit).
+// neighbouring lanes.  Workgroups leave their part of the loss in 64 bits; the last one that is done adds them up, in their order.  Bound by latency: 4 images
+// of 48 bits 2.5 us, a launch and one round of loads; 16384 of 96 bits (14 MB) 10.3 us, of which loads and arithmetic take 5 (a quarter of the lanes have no
+// symbol), counting the workgroups 3 and adding their parts 1.5.
 #include "qrm_train.h"
 
 #include <algorithm>
