@@ -376,7 +376,8 @@ QRM_API qrm_status qrm_profile_read_chunks(qrm_ctx *ctx, int32_t max_chunks, dou
  * Fine-tuning (Section 4.2: the image decoder is taught to write the key, with a message loss on the extractor's logits and some hundred
  * AdamW steps).  The calls below are the parts of such a step that are not matrix products; they take any context, whatever it was
  * created with, unless stated.  They can be recorded into a HIP graph on a stream that has run the same calls on the context before (its
- * workspace is there then); replays of a graph and other calls that use the same stream's workspace must not overlap in time.
+ * workspace is there then; a qrm_message_loss that would have to clear counters first is refused, QRM_E_INVALID); replays of a graph and
+ * other calls that use the same stream's workspace must not overlap in time.
  * Types of tensors: */
 typedef enum { QRM_F32 = 0, QRM_BF16 = 1, QRM_F16 = 2 } qrm_type;
 typedef enum { QRM_ACT_NONE = 0, QRM_ACT_RELU = 1, QRM_ACT_SILU = 2 } qrm_act;
@@ -398,9 +399,10 @@ typedef enum { QRM_ACT_NONE = 0, QRM_ACT_RELU = 1, QRM_ACT_SILU = 2 } qrm_act;
  * The same bits from call to call.  A value that is not finite reaches the outputs of its group in its image and dgamma, dbeta of that
  * group's channels, no others.
  * Errors: QRM_E_INVALID (NULL pointer, N < 0, P < 1, groups that do not divide C, an unknown type or activation, eps not above
- * zero, strides under C or (P-1) * pixel + C, a pointer not aligned to its elements, one of d_mean and d_rstd alone),
+ * zero, strides under C or (P-1) * pixel + C, an output in place of an input with other strides, a pointer not aligned to its elements,
+ * one of d_mean and d_rstd alone),
  * QRM_E_UNSUPPORTED (C above 65536, a group of more than 1024 pieces of what the alignment allows to read at once, up to 16 bytes;
- * N or P of 2^31 and more), QRM_E_NOMEM.
+ * N or P of 2^31 and more, 2^32 threads and more for the tiles of all images: 2^24 images of one pixel), QRM_E_NOMEM.
  */
 typedef struct {
     int64_t N, P;
@@ -436,7 +438,8 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
  * A launch takes the gradients of several hundred tensors.  qrm_adamw_destroy waits for the device; NULL is ignored.
  * Errors: QRM_E_INVALID (NULL pointer, n < 0, unknown type, state_bits not 8 or 32, a copy of other than 16 bits or beside parameters that are
  * not f32, a pointer not aligned to its elements, step < 1, lr, weight_decay, lr_scale or eps negative or not finite, a beta outside [0, 1), a plan of
- * another device), QRM_E_NOMEM, QRM_E_UNSUPPORTED (a plan of 2^31 and more pieces of 4096 elements).
+ * another device), QRM_E_NOMEM, QRM_E_UNSUPPORTED (a plan of 2^24 and more pieces of 4096 elements; 2^36 codes
+ * and more to unpack).
  *
  * qrm_unpack_moment: the values that 8-bit codes stand for, f32 or bf16 [n]: moment 0 = m, 1 = v.
  */

@@ -456,6 +456,7 @@ class AdamW:
         n = len(self._keep)
         rows = (_AdamwTensor * max(1, n))()
         for r, t in zip(rows, self._keep):
+            self._check_sizes(t)
             r.n = t["param"].numel()
             r.d_param, r.d_m, r.d_v = _dptr(t["param"]), _dptr(t["m"]), _dptr(t["v"])
             r.d_m_scale, r.d_v_scale, r.d_copy = _dptr(t.get("m_scale")), _dptr(t.get("v_scale")), _dptr(t.get("copy"))
@@ -470,6 +471,17 @@ class AdamW:
         ctx._check(self._lib.qrm_adamw_create(ctx._h, C.byref(desc), rows, C.byref(self._h)))
         self._n, self._grad_type, self._sizes = n, grad_type, [t["param"].numel() for t in self._keep]
         self._array = C.c_void_p * max(1, n)
+
+    @staticmethod
+    def _check_sizes(t):
+        import torch
+        n, eight = t["param"].numel(), t["m"].dtype == torch.int8
+        assert t["m"].numel() == n and t["v"].numel() == n, "moments have their parameters' sizes"
+        assert t["v"].dtype == (torch.uint8 if eight else t["m"].dtype), "moments are f32 both, or int8 and uint8"
+        if eight and n:
+            assert all(t[k].dtype == torch.float32 and t[k].numel() == -(-n // QRM_MOMENT_BLOCK) for k in ("m_scale", "v_scale")), \
+                "8-bit moments have one f32 scale for QRM_MOMENT_BLOCK elements"
+        assert t.get("copy") is None or t["copy"].numel() == n, "a copy has its parameters' size"
 
     @staticmethod
     def _mixed(what):

@@ -308,7 +308,7 @@ hipError_t launch_adamw(const AdamwTypes &t, const AdamwTensor *tensors, const u
                          : launch_counted<kAdamwGrads>(t, tensors, pieces + first, count, t0, grads, n_grads, step, s);
 }
 
-hipError_t launch_unpack_moment(int moment, const void *codes, const float *scales, int64_t n, int out_type, void *out, int, hipStream_t s)
+hipError_t launch_unpack_moment(int moment, const void *codes, const float *scales, int64_t n, int out_type, void *out, hipStream_t s)
 {
     const dim3 grid((uint32_t)((n + kUnpack * kThreads - 1) / (kUnpack * kThreads)));
     if (out_type == QRM_F32)

@@ -13,7 +13,6 @@ namespace qrm {
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kVm0 = (7 << 4) | (15 << 8); // s_waitcnt vmcnt(0) alone
 
 struct LossArgs {
     const float *logits;
@@ -187,7 +186,7 @@ template <int M> __global__ __launch_bounds__(kThreads) void message_loss_kernel
     // parts and count are stored past the L2s; a part has arrived before its workgroup is counted
     if (threadIdx.x == 0) {
         __hip_atomic_store(a.partial + blockIdx.x, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __builtin_amdgcn_s_waitcnt(kVm0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         last = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
         if (last) __hip_atomic_store(a.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }

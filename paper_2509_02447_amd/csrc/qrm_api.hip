@@ -433,12 +433,16 @@ qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
 qrm_status get_counters(qrm_ctx *c, hipStream_t s, QrmSlot *slot)
 {
     if (slot->counters) return QRM_OK;
+    // (a graph that clears them would do so at every replay)
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone)
+        return fail(c, QRM_E_INVALID, "a stream's first call of this kind cannot be recorded into a graph");
     void *p = nullptr;
     if (hipMalloc(&p, kSlotCounters * sizeof(uint32_t)) != hipSuccess) {
         (void)hipGetLastError();
         return fail(c, QRM_E_NOMEM, "no device memory for a workspace's counters");
     }
-    const hipError_t e = hipMemsetAsync(p, 0, kSlotCounters * sizeof(uint32_t), s); // (never in a graph: nothing can be allocated while one is recorded)
+    const hipError_t e = hipMemsetAsync(p, 0, kSlotCounters * sizeof(uint32_t), s);
     if (e != hipSuccess) {
         (void)hipFree(p);
         return hip_fail(c, e, "hipMemsetAsync(counters)");

@@ -161,7 +161,7 @@ struct AdamwTypes {
 // Pieces first .. first + count - 1 of the plan, which belong to tensors t0 .. t0 + grads - 1.
 hipError_t launch_adamw(const AdamwTypes &t, const AdamwTensor *tensors, const uint2 *pieces, uint32_t first, uint32_t count, uint32_t t0,
                         const void *const *grads, int n_grads, const AdamwStep &step, hipStream_t s);
-hipError_t launch_unpack_moment(int moment, const void *codes, const float *scales, int64_t n, int out_type, void *out, int num_cu, hipStream_t s);
+hipError_t launch_unpack_moment(int moment, const void *codes, const float *scales, int64_t n, int out_type, void *out, hipStream_t s);
 
 // ---- message loss
 

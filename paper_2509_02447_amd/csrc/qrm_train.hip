@@ -58,6 +58,12 @@ qrm_status check_norm(qrm_ctx *c, const qrm_group_norm_desc *desc, qrm_group_nor
     return QRM_OK;
 }
 
+// An output in place of an input has to have its strides: otherwise it falls on pixels that are still to be read.
+bool same_places(const qrm_group_norm_desc &d)
+{
+    return (d.P == 1 || d.x_pixel == d.y_pixel) && (d.N <= 1 || d.x_image == d.y_image);
+}
+
 qrm_status start(qrm_ctx *c)
 {
     hipError_t e = hipSetDevice(c->device);
@@ -68,7 +74,9 @@ qrm_status plan(qrm_ctx *c, const qrm_group_norm_desc &d, int align, bool backwa
 {
     if (!plan_norm(d, align, backward, channels, c->num_cu, p))
         return fail(c, QRM_E_UNSUPPORTED, "a group has more than 1024 pieces of what the alignment allows to read at once");
-    if ((double)d.N * p->first.tiles * p->first.chunks > 2e9 || (!p->whole && (double)d.N * p->second.tiles * p->second.chunks > 2e9)) return fail(c, QRM_E_UNSUPPORTED, "more than 2^31 tiles");
+    // (a launch has less than 2^32 threads; those behind the tiles, of the channels, are under 2^24)
+    auto fits = [&](const NormCut &cut) { return ((double)d.N * cut.tiles * cut.chunks + 8192.0) * cut.threads < 4294967296.0; };
+    if (!fits(p->first) || (!p->whole && !fits(p->second))) return fail(c, QRM_E_UNSUPPORTED, "the tiles of all images need 2^32 threads and more");
     return QRM_OK;
 }
 
@@ -86,6 +94,7 @@ qrm_status qrm_group_norm(qrm_ctx *c, const qrm_group_norm_desc *desc, const voi
     if (!d_mean != !d_rstd) return fail(c, QRM_E_INVALID, "d_mean and d_rstd go together");
     if (call.d.N == 0) return QRM_OK;
     if (!d_x || !d_y) return fail(c, QRM_E_INVALID, "d_x / d_y is NULL");
+    if (d_x == d_y && !same_places(call.d)) return fail(c, QRM_E_INVALID, "d_y is d_x, with other strides");
     const int align = common_alignment({d_x, d_y});
     if (align < type_bytes(call.d.type) || !aligned_to(d_gamma, 4) || !aligned_to(d_beta, 4) || !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4))
         return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
@@ -94,10 +103,9 @@ qrm_status qrm_group_norm(qrm_ctx *c, const qrm_group_norm_desc *desc, const voi
     call.x = d_x; call.y = d_y; call.gamma = d_gamma; call.beta = d_beta; call.mean = d_mean; call.rstd = d_rstd;
     QrmSlot *slot = nullptr;
     if (p.bytes && (st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
+    if (slot) slot_used(slot); // (also where only the first of two launches comes off)
     hipError_t e = launch_norm_forward(call, p, slot ? slot->ws : nullptr, (hipStream_t)stream);
-    if (e != hipSuccess) return hip_fail(c, e, "group_norm launch");
-    if (slot) slot_used(slot);
-    return QRM_OK;
+    return e == hipSuccess ? QRM_OK : hip_fail(c, e, "group_norm launch");
 }
 
 qrm_status qrm_group_norm_backward(qrm_ctx *c, const qrm_group_norm_desc *desc, const void *d_x, const void *d_dy, const float *d_gamma,
@@ -111,6 +119,7 @@ qrm_status qrm_group_norm_backward(qrm_ctx *c, const qrm_group_norm_desc *desc, 
     const bool none = call.d.N == 0;
     if (!none && (!d_x || !d_dy || !d_mean || !d_rstd)) return fail(c, QRM_E_INVALID, "d_x / d_dy / d_mean / d_rstd is NULL");
     if (!d_dx && !d_dgamma && !d_dbeta) return fail(c, QRM_E_INVALID, "no output is asked for");
+    if (!none && d_dx == d_dy && !same_places(call.d)) return fail(c, QRM_E_INVALID, "d_dx is d_dy, with other strides");
     const int align = common_alignment({d_x, d_dy, d_dx});
     if (align < type_bytes(call.d.type) || !aligned_to(d_gamma, 4) || !aligned_to(d_beta, 4) || !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4) ||
         !aligned_to(d_dgamma, 4) || !aligned_to(d_dbeta, 4))
@@ -127,10 +136,9 @@ qrm_status qrm_group_norm_backward(qrm_ctx *c, const qrm_group_norm_desc *desc, 
     if ((st = plan(c, call.d, align, true, d_dgamma || d_dbeta, &p)) != QRM_OK || (st = start(c)) != QRM_OK) return st;
     QrmSlot *slot = nullptr;
     if (p.bytes && (st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
-    hipError_t e = launch_norm_backward(call, p, slot ? slot->ws : nullptr, (hipStream_t)stream);
-    if (e != hipSuccess) return hip_fail(c, e, "group_norm_backward launch");
     if (slot) slot_used(slot);
-    return QRM_OK;
+    hipError_t e = launch_norm_backward(call, p, slot ? slot->ws : nullptr, (hipStream_t)stream);
+    return e == hipSuccess ? QRM_OK : hip_fail(c, e, "group_norm_backward launch");
 }
 
 qrm_status qrm_adamw_create(qrm_ctx *c, const qrm_adamw_desc *desc, const qrm_adamw_tensor *h_tensors, qrm_adamw **out)
@@ -163,7 +171,7 @@ qrm_status qrm_adamw_create(qrm_ctx *c, const qrm_adamw_desc *desc, const qrm_ad
                 return fail(c, QRM_E_INVALID, "weight_decay and lr_scale must be finite and not negative");
             total += ((uint64_t)t.n + kAdamwPiece - 1) / kAdamwPiece;
             elements += (uint64_t)t.n;
-            if (total > INT32_MAX) return fail(c, QRM_E_UNSUPPORTED, "more than 2^31 pieces of 4096 elements");
+            if (total >= (1u << 24)) return fail(c, QRM_E_UNSUPPORTED, "2^24 and more pieces of 4096 elements"); // (a launch has less than 2^32 threads)
         }
         tensors.reserve(n);
         pieces.reserve(total);
@@ -260,12 +268,12 @@ qrm_status qrm_unpack_moment(qrm_ctx *c, int32_t moment, const void *d_codes, co
     if (n < 0) return fail(c, QRM_E_INVALID, "n < 0");
     if (out_type != QRM_F32 && out_type != QRM_BF16) return fail(c, QRM_E_INVALID, "values are f32 or bf16");
     if (n == 0) return QRM_OK;
-    if (n > (int64_t)INT32_MAX * 1024) return fail(c, QRM_E_UNSUPPORTED, "n of 2^41 and more");
+    if (n >= (int64_t)1 << 36) return fail(c, QRM_E_UNSUPPORTED, "n of 2^36 and more"); // (a launch has less than 2^32 threads)
     if (!d_codes || !d_scales || !d_out) return fail(c, QRM_E_INVALID, "d_codes / d_scales / d_out is NULL");
     if (!aligned_to(d_scales, 4) || !aligned_to(d_out, type_bytes(out_type))) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
     qrm_status st = start(c);
     if (st != QRM_OK) return st;
-    hipError_t e = launch_unpack_moment(moment, d_codes, d_scales, n, out_type, d_out, c->num_cu, (hipStream_t)stream);
+    hipError_t e = launch_unpack_moment(moment, d_codes, d_scales, n, out_type, d_out, (hipStream_t)stream);
     return e == hipSuccess ? QRM_OK : hip_fail(c, e, "unpack_moment launch");
 }
 
@@ -291,10 +299,9 @@ qrm_status qrm_message_loss(qrm_ctx *c, const float *d_logits, const uint8_t *d_
     if (blocks > 1 && ((st = get_slot(c, (hipStream_t)stream, (size_t)blocks * sizeof(double), &slot)) != QRM_OK ||
                        (st = get_counters(c, (hipStream_t)stream, slot)) != QRM_OK))
         return st;
-    hipError_t e = launch_message_loss(call, slot ? (double *)slot->ws : nullptr, slot ? slot->counters : nullptr, (hipStream_t)stream);
-    if (e != hipSuccess) return hip_fail(c, e, "message_loss launch");
     if (slot) slot_used(slot);
-    return QRM_OK;
+    hipError_t e = launch_message_loss(call, slot ? (double *)slot->ws : nullptr, slot ? slot->counters : nullptr, (hipStream_t)stream);
+    return e == hipSuccess ? QRM_OK : hip_fail(c, e, "message_loss launch");
 }
 
 } // extern "C"
