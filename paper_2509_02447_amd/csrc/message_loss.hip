@@ -2,8 +2,8 @@
 //
 // A lane takes a symbol, 2^k lanes an image: the image's expected number of wrong symbols, which every bit's gradient depends on, is a sum over
 // neighbouring lanes.  Workgroups leave their part of the loss in 64 bits; the last one that is done adds them up, in their order.  Bound by latency: 4 images
-// of 48 bits 2.5 us, a launch and one round of loads; 16384 of 96 bits (14 MB) 10.3 us, of which loads and arithmetic take 5 (a quarter of the lanes have no
-// symbol), counting the workgroups 3 and adding their parts 1.5.
+// of 48 bits 2.5 us, a launch and one round of loads; 16384 of 96 bits (14 MB) 8.7 us, of which loads and arithmetic take 5 (a quarter of the lanes have no
+// symbol), the rest counting the workgroups and adding their parts.  All 256 counted in one word: 10.5 us; workgroups of 512 or 256 threads: the same within 0.3.
 #include "qrm_train.h"
 
 #include <algorithm>
@@ -13,6 +13,7 @@ namespace qrm {
 namespace {
 
 constexpr int kThreads = 1024;
+constexpr int kSet = 16, kLine = 32; // workgroups that share a count; words from one count to the next
 
 struct LossArgs {
     const float *logits;
@@ -187,8 +188,14 @@ template <int M> __global__ __launch_bounds__(kThreads) void message_loss_kernel
     if (threadIdx.x == 0) {
         __hip_atomic_store(a.partial + blockIdx.x, total, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        last = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
-        if (last) __hip_atomic_store(a.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // (additions to one word follow each other: sixteen workgroups share one, in a line of its own, and the last of them counts on in the first word)
+        const auto counted = [](uint32_t *word, uint32_t all) {
+            const bool full = __hip_atomic_fetch_add(word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == all;
+            if (full) __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            return full;
+        };
+        const uint32_t sets = (gridDim.x + kSet - 1) / kSet, set = blockIdx.x % sets;
+        last = counted(a.done + (1 + set) * kLine, gridDim.x / sets + (set < gridDim.x % sets)) && counted(a.done, sets);
     }
     write_image();
     lds_barrier();
@@ -208,7 +215,7 @@ int lanes_of(int n)
 
 } // namespace
 
-// Workgroups of a call: one for up to four images a lane group of 1024 threads, else at most 256, whose counting takes a microsecond.
+// Workgroups of a call: one for up to four images a lane group of 1024 threads, else at most 256: one to a compute unit.
 int64_t loss_blocks(int64_t N, int n)
 {
     const int64_t per = kThreads / lanes_of(n);

@@ -98,3 +98,20 @@ def test_first_recorded_loss_is_refused(ctx, qrm):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(loss, eager)
+
+
+@pytest.mark.parametrize("workgroups", [5, 15, 16, 17, 31, 33, 100, 255, 256, 300])
+def test_loss_counts_every_workgroup(ctx, workgroups):
+    """64 images of 12 symbols to a workgroup, the last one not full.  All terms are positive: a relative bound of the 48 additions of an image,
+    a logit's functions (four roundings, a unit of each of three) and two roundings of the mean: under 80 half units of 32 bits."""
+    N = 64 * workgroups - 7
+    g = torch.Generator().manual_seed(workgroups)
+    logits = 3 * torch.randn((N, 48), generator=g)
+    target = (torch.rand((N, 48), generator=g) < 0.5).to(torch.uint8)
+    want = torch.nn.functional.binary_cross_entropy_with_logits(logits.double(), target.double()).item()
+    dev, dev_target, loss = logits.cuda(), target.cuda(), torch.zeros(3, device="cuda")
+    for i in range(3):  # (the counts are left as they were found)
+        ctx.qrm_message_loss(dev, dev_target, N, N, 48, 0.0, loss[i:i + 1])
+    got = loss.cpu()
+    assert torch.equal(got[1:], got[:2])
+    assert abs(got[0].item() - want) <= 80 * 2.0 ** -24 * want
