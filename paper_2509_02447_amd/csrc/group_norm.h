@@ -25,6 +25,7 @@ namespace qrm {
 namespace {
 
 constexpr int kThreads = kNormThreads, kMaxThreads = kNormMaxThreads;
+constexpr uint32_t kDies = 8; // workgroups go to the dies in turn, each with an L2 of its own
 
 struct NormArgs {
     const void *x, *dy;
@@ -37,6 +38,8 @@ struct NormArgs {
     int64_t xp, xn, yp, yn;
     int C, G, D;
     int ct, tiles, chunks, rpar; // this launch's cut; rpar: pixels side by side
+    int side;                    // neighbouring tiles that lie in the same lines
+    uint32_t turned;             // .. and the workgroups that are numbered for it
     int parts, parts_rpar;       // the first launch's chunks and pixels side by side
     int act;
     float eps;
@@ -60,6 +63,10 @@ template <int V> __device__ __forceinline__ Tile find_tile(const NormArgs &a)
 {
     Tile t;
     uint32_t b = blockIdx.x;
+    if (b < a.turned) {
+        const uint32_t k = b / kDies, set = kDies * a.side;
+        b = b / set * set + b % kDies * a.side + k % a.side;
+    }
     t.t = b % a.tiles;
     b /= a.tiles;
     t.s = b % a.chunks;
@@ -771,6 +778,8 @@ NormArgs norm_args(const NormCall &c, const NormPlan &p, const NormCut &cut, voi
     a.xp = c.d.x_pixel; a.xn = c.d.x_image; a.yp = c.d.y_pixel; a.yn = c.d.y_image;
     a.C = c.d.C; a.G = c.d.groups; a.D = c.d.C / c.d.groups; 
     a.ct = cut.ct; a.tiles = cut.tiles; a.chunks = cut.chunks; a.rpar = cut.threads / (cut.ct / p.V);
+    a.side = p.whole ? std::max(1, 128 / (cut.ct * type_bytes(c.d.type))) : 1;
+    a.turned = a.side > 1 ? cut.blocks(a.N) / (kDies * a.side) * (kDies * a.side) : 0;
     a.parts = p.first.chunks; a.parts_rpar = p.first.threads / (p.first.ct / p.V);
     a.eps = c.d.eps;
     a.act = c.d.act;

@@ -45,30 +45,38 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
         c.chunks = (int)std::min(want, std::max<int64_t>(1, d.P / (4 * rpar)));
     };
 
-    // One launch where a tile of an image fits a workgroup, if that is over before a second launch would have begun or keeps all compute units
-    // busy.  Where tiles of a line leave compute units idle, they are half a line wide, and a quarter where there are very few (narrow ones share their lines
-    // with other dies' caches).  Measured with silu and bf16, one launch / two, us: 1 image of 512 channels, 64 / 256 / 1024 / 2048 pixels 5.7 / 9.3,
-    // 5.7 / 9.7, 7.4 / 9.8, 10.1 / 9.9; 4 images of 256 / 1024 / 2048 pixels 6.0 / 9.9, 9.6 / 10.3, 13.4 / 12.3; 16 of 1024 13.6 / 16.4; 32 of 2048
-    // 27.7 / 38.5; backward, 1 image, 256 / 1024 / 2048 pixels 7.0 / 11.5, 11.1 / 11.6, 18.7 / 11.8; 4 of 256 / 512 / 1024 9.6 / 11.7, 11.7 / 11.8, 18.0 / 12.3.
+    // A tile for one launch is the narrowest, down to 16 channels (8 forward), of which there are not many more than compute units: a line's tiles are numbered so
+    // that one die's cache serves them all (find_tile).  One launch is taken where a tile fits a workgroup and is over before a second launch would have
+    // begun, or where compute units are busy anyway and the map is read once.  Measured with silu and 512 channels in bf16, one launch / two, us: 1 image of 256 /
+    // 1024 / 2048 pixels 5.7 / 9.7, 7.4 / 9.7, 10.1 / 9.9; 4 images of 1024 / 2048 / 4096 7.9 / 10.2, 11.1 / 12.2, 16.4 / 16.4 (tiles of a line, 1024 pixels: 12.8); 16
+    // images 11.7 / 16.3, 18.9 / 22.5, 28.8 / 34.6 (a line 14.7, 24.1); backward, 1 image of 256 / 1024 / 2048 pixels 6.4 / 11.6, 8.7 / 11.6, 14.8 / 11.8; 4 images 9.1 / 11.7,
+    // 11.8 / 12.3, 18.7 / 15.4; 16 images of 512 / 1024 11.7 / 15.3, 18.3 / 20.2.
     const int most_threads = p.W > 2 ? 256 : backward ? kNormMaxThreads / 2 : kNormMaxThreads;
-    p.first = cut(128, 64);
-    const bool many_tiles = d.N * p.first.tiles >= num_cu;
-    if (!many_tiles) {
-        const NormCut half = cut(64, 64), quarter = cut(32, 64);
-        if (d.N * quarter.tiles <= num_cu / 4) p.first = quarter;
-        else if (d.N * half.tiles <= num_cu) p.first = half;
-    }
-    const int64_t most = backward || p.first.ct * size < 64 ? 16384 : 32768; // elements of a tile
-    const int cols = p.first.ct / p.V;
-    auto threads_for = [&](int pixels) { return std::min<int64_t>(INT32_MAX, ((d.P + pixels - 1) / pixels * cols + 255) / 256 * 256); };
-    p.pixels = threads_for(kNormFew) <= most_threads ? kNormFew : norm_many(backward, p.W);
-    const int64_t threads = threads_for(p.pixels);
-    p.whole = threads <= most_threads && d.P <= p.pixels * (threads / cols) &&
-              (many_tiles || (d.P * p.first.ct <= most && !(backward && d.N > 1 && d.P > 512)));
-    if (p.whole) {
+    const int least = (backward ? 16 : 8) * size;
+    auto fit = [&] { // pixels and threads of a tile
+        const int cols = p.first.ct / p.V;
+        auto threads_for = [&](int pixels) { return std::min<int64_t>(INT32_MAX, ((d.P + pixels - 1) / pixels * cols + 255) / 256 * 256); };
+        p.pixels = threads_for(kNormFew) <= most_threads ? kNormFew : norm_many(backward, p.W);
+        const int64_t threads = threads_for(p.pixels);
         p.first.threads = (int)threads;
-        p.part_words = 0;
-    } else {
+        return threads <= most_threads && d.P <= p.pixels * (threads / cols);
+    };
+    int bytes = 128;
+    p.first = cut(bytes, 64);
+    while (bytes / 2 >= least) {
+        const NormCut half = cut(bytes / 2, 64);
+        if (d.N * half.tiles > num_cu + num_cu / 2) break;
+        p.first = half, bytes /= 2;
+    }
+    p.whole = fit();
+    while (!p.whole && !backward && bytes / 2 >= least) {
+        p.first = cut(bytes /= 2, 64);
+        p.whole = fit();
+    }
+    const int64_t blocks = d.N * p.first.tiles, elements = d.P * p.first.ct;
+    if (backward) p.whole = p.whole && elements * size <= (blocks >= num_cu ? 65536 : 32768);
+    else p.whole = p.whole && (blocks >= num_cu || elements <= (blocks >= num_cu / 2 ? 32768 : 16384));
+    if (!p.whole) {
         // (few chunks in the first launch: every workgroup of the second reads its groups' parts of all of them)
         p.first = p.second = cut(128, kNormThreads);
         deal(p.first, 2);
