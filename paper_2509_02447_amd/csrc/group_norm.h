@@ -1,7 +1,7 @@
 // Group norm with an activation, channels last, forward and backward: the kernels and their launches for one element type (group_norm_f32.hip,
 // group_norm_bf16.hip, group_norm_f16.hip).
 //
-// The work is cut into tiles of whole groups, a 128-byte line wide or a little more, and a tile's pixels into chunks, one to a workgroup.  A
+// The work is cut into tiles of whole groups, a 128-byte line wide or a little more (a part of a line in one launch), and a tile's pixels into chunks, one to a workgroup.  A
 // thread keeps one piece of V channels (up to 16 bytes) and walks down the chunk's pixels, so that scale, bias and statistics of its channels stay in
 // registers.  Statistics need all of a group before the first output: a map whose tiles fit the registers of a workgroup each takes one launch and is read once;
 // all others take two, of which one leaves each chunk's part and the other joins the parts of its groups in a fixed order and reads the map again.
@@ -9,7 +9,7 @@
 // Bound by memory where the map is large: 4 images of 256 x 256 pixels and 128 channels in bf16 take 37.4 us (15.6 + 22.3, 201 MB read and written at 5.4 TB/s; read
 // once, at the rate of a large copy, 26.2), their backward pass 59.9 us (29.7 + 32.5, 335 MB at 5.6 TB/s; 39.2).  The second reading comes from the memory-side cache in part.  Vector
 // instructions (silu: 20 slots an element forward, 43 backward, an exponential and an inverse four each) are 17 and 36 us of that and run beside the memory.  Bound
-// by latency where it is small: 4 images of 32 x 32 and 512 channels 9.7 us, on 64 compute units.
+// by latency where it is small: 4 images of 32 x 32 and 512 channels 7.9 us.
 //
 // Tried and not kept: one launch for large maps, whose chunks stay in registers while the workgroups of a tile send each other their parts through memory.  The map
 // is read once, but loading, arithmetic, exchange (3 .. 15 us: chunks^2 reads of few lines) and storing follow each other in lockstep: 52.6 us for the first map above, 98.6
@@ -58,7 +58,8 @@ struct Tile {
 // Pixels of a chunk that the threads at `r` of those side by side take: the chunks take turns, so that all workgroups move down the map together.
 __device__ __forceinline__ int pixels_at(const Tile &t, int r) { return t.base + (r < t.extra); }
 
-// The tiles of the same pixels lie side by side in the grid.
+// The tiles of the same pixels lie side by side in the grid; those that share lines are numbered kDies apart, so that one die's cache serves them: 4 images of 1024
+// pixels and 512 channels, tiles of a quarter line, 7.9 us against 8.6, of 2048 pixels 11.1 against 15.0.
 template <int V> __device__ __forceinline__ Tile find_tile(const NormArgs &a)
 {
     Tile t;
@@ -342,7 +343,7 @@ template <int V, int W> struct Affine {
 
 // One launch: R pixels a thread, a whole tile a workgroup.  1 image of 256 pixels and 512 channels (bf16, silu) 5.7 us, of which 4 are launch and
 // the first loads; two launches 9.7.
-template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__(kMaxThreads) void norm_whole_kernel(NormArgs a)
+template <typename T, int V, int W, int ACT, int R, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_whole_kernel(NormArgs a)
 {
     extern __shared__ __align__(16) float2 lds[];
     float *stats = (float *)(lds + join_floats2(blockDim.x, W, a.rpar)); // mean, rstd of the tile's groups
@@ -367,7 +368,7 @@ template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__
     for (int i = 0; i < R; ++i)
         if (i < pixels) {
             x[i].pin();
-            store_words<false, T, V>(q + i * ys, f.template apply<ACT>(x[i], a.act));
+            store_words<STREAM, T, V>(q + i * ys, f.template apply<ACT>(x[i], a.act));
         }
 }
 
@@ -825,8 +826,12 @@ template <typename T> hipError_t norm_forward(const NormCall &c, const NormPlan 
         const size_t join = join_floats2(p.first.threads, W, a.rpar) * sizeof(float2);
         if (p.whole) {
             const size_t own = 2 * (p.first.ct / a.D) * sizeof(float);
-            if (p.pixels > kNormFew) hipLaunchKernelGGL((norm_whole_kernel<T, V, W, ACT, norm_many(false, W)>), grid, block, join + own, s, a);
-            else hipLaunchKernelGGL((norm_whole_kernel<T, V, W, ACT, kNormFew>), grid, block, join + own, s, a);
+            auto whole = [&](auto stream) {
+                constexpr bool STREAM = decltype(stream)::value;
+                if (p.pixels > kNormFew) hipLaunchKernelGGL((norm_whole_kernel<T, V, W, ACT, norm_many(false, W), STREAM>), grid, block, join + own, s, a);
+                else hipLaunchKernelGGL((norm_whole_kernel<T, V, W, ACT, kNormFew, STREAM>), grid, block, join + own, s, a);
+            };
+            p.stream ? whole(std::true_type()) : whole(std::false_type());
             return hipGetLastError();
         }
         hipLaunchKernelGGL((norm_stats_kernel<T, V, W>), grid, block, join, s, a);

@@ -2,6 +2,7 @@
 #include "qrm_train.h"
 
 #include <algorithm>
+#include <cmath>
 #include <numeric>
 
 namespace qrm {
@@ -45,12 +46,12 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
         c.chunks = (int)std::min(want, std::max<int64_t>(1, d.P / (4 * rpar)));
     };
 
-    // A tile for one launch is the narrowest, down to 16 channels (8 forward), of which there are not many more than compute units: a line's tiles are numbered so
-    // that one die's cache serves them all (find_tile).  One launch is taken where a tile fits a workgroup and is over before a second launch would have
-    // begun, or where compute units are busy anyway and the map is read once.  Measured with silu and 512 channels in bf16, one launch / two, us: 1 image of 256 /
-    // 1024 / 2048 pixels 5.7 / 9.7, 7.4 / 9.7, 10.1 / 9.9; 4 images of 1024 / 2048 / 4096 7.9 / 10.2, 11.1 / 12.2, 16.4 / 16.4 (tiles of a line, 1024 pixels: 12.8); 16
-    // images 11.7 / 16.3, 18.9 / 22.5, 28.8 / 34.6 (a line 14.7, 24.1); backward, 1 image of 256 / 1024 / 2048 pixels 6.4 / 11.6, 8.7 / 11.6, 14.8 / 11.8; 4 images 9.1 / 11.7,
-    // 11.8 / 12.3, 18.7 / 15.4; 16 images of 512 / 1024 11.7 / 15.3, 18.3 / 20.2.
+    // A tile for one launch is the narrowest, down to 16 channels (8 forward), of which there are not more than compute units: a line's tiles are numbered so that one
+    // die's cache serves them all (find_tile).  One launch is taken where a tile fits a workgroup and is over before a second launch would have begun, or
+    // where compute units are busy anyway and the map is read once.  Measured with silu and 512 channels in bf16, one launch / two, us: 1 image of 256 / 1024 /
+    // 2048 pixels 5.7 / 9.7, 7.4 / 9.7, 10.1 / 9.9; 4 images of 1024 / 2048 / 4096 7.9 / 10.2, 11.1 / 12.2, 16.4 / 16.4 (tiles of a line, 1024 pixels: 12.8); 16 images
+    // 11.7 / 16.3, 18.9 / 22.5, 28.8 / 34.6 (a line 14.7, 24.1); 64 images of 1024, on other maps in turn, 24.5 / 39.0; backward, 1 image of 256 / 1024 / 2048 pixels
+    // 6.4 / 11.6, 8.7 / 11.6, 14.8 / 11.8; 4 images 9.1 / 11.7, 11.8 / 12.3, 18.7 / 15.4; 16 images of 512 / 1024 11.7 / 15.3, 18.3 / 20.2.
     const int most_threads = p.W > 2 ? 256 : backward ? kNormMaxThreads / 2 : kNormMaxThreads;
     const int least = (backward ? 16 : 8) * size;
     auto fit = [&] { // pixels and threads of a tile
@@ -61,21 +62,29 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
         p.first.threads = (int)threads;
         return threads <= most_threads && d.P <= p.pixels * (threads / cols);
     };
+    auto rounds = [&] { // of workgroups that run at once
+        const int64_t at_once = (int64_t)num_cu * std::max(1, (p.pixels == kNormFew ? 2 : 1) * kNormMaxThreads / p.first.threads); // (for their registers)
+        return (double)(d.N * p.first.tiles) / at_once;
+    };
+    auto pays = [&] {
+        const int64_t blocks = d.N * p.first.tiles, elements = d.P * p.first.ct;
+        if (!fit()) return false;
+        if (backward) return elements * size <= (blocks >= num_cu ? 65536 : 32768);
+        return blocks >= num_cu || elements <= (blocks >= num_cu / 2 ? 32768 : 16384);
+    };
     int bytes = 128;
     p.first = cut(bytes, 64);
     while (bytes / 2 >= least) {
         const NormCut half = cut(bytes / 2, 64);
-        if (d.N * half.tiles > num_cu + num_cu / 2) break;
+        if (d.N * half.tiles > num_cu) break;
         p.first = half, bytes /= 2;
     }
-    p.whole = fit();
-    while (!p.whole && !backward && bytes / 2 >= least) {
-        p.first = cut(bytes /= 2, 64);
-        p.whole = fit();
+    // (rounds have to be three quarters full: 48 images of 2048 pixels and 512 channels, one and a half rounds 55.9 us, two launches 57.3; 24 of 4096 76.0 and 56.0)
+    p.whole = pays() && (rounds() <= 1.0 || rounds() >= 0.75 * std::ceil(rounds()));
+    if (!p.whole && bytes / 2 >= least) { // a few more tiles than compute units, side by side: 20 images of 2048 pixels 25.0, two launches 26.7
+        p.first = cut(bytes / 2, 64);
+        p.whole = pays() && rounds() <= 1.0 && !(backward && d.P * p.first.ct * size > 32768);
     }
-    const int64_t blocks = d.N * p.first.tiles, elements = d.P * p.first.ct;
-    if (backward) p.whole = p.whole && elements * size <= (blocks >= num_cu ? 65536 : 32768);
-    else p.whole = p.whole && (blocks >= num_cu || elements <= (blocks >= num_cu / 2 ? 32768 : 16384));
     if (!p.whole) {
         // (few chunks in the first launch: every workgroup of the second reads its groups' parts of all of them)
         p.first = p.second = cut(128, kNormThreads);
@@ -85,8 +94,9 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
     }
     // Outputs larger than all L2s (8 x 4 MiB) are written past the caches: who reads them next finds little of them there, and what they would push out of the memory-side
     // cache is written to memory while the next launch reads.  4 images of 256 x 256 pixels, 128 channels, bf16 (64 MiB): 43.6 us without, 38.6 with;
-    // backward 72.0 and 62.4.
-    p.stream = (double)d.N * d.P * d.C * size > 32.0 * (1 << 20);
+    // backward 72.0 and 62.4; in one launch 64 images of 1024 pixels, 512 channels 37.8 and 24.5.  Parts of lines, from several workgroups, are better put together in the
+    // caches: 16 images of 4096 pixels, 512 channels in f32, half lines, 71.7 without, 85.6 with.
+    p.stream = (double)d.N * d.P * d.C * size > 32.0 * (1 << 20) && (!p.whole || p.first.ct * size >= 128);
     p.channels = backward && channels && !(p.whole && d.N == 1);
     p.bytes = (p.part_words + (p.channels ? (size_t)d.N * p.first.chunks * d.C : 0)) * sizeof(float2);
     *out = p;

@@ -1,9 +1,11 @@
 """What the fine-tuning calls refuse before anything is launched: sizes past a launch, maps written over themselves, moments of other sizes, a first
-recorded call."""
+recorded call.  And sizes at which a launch is cut in another way."""
 import ctypes as C
 
 import pytest
 import torch
+
+from test_gpu_finetune import check_backward, check_norm
 
 pytestmark = pytest.mark.gpu
 
@@ -115,3 +117,20 @@ def test_loss_counts_every_workgroup(ctx, workgroups):
     got = loss.cpu()
     assert torch.equal(got[1:], got[:2])
     assert abs(got[0].item() - want) <= 80 * 2.0 ** -24 * want
+
+
+# images, pixels, channels, groups: tiles of a part of a line, in numbers that eight dies divide or not; a few more tiles than compute units; one round of
+# workgroups, one and a bit, one and a half
+CUTS = [(1, 100, 488, 61), (3, 100, 512, 32), (5, 33, 520, 65), (13, 70, 72, 9), (16, 200, 512, 32), (17, 300, 512, 32), (20, 1030, 256, 16), (33, 40, 512, 32),
+        (48, 1025, 256, 8), (270, 9, 32, 4), (600, 17, 40, 5)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,p,c,groups", CUTS)
+def test_norm_however_it_is_cut(ctx, qrm, n, p, c, groups, dtype):
+    check_norm(ctx, qrm, n, p, c, groups, dtype, "silu", seed=n + p)
+    check_backward(ctx, qrm, n, p, c, groups, dtype, "silu", seed=n + p)
+
+
+def test_norm_past_the_caches_in_one_launch(ctx, qrm):
+    check_norm(ctx, qrm, 64, 601, 512, 32, torch.bfloat16, "silu", seed=5)
