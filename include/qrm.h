@@ -40,6 +40,9 @@
  *     last call was one of the fine-tuning calls, the host waits for the
  *     device instead: those calls leave no event behind.)
  *     qrm_release_stream hands a stream's workspace back explicitly.
+ *   - A stream on which a call has been recorded into a HIP graph keeps what the call works in: its workspace goes to no other stream, and
+ *     where a later call needs a larger one, the earlier one stays for the graph.  qrm_release_stream and qrm_destroy free it: the graph is
+ *     not to be replayed after that.  Replays and other calls on that stream share the workspace and must not overlap in time.
  */
 #ifndef QRM_H
 #define QRM_H
@@ -136,7 +139,8 @@ QRM_API qrm_status qrm_set_micro_batch(qrm_ctx *ctx, int32_t images);
 /*
  * Tells the context that `stream` will not be used with it again (e.g. before the caller destroys the
  * stream): waits for the context's last call on that stream and marks its workspace free for another
- * stream; the memory is kept for reuse.  A stream the context has never seen is a successful no-op.
+ * stream; the memory is kept for reuse.  Where a call on it has been recorded into a graph, waits for the device instead; the
+ * graph is not to be replayed any more.  A stream the context has never seen is a successful no-op.
  */
 QRM_API qrm_status qrm_release_stream(qrm_ctx *ctx, void *stream);
 
@@ -376,8 +380,7 @@ QRM_API qrm_status qrm_profile_read_chunks(qrm_ctx *ctx, int32_t max_chunks, dou
  * Fine-tuning (Section 4.2: the image decoder is taught to write the key, with a message loss on the extractor's logits and some hundred
  * AdamW steps).  The calls below are the parts of such a step that are not matrix products; they take any context, whatever it was
  * created with, unless stated.  They can be recorded into a HIP graph on a stream that has run the same calls on the context before (its
- * workspace is there then; a qrm_message_loss that would have to clear counters first is refused, QRM_E_INVALID); replays of a graph and
- * other calls that use the same stream's workspace must not overlap in time.
+ * workspace is there then; a qrm_message_loss that would have to clear counters first is refused, QRM_E_INVALID).
  * Types of tensors: */
 typedef enum { QRM_F32 = 0, QRM_BF16 = 1, QRM_F16 = 2 } qrm_type;
 typedef enum { QRM_ACT_NONE = 0, QRM_ACT_RELU = 1, QRM_ACT_SILU = 2 } qrm_act;

@@ -43,6 +43,12 @@ QRM_API qrm_status qrm_diag_chain_count(qrm_ctx *ctx, void *stream, int32_t shar
 QRM_API qrm_status qrm_diag_chain_left_over(qrm_ctx *ctx, void *stream, int32_t shared, uint32_t value);
 
 /*
+ * Where calls on `stream` work: *ws the address of its workspace (NULL: it has none, or none yet), *bytes its size, *kept how many
+ * earlier ones are kept because a call that used them has been recorded into a graph.  Host code.
+ */
+QRM_API qrm_status qrm_diag_workspace(qrm_ctx *ctx, void *stream, void **ws, int64_t *bytes, int32_t *kept);
+
+/*
  * Whether n_img tiles of h x w go through `blocks` blocks of `channels` in one launch on num_cu compute units: *fits such a launch takes
  * them, *taken it does so by the rule.  Host code, no device needed.
  */

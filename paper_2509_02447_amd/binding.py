@@ -61,7 +61,7 @@ EXPORTS = ["qrm_create", "qrm_destroy", "qrm_last_error", "qrm_set_micro_batch",
 DIAG_EXPORTS = ["qrm_diag_set_flags", "qrm_diag_matrix_rate", "qrm_diag_pair_split",
                 "qrm_diag_wide_schedule", "qrm_diag_last_lines", "qrm_diag_host_plan",
                 "qrm_diag_preprocess_strips", "qrm_diag_rs_lanes", "qrm_diag_chain_patience", "qrm_diag_chain_count",
-                "qrm_diag_chain_left_over", "qrm_diag_chain_rule"]   # include/qrm_diag.h: bench and test tooling
+                "qrm_diag_chain_left_over", "qrm_diag_chain_rule", "qrm_diag_workspace"]   # include/qrm_diag.h: bench and test tooling
 
 QRM_MAX_STREAMS = 8   # include/qrm.h
 QRM_F32, QRM_BF16, QRM_F16 = 0, 1, 2
@@ -160,6 +160,8 @@ def load_library():
     lib.qrm_diag_chain_left_over.restype = C.c_int
     lib.qrm_diag_chain_rule.argtypes = [i32] * 6 + [C.POINTER(i32)] * 2
     lib.qrm_diag_chain_rule.restype = C.c_int
+    lib.qrm_diag_workspace.argtypes = [vp, vp, C.POINTER(vp), C.POINTER(i64), C.POINTER(i32)]
+    lib.qrm_diag_workspace.restype = C.c_int
     lib.qrm_group_norm.argtypes = [vp, C.POINTER(_GroupNormDesc)] + [vp] * 7
     lib.qrm_group_norm.restype = C.c_int
     lib.qrm_group_norm_backward.argtypes = [vp, C.POINTER(_GroupNormDesc)] + [vp] * 10
@@ -349,6 +351,12 @@ class Context:
 
     def qrm_diag_chain_left_over(self, shared: bool, value: int, stream=None):
         self._check(self._lib.qrm_diag_chain_left_over(self._h, _stream_handle(stream), int(bool(shared)), int(value)))
+
+    def qrm_diag_workspace(self, stream=None):
+        """-> (address or None, bytes, earlier ones that are kept) of the workspace of a stream."""
+        ws, size, kept = C.c_void_p(), C.c_int64(), C.c_int32()
+        self._check(self._lib.qrm_diag_workspace(self._h, _stream_handle(stream), C.byref(ws), C.byref(size), C.byref(kept)))
+        return ws.value, size.value, kept.value
 
     def qrm_diag_matrix_rate(self, data: int) -> float:
         """-> TFLOP/s the matrix pipes sustain on zeros (0), a constant (1) or random operands (2)."""

@@ -368,21 +368,63 @@ WsLayout ws_layout(const qrm_ctx *c, int64_t N, int h, int w, bool want_symbols,
     return L;
 }
 
+// Whether work on s is being recorded into a graph.
+static bool recording(hipStream_t s)
+{
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &status) == hipSuccess) return status == hipStreamCaptureStatusActive;
+    (void)hipGetLastError(); // (the launches on s will say what is wrong with it)
+    return false;
+}
+
+// One workspace more, free, without memory.
+static qrm_status add_slot(qrm_ctx *c, QrmSlot **out)
+{
+    void *words = nullptr;
+    if (c->has_ext && hipMalloc(&words, kChainStateBytes) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(c, QRM_E_NOMEM, "no device memory for a workspace's chain state");
+    }
+    try {
+        c->slots.emplace_back();
+    } catch (const std::bad_alloc &) {
+        (void)hipFree(words);
+        return fail(c, QRM_E_NOMEM, "no host memory for a workspace");
+    }
+    QrmSlot &sl = c->slots.back();
+    sl.own_chain = words;
+    sl.chain.words = (uint32_t *)words;
+    sl.chain.dirty = words != nullptr; // (the first call that counts in it clears it)
+    *out = &sl;
+    return QRM_OK;
+}
+
 // Hands the caller's stream its workspace of at least `bytes` bytes.  A stream keeps its workspace from call
 // to call.  A stream not seen before takes a free one, or - when all are taken - the one whose last call lies
 // furthest back: the new stream is then made to wait (on the device) for that call to finish, so nothing is
-// overwritten while in use, whether or not the old stream still exists.
+// overwritten while in use, whether or not the old stream still exists.  Those that graphs work in are not dealt again: where
+// fewer than kSlots are left, or the wait would be recorded, there is one more.
 qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
 {
+    const bool in_graph = recording(s);
     QrmSlot *slot = nullptr;
     for (auto &sl : c->slots)
         if (sl.used && sl.stream == s) { slot = &sl; break; }
     if (!slot) {
         for (auto &sl : c->slots) // a free one, preferably one whose memory is already large enough
             if (!sl.used && (!slot || (slot->bytes < bytes && sl.bytes > slot->bytes))) slot = &sl;
-        if (!slot)
+        if (!slot) {
+            int dealt = 0;
             for (auto &sl : c->slots)
-                if (!slot || sl.last_use < slot->last_use) slot = &sl;
+                if (!sl.recorded) {
+                    ++dealt;
+                    if (!slot || sl.last_use < slot->last_use) slot = &sl;
+                }
+            if (dealt < kSlots || in_graph) {
+                qrm_status st = add_slot(c, &slot);
+                if (st != QRM_OK) return st;
+            }
+        }
         if (slot->unmarked) {
             // (its stream may be gone: there is nothing else to wait for)
             hipError_t e = hipDeviceSynchronize();
@@ -400,16 +442,24 @@ qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
         hipError_t e = hipEventCreateWithFlags(&slot->done, hipEventDisableTiming);
         if (e != hipSuccess) return hip_fail(c, e, "hipEventCreateWithFlags");
     }
+    slot->recorded |= in_graph;
     if (slot->bytes < bytes) {
-        if (slot->ws) {
+        if (slot->ws && (slot->ws_recorded || in_graph)) { // (s cannot be waited for while it is recorded)
+            try {
+                slot->kept.push_back(slot->ws);
+            } catch (const std::bad_alloc &) {
+                return fail(c, QRM_E_NOMEM, "no host memory for a workspace");
+            }
+        } else if (slot->ws) {
             // everything that used the old memory is behind `done` (calls on earlier streams) or on s itself
             hipError_t e = hipEventSynchronize(slot->done);
             if (e == hipSuccess) e = hipStreamSynchronize(s);
             if (e != hipSuccess) return hip_fail(c, e, "hipStreamSynchronize");
             (void)hipFree(slot->ws);
-            slot->ws = nullptr;
-            slot->bytes = 0;
         }
+        slot->ws = nullptr;
+        slot->bytes = 0;
+        slot->ws_recorded = false;
         hipError_t e = hipMalloc(&slot->ws, bytes);
         if (e != hipSuccess) {
             (void)hipGetLastError();
@@ -426,6 +476,7 @@ qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
             if (e != hipSuccess) return hip_fail(c, e, "hipMemsetAsync(workspace poison)");
         }
     }
+    slot->ws_recorded |= in_graph;
     *out = slot;
     return QRM_OK;
 }
@@ -454,6 +505,7 @@ qrm_status get_counters(qrm_ctx *c, hipStream_t s, QrmSlot *slot)
 // behind the last kernel of a call: whoever takes the workspace over waits for this
 qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s)
 {
+    if (slot->recorded) return QRM_OK; // (nobody takes it over; in a graph the event would be one of its nodes)
     hipError_t e = hipEventRecord(slot->done, s);
     if (e != hipSuccess) return hip_fail(c, e, "hipEventRecord");
     slot->unmarked = false; // (short calls before this one are on the same stream)
@@ -770,7 +822,7 @@ qrm_status qrm_create(const qrm_extractor_desc *ext, const qrm_rs_desc *rs, int 
         }
 
         const size_t frag_bytes = align_up(frag.size() * 2);
-        const size_t chain_at = frag_bytes + align_up(fl.size() * 4), chain_bytes = kChainStateBytes * (sizeof c->slots / sizeof c->slots[0]);
+        const size_t chain_at = frag_bytes + align_up(fl.size() * 4), chain_bytes = kChainStateBytes * kSlots;
         e = hipMalloc(&c->d_weights, chain_at + chain_bytes);
         if (e != hipSuccess) { delete c; return hip_fail(nullptr, e, "hipMalloc(weights)"); }
         e = hipMemset((uint8_t *)c->d_weights + chain_at, 0, chain_bytes); // (done before the copies behind it on the same stream are)
@@ -779,7 +831,11 @@ qrm_status qrm_create(const qrm_extractor_desc *ext, const qrm_rs_desc *rs, int 
             e = hipMemcpy((uint8_t *)c->d_weights + frag_bytes, fl.data(), fl.size() * 4, hipMemcpyHostToDevice);
         if (e != hipSuccess) { (void)hipFree(c->d_weights); delete c; return hip_fail(nullptr, e, "hipMemcpy(weights)"); }
         take_host_word(device, &c->h_lost, &c->d_lost); // (without one, an image whose items are missing has its NaN logits all the same)
-        for (QrmSlot &sl : c->slots) sl.chain.words = (uint32_t *)((uint8_t *)c->d_weights + chain_at + (&sl - c->slots) * kChainStateBytes);
+        size_t words_at = chain_at;
+        for (QrmSlot &sl : c->slots) {
+            sl.chain.words = (uint32_t *)((uint8_t *)c->d_weights + words_at);
+            words_at += kChainStateBytes;
+        }
         const bf16_t *fb = (const bf16_t *)c->d_weights;
         c->d_w_first = fb + frag_off[0];
         for (int b = 1; b < nb; ++b) c->d_w_mid.push_back(fb + frag_off[b]);
@@ -817,13 +873,15 @@ void qrm_destroy(qrm_ctx *c)
     (void)hipSetDevice(c->device);
     for (auto &sl : c->slots) {
         // the caller's stream may be gone by now: the event behind the workspace's last call is what is waited for
-        if (sl.unmarked) (void)hipDeviceSynchronize();
+        if (sl.unmarked || sl.recorded) (void)hipDeviceSynchronize();
         if (sl.done) {
             if (sl.last_use) (void)hipEventSynchronize(sl.done);
             (void)hipEventDestroy(sl.done);
         }
         if (sl.ws) (void)hipFree(sl.ws);
         if (sl.counters) (void)hipFree(sl.counters);
+        for (void *p : sl.kept) (void)hipFree(p);
+        if (sl.own_chain) (void)hipFree(sl.own_chain);
     }
     for (auto &t : c->timed) {
         (void)hipEventDestroy(t.start);
@@ -856,7 +914,13 @@ qrm_status qrm_release_stream(qrm_ctx *c, void *stream)
     if (e != hipSuccess) return hip_fail(c, e, "hipSetDevice");
     for (auto &sl : c->slots)
         if (sl.used && sl.stream == (hipStream_t)stream) {
-            if (sl.done && sl.last_use) {
+            if (sl.recorded) { // (replays may have been put on any stream)
+                e = hipDeviceSynchronize();
+                if (e != hipSuccess) return hip_fail(c, e, "hipDeviceSynchronize");
+                for (void *p : sl.kept) (void)hipFree(p);
+                sl.kept.clear();
+                sl.recorded = sl.ws_recorded = sl.unmarked = false;
+            } else if (sl.done && sl.last_use) {
                 e = hipEventSynchronize(sl.done);
                 if (e != hipSuccess) return hip_fail(c, e, "hipEventSynchronize");
             }

@@ -2,6 +2,7 @@
 // qrm_diag.hip).  Nothing here is visible outside the library.
 #pragma once
 
+#include <list>
 #include <string>
 #include <vector>
 
@@ -18,6 +19,7 @@ struct ChainMemory {
 };
 
 constexpr int kSlotCounters = 1024;
+constexpr int kSlots = QRM_MAX_STREAMS + 1;
 
 // A workspace of the context: the device memory the kernels of one caller stream work in.
 struct QrmSlot {
@@ -29,6 +31,12 @@ struct QrmSlot {
     uint32_t *counters = nullptr; // kSlotCounters, all zero between calls: how many workgroups of a launch are done (get_counters)
     hipEvent_t done = nullptr;    // recorded behind the last kernel of every call that used the workspace
     bool unmarked = false;        // .. but for those of short calls, for which recording an event would cost as much as a launch (slot_used)
+    // A call on the stream has been recorded into a graph, whose replays work in this memory when nobody here sees it: until the stream is
+    // released nothing that a graph may use is freed, and the workspace serves no other stream.
+    bool recorded = false;
+    bool ws_recorded = false;     // .. and in `ws` as it is now
+    std::vector<void *> kept;     // what `ws` was when such calls were recorded
+    void *own_chain = nullptr;    // `chain`, where it is not a part of the context's weights (add_slot)
     uint64_t last_use = 0;        // value of the context's call counter at that call
 };
 
@@ -59,7 +67,7 @@ struct qrm_ctx {
     int key_tau = 0;
     // workspaces: one per caller stream in use, plus the kernel stream of qrm_detect_host
     int micro_batch = 0; // 0 = default
-    QrmSlot slots[QRM_MAX_STREAMS + 1];
+    std::list<QrmSlot> slots = std::list<QrmSlot>(kSlots); // and one more where graphs have them and a stream would go without
     uint64_t use_clock = 0;
     int diag_flags = 0;  // QRM_DIAG_* (include/qrm_diag.h); 0 in production
     int chain_patience = -1; // looks of a wait in conv_chain_kernel, below zero the usual number (qrm_diag_chain_patience)

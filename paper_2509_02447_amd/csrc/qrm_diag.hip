@@ -100,6 +100,21 @@ qrm_status qrm_diag_chain_left_over(qrm_ctx *c, void *stream, int32_t shared, ui
     return QRM_OK;
 }
 
+qrm_status qrm_diag_workspace(qrm_ctx *c, void *stream, void **ws, int64_t *bytes, int32_t *kept)
+{
+    if (!c) return QRM_E_INVALID;
+    if (!ws || !bytes || !kept) return fail(c, QRM_E_INVALID, "ws / bytes / kept is NULL");
+    *ws = nullptr;
+    *bytes = *kept = 0;
+    for (QrmSlot &sl : c->slots)
+        if (sl.used && sl.stream == (hipStream_t)stream) {
+            *ws = sl.ws;
+            *bytes = (int64_t)sl.bytes;
+            *kept = (int32_t)sl.kept.size();
+        }
+    return QRM_OK;
+}
+
 qrm_status qrm_diag_chain_rule(int32_t channels, int32_t blocks, int32_t n_img, int32_t h, int32_t w, int32_t num_cu, int32_t *fits,
                                int32_t *taken)
 {
