@@ -36,9 +36,10 @@
  *     call.  When more streams than that have been used, a stream not seen
  *     before takes over the workspace whose last call lies furthest back; its
  *     work is ordered (on the device) behind that call, so results stay
- *     correct, and streams that no longer exist cost nothing.  (Where that
- *     last call was one of the fine-tuning calls, the host waits for the
- *     device instead: those calls leave no event behind.)
+ *     correct, and streams that no longer exist cost nothing.  (A context's
+ *     first stream, if it has last made a fine-tuning call and not called
+ *     again since another stream did, keeps its workspace until it is released:
+ *     with one stream those calls leave no event behind.)
  *     qrm_release_stream hands a stream's workspace back explicitly.
  *   - A stream on which a call has been recorded into a HIP graph keeps what the call works in: its workspace goes to no other stream, and
  *     where a later call needs a larger one, the earlier one stays for the graph.  qrm_release_stream and qrm_destroy free it: the graph is

@@ -402,8 +402,8 @@ static qrm_status add_slot(qrm_ctx *c, QrmSlot **out)
 // Hands the caller's stream its workspace of at least `bytes` bytes.  A stream keeps its workspace from call
 // to call.  A stream not seen before takes a free one, or - when all are taken - the one whose last call lies
 // furthest back: the new stream is then made to wait (on the device) for that call to finish, so nothing is
-// overwritten while in use, whether or not the old stream still exists.  Those that graphs work in are not dealt again: where
-// fewer than kSlots are left, or the wait would be recorded, there is one more.
+// overwritten while in use, whether or not the old stream still exists.  Those that graphs work in are not dealt again, nor is one without an
+// event behind its last call: where fewer than kSlots are left, or the wait would be recorded, there is one more.
 qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
 {
     const bool in_graph = recording(s);
@@ -411,12 +411,13 @@ qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
     for (auto &sl : c->slots)
         if (sl.used && sl.stream == s) { slot = &sl; break; }
     if (!slot) {
+        for (auto &sl : c->slots) c->several |= sl.used;
         for (auto &sl : c->slots) // a free one, preferably one whose memory is already large enough
             if (!sl.used && (!slot || (slot->bytes < bytes && sl.bytes > slot->bytes))) slot = &sl;
         if (!slot) {
             int dealt = 0;
             for (auto &sl : c->slots)
-                if (!sl.recorded) {
+                if (!sl.recorded && !sl.unmarked) {
                     ++dealt;
                     if (!slot || sl.last_use < slot->last_use) slot = &sl;
                 }
@@ -425,12 +426,7 @@ qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out)
                 if (st != QRM_OK) return st;
             }
         }
-        if (slot->unmarked) {
-            // (its stream may be gone: there is nothing else to wait for)
-            hipError_t e = hipDeviceSynchronize();
-            if (e != hipSuccess) return hip_fail(c, e, "hipDeviceSynchronize(workspace hand-over)");
-            slot->unmarked = false;
-        } else if (slot->done && slot->last_use) {
+        if (slot->done && slot->last_use) {
             hipError_t e = hipStreamWaitEvent(s, slot->done, 0);
             if (e != hipSuccess) return hip_fail(c, e, "hipStreamWaitEvent(workspace hand-over)");
         }
@@ -503,12 +499,16 @@ qrm_status get_counters(qrm_ctx *c, hipStream_t s, QrmSlot *slot)
 }
 
 // behind the last kernel of a call: whoever takes the workspace over waits for this
-qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s)
+qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s, bool brief)
 {
     if (slot->recorded) return QRM_OK; // (nobody takes it over; in a graph the event would be one of its nodes)
+    if (brief && !c->several) {
+        slot->unmarked = true;
+        return QRM_OK;
+    }
     hipError_t e = hipEventRecord(slot->done, s);
     if (e != hipSuccess) return hip_fail(c, e, "hipEventRecord");
-    slot->unmarked = false; // (short calls before this one are on the same stream)
+    slot->unmarked = false; // (the calls before this one are on the same stream)
     return QRM_OK;
 }
 
@@ -914,7 +914,7 @@ qrm_status qrm_release_stream(qrm_ctx *c, void *stream)
     if (e != hipSuccess) return hip_fail(c, e, "hipSetDevice");
     for (auto &sl : c->slots)
         if (sl.used && sl.stream == (hipStream_t)stream) {
-            if (sl.recorded) { // (replays may have been put on any stream)
+            if (sl.recorded || sl.unmarked) { // (replays may have been put on any stream; the stream itself may be gone)
                 e = hipDeviceSynchronize();
                 if (e != hipSuccess) return hip_fail(c, e, "hipDeviceSynchronize");
                 for (void *p : sl.kept) (void)hipFree(p);
@@ -923,11 +923,6 @@ qrm_status qrm_release_stream(qrm_ctx *c, void *stream)
             } else if (sl.done && sl.last_use) {
                 e = hipEventSynchronize(sl.done);
                 if (e != hipSuccess) return hip_fail(c, e, "hipEventSynchronize");
-            }
-            if (sl.unmarked) {
-                e = hipStreamSynchronize(sl.stream);
-                if (e != hipSuccess) return hip_fail(c, e, "hipStreamSynchronize");
-                sl.unmarked = false;
             }
             sl.used = false;
             sl.stream = nullptr;

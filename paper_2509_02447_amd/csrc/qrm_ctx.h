@@ -30,7 +30,7 @@ struct QrmSlot {
     ChainMemory chain;            // its own, for as long as the context lives
     uint32_t *counters = nullptr; // kSlotCounters, all zero between calls: how many workgroups of a launch are done (get_counters)
     hipEvent_t done = nullptr;    // recorded behind the last kernel of every call that used the workspace
-    bool unmarked = false;        // .. but for those of short calls, for which recording an event would cost as much as a launch (slot_used)
+    bool unmarked = false;        // .. but for short calls that came before a second stream did (slot_done): nobody can tell when it is free
     // A call on the stream has been recorded into a graph, whose replays work in this memory when nobody here sees it: until the stream is
     // released nothing that a graph may use is freed, and the workspace serves no other stream.
     bool recorded = false;
@@ -68,6 +68,7 @@ struct qrm_ctx {
     // workspaces: one per caller stream in use, plus the kernel stream of qrm_detect_host
     int micro_batch = 0; // 0 = default
     std::list<QrmSlot> slots = std::list<QrmSlot>(kSlots); // and one more where graphs have them and a stream would go without
+    bool several = false; // streams have had a workspace at the same time
     uint64_t use_clock = 0;
     int diag_flags = 0;  // QRM_DIAG_* (include/qrm_diag.h); 0 in production
     int chain_patience = -1; // looks of a wait in conv_chain_kernel, below zero the usual number (qrm_diag_chain_patience)
@@ -122,13 +123,13 @@ qrm_status run_extractor(qrm_ctx *c, uint8_t *base, ChainMemory &chain_memory, c
                          float *d_logits, uint8_t *d_bits, uint8_t *d_symbols, int m_sym, const WordArgs &word, float *d_act,
                          bool may_time, hipStream_t s);
 
-// The workspace of at least `bytes` bytes of the caller's stream, and what goes behind the last kernel that uses it.
+// The workspace of at least `bytes` bytes of the caller's stream, and what goes behind the last kernel that uses it, also where a launch has
+// failed.  brief: a call of a few microseconds, for which an event is 3 more (a norm of 4 images of 4096 pixels, backward, 20.8 us without, 23.8
+// with): as long as the context has seen one stream alone, nobody can take the workspace over and there is none.
 qrm_status get_slot(qrm_ctx *c, hipStream_t s, size_t bytes, QrmSlot **out);
-qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s);
+qrm_status slot_done(qrm_ctx *c, QrmSlot *slot, hipStream_t s, bool brief = false);
 // The counters of a slot, allocated at their first use.
 qrm_status get_counters(qrm_ctx *c, hipStream_t s, QrmSlot *slot);
-// .. of a short call: nothing is recorded, and who takes the workspace over, frees or gives it back waits for the device or the stream instead.
-inline void slot_used(QrmSlot *slot) { slot->unmarked = true; }
 
 // QRM_E_DEVICE, once, if an earlier call's launch has lost images.
 qrm_status report_lost(qrm_ctx *c);

@@ -103,9 +103,9 @@ qrm_status qrm_group_norm(qrm_ctx *c, const qrm_group_norm_desc *desc, const voi
     call.x = d_x; call.y = d_y; call.gamma = d_gamma; call.beta = d_beta; call.mean = d_mean; call.rstd = d_rstd;
     QrmSlot *slot = nullptr;
     if (p.bytes && (st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
-    if (slot) slot_used(slot); // (also where only the first of two launches comes off)
     hipError_t e = launch_norm_forward(call, p, slot ? slot->ws : nullptr, (hipStream_t)stream);
-    return e == hipSuccess ? QRM_OK : hip_fail(c, e, "group_norm launch");
+    if (slot) st = slot_done(c, slot, (hipStream_t)stream, true);
+    return e == hipSuccess ? st : hip_fail(c, e, "group_norm launch");
 }
 
 qrm_status qrm_group_norm_backward(qrm_ctx *c, const qrm_group_norm_desc *desc, const void *d_x, const void *d_dy, const float *d_gamma,
@@ -136,9 +136,9 @@ qrm_status qrm_group_norm_backward(qrm_ctx *c, const qrm_group_norm_desc *desc, 
     if ((st = plan(c, call.d, align, true, d_dgamma || d_dbeta, &p)) != QRM_OK || (st = start(c)) != QRM_OK) return st;
     QrmSlot *slot = nullptr;
     if (p.bytes && (st = get_slot(c, (hipStream_t)stream, p.bytes, &slot)) != QRM_OK) return st;
-    if (slot) slot_used(slot);
     hipError_t e = launch_norm_backward(call, p, slot ? slot->ws : nullptr, (hipStream_t)stream);
-    return e == hipSuccess ? QRM_OK : hip_fail(c, e, "group_norm_backward launch");
+    if (slot) st = slot_done(c, slot, (hipStream_t)stream, true);
+    return e == hipSuccess ? st : hip_fail(c, e, "group_norm_backward launch");
 }
 
 qrm_status qrm_adamw_create(qrm_ctx *c, const qrm_adamw_desc *desc, const qrm_adamw_tensor *h_tensors, qrm_adamw **out)
@@ -299,9 +299,9 @@ qrm_status qrm_message_loss(qrm_ctx *c, const float *d_logits, const uint8_t *d_
     if (blocks > 1 && ((st = get_slot(c, (hipStream_t)stream, (size_t)blocks * sizeof(double), &slot)) != QRM_OK ||
                        (st = get_counters(c, (hipStream_t)stream, slot)) != QRM_OK))
         return st;
-    if (slot) slot_used(slot);
     hipError_t e = launch_message_loss(call, slot ? (double *)slot->ws : nullptr, slot ? slot->counters : nullptr, (hipStream_t)stream);
-    return e == hipSuccess ? QRM_OK : hip_fail(c, e, "message_loss launch");
+    if (slot) st = slot_done(c, slot, (hipStream_t)stream, true);
+    return e == hipSuccess ? st : hip_fail(c, e, "message_loss launch");
 }
 
 } // extern "C"

@@ -186,3 +186,68 @@ def test_a_recorded_detection_keeps_its_workspace(qrm, chain):
         torch.cuda.synchronize()
     ctx.qrm_release_stream(streams[0])
     ctx.close()
+
+
+def test_a_workspace_is_taken_over_without_the_host_waiting(qrm):
+    """Fine-tuning and detection calls on more streams than workspaces, beside a stream that is busy for long: all of them return before it is done."""
+    import synth
+    cfg = synth.CONFIGS["C1"]
+    ctx = qrm.Context(weights=synth.config_weights(cfg), rs=dict(m=cfg.m, prim_poly=cfg.prim_poly, n=cfg.n, k=cfg.k, fcr=cfg.fcr))
+    n = 16
+    d_img, d_off = torch.from_numpy(synth.images(cfg, 0, n)).cuda(), torch.from_numpy(synth.offsets(cfg, 0, n)).cuda()
+    logits, msg, nerr = torch.empty((n, cfg.n_bits), device="cuda"), torch.empty((n, cfg.k), dtype=torch.uint8, device="cuda"), torch.empty(n, dtype=torch.int8, device="cuda")
+    x = torch.randn((2, 9000, 64), generator=torch.Generator().manual_seed(1)).cuda()
+    y, desc = torch.empty_like(x), qrm.group_norm_desc(2, 9000, 64, GROUPS, torch.float32)
+
+    def detect(stream):
+        ctx.qrm_detect(d_img, n, cfg.H, cfg.W, d_off, cfg.tile, logits, None, msg, None, nerr, stream=stream)
+
+    def norm(stream):
+        ctx.qrm_group_norm(desc, x, None, None, y, stream=stream)
+
+    streams = [torch.cuda.Stream() for _ in range(3 * qrm.QRM_MAX_STREAMS)]
+    a = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    b = torch.empty_like(a)
+    norm(streams[0])                                         # (before there is a second stream)
+    for s in streams[:qrm.QRM_MAX_STREAMS + 4]:               # all workspaces are there, and large enough
+        detect(s), norm(s)
+    busy, done = torch.cuda.Stream(), torch.cuda.Event()
+    with torch.cuda.stream(busy):
+        torch.matmul(a, a, out=b)
+        torch.cuda.synchronize()
+        for _ in range(200):
+            torch.matmul(a, a, out=b)
+        done.record()
+    for s in streams[qrm.QRM_MAX_STREAMS + 4:]:
+        norm(s), detect(s), norm(s)
+    assert not done.query()
+    torch.cuda.synchronize()
+    want = torch.nn.functional.group_norm(x.double().transpose(1, 2), GROUPS, eps=1e-6).transpose(1, 2)
+    assert float((y - want).abs().max()) <= 1e-5             # (values of up to 5, a few roundings of 2^-22)
+    ctx.close()
+
+
+def test_streams_that_are_gone_are_released(qrm, ctx):
+    """A stream that is destroyed before it is handed back: alone on its context, and beside another one."""
+    import ctypes
+    hip = ctypes.CDLL("libamdhip64.so")
+    step = Step(qrm, ctx, 40)
+    step.expect()
+    for beside in (False, True):
+        own = qrm.Context(rs=CODE)
+        step.ctx = own
+        handle = ctypes.c_void_p()
+        assert hip.hipStreamCreateWithFlags(ctypes.byref(handle), 1) == 0
+        if beside:
+            step()
+            torch.cuda.synchronize()
+        with torch.cuda.stream(torch.cuda.ExternalStream(handle.value)):
+            step()
+        step.check()
+        assert hip.hipStreamDestroy(handle) == 0
+        assert own.qrm_diag_workspace(handle.value)[0]
+        own.qrm_release_stream(handle.value)
+        assert own.qrm_diag_workspace(handle.value) == (None, 0, 0)
+        step()
+        step.check()
+        own.close()
