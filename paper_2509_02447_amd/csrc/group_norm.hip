@@ -40,10 +40,10 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
         c.chunks = 1;
         return c;
     };
-    auto deal = [&](NormCut &c, int per_cu) { // so many workgroups to a compute unit, if that leaves each four pixels a thread
+    auto deal = [&](NormCut &c, int per_cu, int most) { // so many workgroups to a compute unit, if that leaves each four pixels a thread, and up to `most`
         const int rpar = c.threads / (c.ct / p.V);
         const int64_t want = std::max<int64_t>(1, (int64_t)per_cu * num_cu / std::max<int64_t>(1, d.N * c.tiles));
-        c.chunks = (int)std::min(want, std::max<int64_t>(1, d.P / (4 * rpar)));
+        c.chunks = (int)std::max(std::min(want, std::max<int64_t>(1, d.P / (4 * rpar))), (d.P - 1) / ((int64_t)most * rpar) + 1);
     };
 
     // A tile for one launch is the narrowest, down to 16 channels (8 forward), of which there are not more than compute units: a line's tiles are numbered so that one
@@ -88,8 +88,8 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
     if (!p.whole) {
         // (few chunks in the first launch: every workgroup of the second reads its groups' parts of all of them)
         p.first = p.second = cut(128, kNormThreads);
-        deal(p.first, 2);
-        deal(p.second, backward ? 2 : 4);
+        deal(p.first, 2, kNormRow);
+        deal(p.second, backward ? 2 : 4, INT32_MAX);
         p.part_words = (size_t)d.N * d.groups * p.first.chunks;
     }
     // Outputs larger than all L2s (8 x 4 MiB) are written past the caches: who reads them next finds little of them there, and what they would push out of the memory-side
