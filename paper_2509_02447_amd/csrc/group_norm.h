@@ -662,7 +662,9 @@ template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__
 }
 
 // Two launches, the first: sums of dz and dz h over the chunk, channel by channel and weighted with gamma group by group.  134 MB in 29.7 us, 4.5
-// TB/s, and 17 us of arithmetic, not all of it beside the loads.
+// TB/s, and 17 us of arithmetic, not all of it beside the loads.  A thread adds runs of kRun pixels, then their sums, of which kNormRow pixels leave 43: with
+// thousands of equal numbers one after the other, roundings that all go one way would grow to a thousand units in the last place.
+constexpr int kRun = 48;
 template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxThreads) void norm_grad_sums_kernel(NormArgs a)
 {
     constexpr int R = 3;
@@ -678,6 +680,7 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
         fetch<T, V, R, false>(q, ys, 0, pixels, dy);
     }
     const Slopes<V, W, ACT> c(a, t);
+    float2 *runs = lds + threadIdx.x * V; // the thread's sums of the runs so far
     float b[V], g[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) b[v] = g[v] = 0.f;
@@ -698,6 +701,13 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
             }
 #pragma unroll
         for (int i = 0; i < R; ++i) x[i] = next_x[i], dy[i] = next_dy[i];
+        if ((at / R + 1) % (kRun / R) == 0 || at + R >= pixels) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (at >= kRun) b[v] += runs[v].x, g[v] += runs[v].y;
+                if (at + R < pixels) runs[v] = make_float2(b[v], g[v]), b[v] = g[v] = 0.f;
+            }
+        }
     }
     sum_chunk(a, t, c, b, g, lds, [&](int ch, float sb, float sg) {
         if (a.chan) a.chan[((size_t)t.n * a.parts + t.s) * a.C + t.c0 + ch] = make_float2(sb, sg);

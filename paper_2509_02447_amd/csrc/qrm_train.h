@@ -109,7 +109,7 @@ constexpr int kNormThreads = 256, kNormMaxThreads = 1024;
 // Pixels a thread holds in one launch: as many as the registers take, or few.
 constexpr int norm_many(bool backward, int W) { return backward ? (W <= 2 ? 12 : 8) : W <= 2 ? 16 : 8; }
 constexpr int kNormFew = 4;
-// .. and walks down in the first of two launches: what it adds up in 32 bits stays short.
+// .. and walks down in the first of two launches: what it adds up in 32 bits stays short (norm_stats_kernel, norm_grad_sums_kernel).
 constexpr int kNormRow = 2048;
 
 // How a launch cuts a map: tiles of `ct` channels (whole groups, the last one narrower), of which a workgroup takes a chunk of one image's pixels.

@@ -1,9 +1,13 @@
 """Group norms of so many images that a thread walks down thousands of pixels: what it adds up stays within the bounds that short sums have.
 
-The inputs are those whose roundings all go one way: values whose squares are the same.  u = 2^-24."""
+The inputs are those whose roundings all go one way: a gradient that is the same at every pixel, values whose squares are.  u = 2^-24.  A thread adds 48
+pixels, the sums of up to 43 such runs, a few rows' sums; those are added in 64 bits: within 128 u of the sum of the magnitudes (equal numbers added one after
+the other in 32 bits are off by 240 u after 1024 of them and by 1000 u after 4096)."""
 import numpy as np
 import pytest
 import torch
+
+from oracle import finetune as ft
 
 pytestmark = pytest.mark.gpu
 
@@ -26,6 +30,32 @@ def ctx(qrm):
 
 def maps(pixels, channels, pitch):
     return torch.empty((IMAGES, pixels, pitch), device="cuda")[:, :, :channels]
+
+
+# channels, their distance, groups, pixels: single channels, four at once; 4096 pixels a thread
+@pytest.mark.parametrize("c,pitch,groups,p", [(31, 31, 31, 32768), (32, 32, 4, 131072)])
+def test_gradients_that_are_the_same_everywhere(ctx, qrm, c, pitch, groups, p):
+    x, dy = maps(p, c, pitch), maps(p, c, pitch)
+    x.normal_(generator=torch.Generator(device="cuda").manual_seed(c))
+    dy.fill_(0.1)
+    gradient = float(dy[0, 0, 0])
+    rows = x.view(IMAGES, p, groups, -1)
+    mean = torch.stack([r.double().mean(dim=(0, 2)) for r in rows]).float()
+    rstd = torch.ones_like(mean)
+    dgamma, dbeta = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    first = x[0].double().cpu().numpy()[None]
+    d = qrm.group_norm_desc(IMAGES, p, c, groups, torch.float32, "none", 1e-6, pitch, p * pitch, pitch, p * pitch)
+    ctx.qrm_group_norm_backward(d, x, dy, None, None, mean, rstd, dy, dgamma, dbeta)
+    want = IMAGES * p * gradient
+    assert (np.abs(dbeta.double().cpu().numpy() - want) <= 128 * U * want).all()
+    # dx of the first image: gradient, its mean and what h takes of it, each mean within 128 u of its magnitudes; a dozen roundings
+    m = mean[:1].double().cpu().numpy()
+    rdx = ft.group_norm_backward(first, np.full_like(first, gradient), None, None, m, np.ones_like(m), groups, "none")[0]
+    h = np.abs(first - np.repeat(m, c // groups, 1)[:, None])
+    share = np.repeat(h.reshape(1, p, groups, -1).mean(axis=(1, 3)), c // groups, 1)[:, None]
+    tol = 140 * U * gradient * (2 + h * share)
+    err = np.abs(dy[:1].double().cpu().numpy() - rdx)
+    assert (err <= tol).all(), f"off by {(err / tol).max()} of what is allowed"
 
 
 def test_values_whose_squares_are_the_same_everywhere(ctx, qrm):
