@@ -215,18 +215,69 @@ def _dptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _dptr_map(t) -> Optional[int]:
-    """Device pointer of a map [..., C] whose pixels may lie further apart than C elements (or None)."""
+class _Kinds:
+    """The torch dtypes that calls take, known once a caller has torch."""
+    _known = None
+
+    def __init__(self):
+        import torch
+        self.f32, self.i32, self.byte = (torch.float32,), (torch.int32,), (torch.uint8, torch.int8, torch.bool)
+        self.codes = {torch.float32: QRM_F32, torch.bfloat16: QRM_BF16, torch.float16: QRM_F16}
+
+
+def _kinds() -> _Kinds:
+    if _Kinds._known is None:
+        _Kinds._known = _Kinds()
+    return _Kinds._known
+
+
+def _dptr_of(t, kinds, n: int) -> Optional[int]:
+    """Device pointer of a contiguous tensor of one of the dtypes `kinds` and at least n elements (or None)."""
     if t is None:
         return None
-    assert t.is_cuda and (t.shape[-1] == 1 or t.stride(-1) == 1), "channels must lie side by side, on the GPU"
+    assert t.dtype in kinds and t.numel() >= n, "a tensor has another type than the call takes, or too few elements"
+    assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous and on the GPU"
+    return t.data_ptr()
+
+
+def _lies(t, N: int, P: int, C: int, pixel: int, image: int) -> bool:
+    """Whether channel c of pixel p of image i of a map [..,C] lies i * image + p * pixel + c elements from its first one.  The tensor's
+    channels may be more than C and its images more than N; pixels may have several dimensions."""
+    shape, stride = t.shape, t.stride()
+    if stride == (image, pixel, 1) and shape == (N, P, C):
+        return True
+    if N < 1 or P < 1 or C < 1:                              # no images, or refused
+        return True
+    if pixel == C and (image == P * C or N == 1) and t.numel() == N * P * C and t.is_contiguous():
+        return True
+    if len(shape) < 2:                                       # a buffer
+        return t.is_contiguous() and t.numel() >= (N - 1) * image + (P - 1) * pixel + C
+    if shape[-1] < C or (C > 1 and stride[-1] != 1):
+        return False
+    inside, left = 1, N * P                                  # pixels of the dimensions so far
+    for k in range(len(shape) - 2, -1, -1):
+        size = min(shape[k], left // inside) if k == 0 else shape[k]
+        if size > 1:
+            whole = inside % P == 0                          # of images; else of pixels, which end with the image unless images follow as pixels do
+            if stride[k] != (image * (inside // P) if whole else pixel * inside) or not (whole or P % (inside * size) == 0 or image == P * pixel or N <= 1):
+                return False
+        inside *= size
+    return inside == left
+
+
+def _dptr_map(t, codes, code: int, N: int, P: int, C: int, pixel: int, image: int) -> Optional[int]:
+    """Device pointer of a map that lies as its descriptor says, strides in elements, 0 = dense (or None)."""
+    if t is None:
+        return None
+    pixel = pixel or C
+    assert t.is_cuda, "device tensors must be on the GPU"
+    assert codes.get(t.dtype, -1) == code and _lies(t, N, P, C, pixel, image or P * pixel), "a map has another type, size or strides than its descriptor"
     return t.data_ptr()
 
 
 def type_code(dtype) -> int:
     """qrm_type of a torch dtype."""
-    import torch
-    return {torch.float32: QRM_F32, torch.bfloat16: QRM_BF16, torch.float16: QRM_F16}[dtype]
+    return _kinds().codes[dtype]
 
 
 def group_norm_desc(N: int, P: int, C: int, groups: int, dtype, act: str = "none", eps: float = 1e-6, x_pixel: int = 0,
@@ -309,7 +360,7 @@ class Context:
             pass
 
     def _check(self, st: int):
-        if st != QRM_OK:
+        if st:                                               # (QRM_OK is 0)
             raise QrmError(st, self._lib.qrm_last_error(self._h).decode())
 
     def last_error(self) -> str:
@@ -432,24 +483,33 @@ class Context:
                                                 _stream_handle(stream)))
 
     def qrm_group_norm(self, desc, d_x, d_gamma, d_beta, d_y, d_mean=None, d_rstd=None, stream=None):
-        self._check(self._lib.qrm_group_norm(self._h, C.byref(desc), _dptr_map(d_x), _dptr(d_gamma), _dptr(d_beta), _dptr_map(d_y),
-                                             _dptr(d_mean), _dptr(d_rstd), _stream_handle(stream)))
+        k, N, C_ = _kinds(), desc.N, desc.C
+        f32, stats, lie = k.f32, N * desc.groups, (k.codes, desc.type, N, desc.P, C_)
+        self._check(self._lib.qrm_group_norm(self._h, C.byref(desc), _dptr_map(d_x, *lie, desc.x_pixel, desc.x_image), _dptr_of(d_gamma, f32, C_),
+                                             _dptr_of(d_beta, f32, C_), _dptr_map(d_y, *lie, desc.y_pixel, desc.y_image), _dptr_of(d_mean, f32, stats),
+                                             _dptr_of(d_rstd, f32, stats), _stream_handle(stream)))
 
     def qrm_group_norm_backward(self, desc, d_x, d_dy, d_gamma, d_beta, d_mean, d_rstd, d_dx, d_dgamma=None, d_dbeta=None,
                                 stream=None):
-        self._check(self._lib.qrm_group_norm_backward(self._h, C.byref(desc), _dptr_map(d_x), _dptr_map(d_dy), _dptr(d_gamma),
-                                                      _dptr(d_beta), _dptr(d_mean), _dptr(d_rstd), _dptr_map(d_dx),
-                                                      _dptr(d_dgamma), _dptr(d_dbeta), _stream_handle(stream)))
+        k, N, C_ = _kinds(), desc.N, desc.C
+        f32, stats, lie, x_pixel, x_image = k.f32, N * desc.groups, (k.codes, desc.type, N, desc.P, C_), desc.x_pixel, desc.x_image
+        self._check(self._lib.qrm_group_norm_backward(self._h, C.byref(desc), _dptr_map(d_x, *lie, x_pixel, x_image),
+                                                      _dptr_map(d_dy, *lie, desc.y_pixel, desc.y_image), _dptr_of(d_gamma, f32, C_),
+                                                      _dptr_of(d_beta, f32, C_), _dptr_of(d_mean, f32, stats), _dptr_of(d_rstd, f32, stats),
+                                                      _dptr_map(d_dx, *lie, x_pixel, x_image), _dptr_of(d_dgamma, f32, C_),
+                                                      _dptr_of(d_dbeta, f32, C_), _stream_handle(stream)))
 
     def qrm_unpack_moment(self, moment: int, d_codes, d_scales, n, d_out, stream=None):
-        self._check(self._lib.qrm_unpack_moment(self._h, int(moment), _dptr(d_codes), _dptr(d_scales), int(n), type_code(d_out.dtype),
-                                                _dptr(d_out), _stream_handle(stream)))
+        n, k = int(n), _kinds()
+        self._check(self._lib.qrm_unpack_moment(self._h, int(moment), _dptr_of(d_codes, k.byte, n), _dptr_of(d_scales, k.f32, -(-n // QRM_MOMENT_BLOCK)), n,
+                                                type_code(d_out.dtype), _dptr_of(d_out, k.codes, n), _stream_handle(stream)))
 
     def qrm_message_loss(self, d_logits, d_target, target_rows, N, n_bits, rs_weight, d_loss, d_grad=None, d_bit_errors=None,
                          d_symbol_errors=None, stream=None):
-        self._check(self._lib.qrm_message_loss(self._h, _dptr(d_logits), _dptr(d_target), int(target_rows), int(N), int(n_bits),
-                                               float(rs_weight), _dptr(d_loss), _dptr(d_grad), _dptr(d_bit_errors),
-                                               _dptr(d_symbol_errors), _stream_handle(stream)))
+        N, n_bits, target_rows, k = int(N), int(n_bits), int(target_rows), _kinds()
+        self._check(self._lib.qrm_message_loss(self._h, _dptr_of(d_logits, k.f32, N * n_bits), _dptr_of(d_target, k.byte, target_rows * n_bits), target_rows,
+                                               N, n_bits, float(rs_weight), _dptr_of(d_loss, k.f32, 1), _dptr_of(d_grad, k.f32, N * n_bits),
+                                               _dptr_of(d_bit_errors, k.i32, N), _dptr_of(d_symbol_errors, k.i32, N), _stream_handle(stream)))
 
 
 class AdamW:
@@ -504,7 +564,7 @@ class AdamW:
             "gradients must have the plan's type and sizes, be contiguous and on the GPU"
         ptrs = self._array(*[None if g is None else g.data_ptr() for g in grads])
         self._ctx._check(self._lib.qrm_adamw_step(self._ctx._h, self._h, ptrs, int(step), float(lr), float(beta1), float(beta2),
-                                                  float(eps), _dptr(d_grad_scale), _stream_handle(stream)))
+                                                  float(eps), _dptr_of(d_grad_scale, _kinds().f32, 1), _stream_handle(stream)))
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h:
