@@ -519,7 +519,7 @@ class AdamW:
 
     def __init__(self, ctx: Context, tensors, grad_type):
         self._h = C.c_void_p()
-        self._ctx, self._keep = ctx, list(tensors)
+        self._ctx, self._keep = ctx, [dict(t) for t in tensors]
         self._lib = ctx._lib
         n = len(self._keep)
         rows = (_AdamwTensor * max(1, n))()

@@ -1,4 +1,7 @@
 """What the binding of the fine-tuning calls refuses before the library sees it: the C calls get addresses alone."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -93,3 +96,22 @@ def test_moments_and_scales_have_the_right_types(ctx, qrm):
         with pytest.raises(AssertionError):
             opt.qrm_adamw_step([zeros(9)], 1, 0.1, d_grad_scale=scale)
     torch.cuda.synchronize()
+
+
+def test_a_plan_keeps_its_tensors_whatever_becomes_of_the_callers_rows(ctx, qrm):
+    """The plan holds addresses: the tensors live as long as it does, also when the caller's dicts are changed or gone."""
+    n = 300
+    rows = [dict(param=zeros(n), m=zeros(n, dtype=torch.int8), v=zeros(n, dtype=torch.uint8), m_scale=zeros(2), v_scale=zeros(2), copy=zeros(n, dtype=torch.bfloat16)),
+            dict(param=zeros(n), m=zeros(n, dtype=torch.int8), v=zeros(n, dtype=torch.uint8), m_scale=zeros(2), v_scale=zeros(2))]
+    alive = [weakref.ref(t) for row in rows for t in row.values()]
+    opt = qrm.AdamW(ctx, rows, torch.float32)
+    rows[0]["m"] = rows[0]["copy"] = None
+    rows[0].pop("v_scale")
+    rows[1].clear()
+    del rows
+    gc.collect()
+    assert all(r() is not None for r in alive)
+    opt.close()
+    del opt
+    gc.collect()
+    assert all(r() is None for r in alive)
