@@ -390,7 +390,8 @@ typedef enum { QRM_ACT_NONE = 0, QRM_ACT_RELU = 1, QRM_ACT_SILU = 2 } qrm_act;
  * Group norm with an activation, channels last.  x [N,P,C]: N images of P pixels of C channels; group g is the C / groups channels
  * from g * C / groups on.  Over the M = P * C / groups values of a group in one image
  *   mean = sum x / M,  rstd = 1 / sqrt(sum (x - mean)^2 / M + eps),  z = gamma[c] (x - mean) rstd + beta[c],  y = act(z)
- * with act z, max(z, 0) or z / (1 + exp(-z)); sums and all that follows in 32 bits, y rounded once to its type.
+ * with act z, max(z, 0) or z / (1 + exp(-z)); sums and all that follows in 32 bits, y rounded once to its type.  A ReLU's z is rounded
+ * operation by operation, forward and backward alike: its slope is one where max(z, 0) is above zero, and nowhere else.
  * Neighbouring channels lie side by side; pixels and images may lie further apart than C and P * C (the map is a part of a wider
  * buffer): strides in elements, 0 = dense.  y has strides of its own, dy those of y, dx those of x.
  * d_gamma, d_beta f32 [C] or NULL (ones, zeros); d_mean, d_rstd f32 [N,groups], what the backward pass needs, or NULL both.

@@ -298,17 +298,23 @@ __device__ __forceinline__ void keep_stats(const NormArgs &a, const Tile &t, int
 
 // ACT: a qrm_act, or kAnyAct: the call's, looked up value by value (narrow pieces).
 constexpr int kAnyAct = -1;
-template <int ACT> __device__ __forceinline__ float activate(float z, int act)
+template <int ACT> __device__ __forceinline__ float activate(float z)
 {
-    if (ACT == kAnyAct) return act == QRM_ACT_SILU ? activate<QRM_ACT_SILU>(z, 0) : act == QRM_ACT_RELU ? activate<QRM_ACT_RELU>(z, 0) : z;
     if (ACT == QRM_ACT_RELU) return z < 0.f ? 0.f : z; // (a NaN stays one)
     if (ACT == QRM_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); // both within 1 ulp
     return z;
 }
 
+// A ReLU's argument, rounded product by product, as the definition is written, forward and backward alike: where y is above zero its slope is one.
+__device__ __forceinline__ float relu_z(float d, float rstd, float gamma, float beta)
+{
+#pragma clang fp contract(off)
+    return (d * rstd) * gamma + beta;
+}
+
 // act(gamma (x - mean) rstd + beta) of one thread's channels.  gamma and beta are read before anything is waited for.
 template <int V, int W> struct Affine {
-    float mean[W], scale[V], bias[V];
+    float mean[W], rstd[W], gamma[V], scale[V], bias[V]; // scale: gamma rstd
     int group[W];
     __device__ __forceinline__ Affine(const NormArgs &a, const Tile &t)
     {
@@ -317,7 +323,7 @@ template <int V, int W> struct Affine {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = t.c0 + min(t.col, t.cols - 1) * V + v;
-            scale[v] = a.gamma ? a.gamma[c] : 1.f;
+            gamma[v] = a.gamma ? a.gamma[c] : 1.f;
             bias[v] = a.beta ? a.beta[c] : 0.f;
         }
     }
@@ -326,15 +332,24 @@ template <int V, int W> struct Affine {
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             mean[w] = stats[2 * group[w]];
+            rstd[w] = stats[2 * group[w] + 1];
 #pragma unroll
-            for (int v = 0; v < V / W; ++v) scale[w * (V / W) + v] *= stats[2 * group[w] + 1];
+            for (int v = 0; v < V / W; ++v) scale[w * (V / W) + v] = gamma[w * (V / W) + v] * rstd[w];
         }
+    }
+    template <int KIND> __device__ __forceinline__ float value(int v, float d) const
+    {
+        return activate<KIND>(KIND == QRM_ACT_RELU ? relu_z(d, rstd[v * W / V], gamma[v], bias[v]) : fmaf(d, scale[v], bias[v]));
     }
     template <int ACT, typename T> __device__ __forceinline__ Words<T, V> apply(const Words<T, V> &x, int act) const
     {
         float f[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) f[v] = activate<ACT>((x.get(v) - mean[v * W / V]) * scale[v] + bias[v], act);
+        for (int v = 0; v < V; ++v) {
+            const float d = x.get(v) - mean[v * W / V];
+            if constexpr (ACT != kAnyAct) f[v] = value<ACT>(v, d);
+            else f[v] = act == QRM_ACT_SILU ? value<QRM_ACT_SILU>(v, d) : act == QRM_ACT_RELU ? value<QRM_ACT_RELU>(v, d) : value<QRM_ACT_NONE>(v, d);
+        }
         Words<T, V> y;
         y.set(f);
         return y;
@@ -465,13 +480,13 @@ template <int V, int W, int ACT> struct Slopes {
             beta[v] = a.beta ? a.beta[c] : 0.f;
         }
     }
-    // dy act'(z).  A ReLU's z is rounded product by product, as the definition is written: its sign alone counts.
+    // dy act'(z)
     template <int KIND> __device__ __forceinline__ float dz_of(int v, float d, float dy) const
     {
 #pragma clang fp contract(off)
         const float r = rstd[v * W / V];
         if (KIND == QRM_ACT_NONE) return dy;
-        if (KIND == QRM_ACT_RELU) return (d * r) * gamma[v] + beta[v] <= 0.f ? 0.f : dy;
+        if (KIND == QRM_ACT_RELU) return relu_z(d, r, gamma[v], beta[v]) <= 0.f ? 0.f : dy;
         const float z = fmaf(d, gamma[v] * r, beta[v]); // (gamma rstd is the same for all pixels: kept in a register)
         const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f));
         return dy * (s * fmaf(z, 1.f - s, 1.f));
