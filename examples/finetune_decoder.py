@@ -30,6 +30,19 @@ WHITEN = 1e-5                               # of the strongest axis: the least t
 MEAN, STD = (0.485, 0.456, 0.406), (0.229, 0.224, 0.225)
 
 
+class Once(torch.autograd.Function):
+    """A gradient as it is.  The library has first derivatives alone: who differentiates one again, with respect to what it was computed of,
+    is told so instead of losing its share."""
+
+    @staticmethod
+    def forward(fn, grad, *of):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(fn, *_):
+        raise RuntimeError("the library's gradients cannot be differentiated again")
+
+
 class NormAct(torch.autograd.Function):
     """SiLU of a group norm over x [N,H,W,C], channels last, through the library."""
 
@@ -49,7 +62,7 @@ class NormAct(torch.autograd.Function):
         x, gamma, beta, mean, rstd = fn.saved_tensors
         dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
         fn.ctx.qrm_group_norm_backward(fn.desc, x, dy.contiguous(), gamma, beta, mean, rstd, dx, dgamma, dbeta)
-        return dx, dgamma, dbeta, None, None
+        return *(Once.apply(g, x, gamma, beta, dy) for g in (dx, dgamma, dbeta)), None, None
 
 
 class MessageLoss(torch.autograd.Function):
@@ -59,12 +72,13 @@ class MessageLoss(torch.autograd.Function):
     def forward(fn, logits, target, ctx, rs_weight, errors):
         loss, grad = logits.new_empty(1), torch.empty_like(logits)
         ctx.qrm_message_loss(logits.contiguous(), target, 1, logits.shape[0], BITS, rs_weight, loss, grad, errors)
-        fn.save_for_backward(grad)
+        fn.save_for_backward(logits, grad)
         return loss[0]
 
     @staticmethod
     def backward(fn, g):
-        return g * fn.saved_tensors[0], None, None, None, None
+        logits, grad = fn.saved_tensors
+        return Once.apply(g * grad, logits, g), None, None, None, None
 
 
 def conv3x3(x, w):
