@@ -406,7 +406,8 @@ typedef enum { QRM_ACT_NONE = 0, QRM_ACT_RELU = 1, QRM_ACT_SILU = 2 } qrm_act;
  * Errors: QRM_E_INVALID (NULL pointer, N < 0, P < 1, groups that do not divide C, an unknown type or activation, eps not above
  * zero, strides under C or (P-1) * pixel + C, an output in place of an input with other strides, a pointer not aligned to its elements,
  * one of d_mean and d_rstd alone),
- * QRM_E_UNSUPPORTED (C above 65536, a group of more than 1024 pieces of what the alignment allows to read at once, up to 16 bytes;
+ * QRM_E_UNSUPPORTED (C above 65536; a group of more than 1024 pieces: with D = C / groups, and V = the elements of up to 16 bytes that C,
+ * the strides and the addresses allow to be read at once, D / gcd(D, V) above 1024, as pieces have to divide a wide group: any odd D above 1024;
  * N or P of 2^31 and more, 2^32 threads and more for the tiles of all images: 2^24 images of one pixel), QRM_E_NOMEM.
  */
 typedef struct {

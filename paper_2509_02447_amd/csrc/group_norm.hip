@@ -26,11 +26,11 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
     p.V = std::min(16, align_bytes) / size;
     while (d.C % p.V || d.x_pixel % p.V || d.y_pixel % p.V || d.x_image % p.V || d.y_image % p.V) p.V /= 2;
     int64_t unit = std::lcm<int64_t>(D, p.V);
-    if (unit / p.V > kNormThreads) { // (pieces that straddle groups: the shared memory holds 256 of them)
+    if (unit / p.V > kNormThreads) { // (pieces that straddle groups: the shared memory holds 256 of them; those that divide a group are no more)
         p.V = std::gcd(D, p.V);
         unit = D;
     }
-    if (unit / p.V > kNormMaxThreads) return false;
+    if (unit / p.V > kNormMaxThreads) return false; // D / gcd(D, V), whichever
     p.W = D % p.V == 0 ? 1 : p.V % D == 0 ? p.V / D : p.V;
     auto cut = [&](int bytes, int threads) { // whole groups, at least so many bytes wide
         NormCut c;

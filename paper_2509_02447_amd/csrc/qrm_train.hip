@@ -73,7 +73,7 @@ qrm_status start(qrm_ctx *c)
 qrm_status plan(qrm_ctx *c, const qrm_group_norm_desc &d, int align, bool backward, bool channels, NormPlan *p)
 {
     if (!plan_norm(d, align, backward, channels, c->num_cu, p))
-        return fail(c, QRM_E_UNSUPPORTED, "a group has more than 1024 pieces of what the alignment allows to read at once");
+        return fail(c, QRM_E_UNSUPPORTED, "a group has more than 1024 pieces: its channels over their common divisor with the elements that are read at once");
     // (a launch has less than 2^32 threads; those behind the tiles, of the channels, are under 2^24)
     auto fits = [&](const NormCut &cut) { return ((double)d.N * cut.tiles * cut.chunks + 8192.0) * cut.threads < 4294967296.0; };
     if (!fits(p->first) || (!p->whole && !fits(p->second))) return fail(c, QRM_E_UNSUPPORTED, "the tiles of all images need 2^32 threads and more");
