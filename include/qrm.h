@@ -19,8 +19,9 @@
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *     Calls enqueue work on it and return without waiting.
  *   - Return value is a qrm_status; nothing aborts or throws.  On anything but
- *     QRM_OK no kernel of that call has been launched unless stated, and
- *     qrm_last_error() describes the reason.
+ *     QRM_OK and QRM_E_DEVICE no kernel of that call has been launched, and
+ *     qrm_last_error() describes the reason.  QRM_E_DEVICE: a HIP call has failed; launches of the same call before it may run, its
+ *     outputs are not to be used.
  *   - N == 0 is a successful no-op.
  *   - Outputs are the same bits from call to call, on any stream, and a tile's do not depend on the tiles around it as long as its
  *     batch runs the same schedule: a launch per block and all blocks in one launch (batches of few tiles) give the same bits; two
@@ -441,7 +442,9 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
  * qrm_adamw_create: h_tensors HOST [n_tensors], read during the call.  qrm_adamw_step: h_grads HOST [n_tensors] of device pointers of
  * grad_type, read during the call; NULL = the tensor has no gradient at this step and stays as it is, moments included.  step counts from
  * 1.  d_grad_scale f32 [1] on the device, read by the kernels (a clipping factor, the inverse of a loss scale), or NULL = 1.
- * A launch takes the gradients of several hundred tensors.  qrm_adamw_destroy waits for the device; NULL is ignored.
+ * A launch takes the gradients of several hundred tensors: after QRM_E_DEVICE the tensors before the one that qrm_last_error names have made
+ * their step, which is not to be repeated for them.  Recorded into a graph, a step keeps its number, rates and gradients' addresses: a replay makes
+ * the same step once more, not the next one.  qrm_adamw_destroy waits for the device; NULL is ignored.
  * Errors: QRM_E_INVALID (NULL pointer, n < 0, unknown type, state_bits not 8 or 32, a copy of other than 16 bits or beside parameters that are
  * not f32, a pointer not aligned to its elements, step < 1, lr, weight_decay, lr_scale or eps negative or not finite, a beta outside [0, 1), a plan of
  * another device), QRM_E_NOMEM, QRM_E_UNSUPPORTED (a plan of 2^24 and more pieces of 4096 elements; 2^36 codes

@@ -2,6 +2,7 @@
 #include "qrm_train.h"
 
 #include <math.h>
+#include <stdio.h>
 
 #include <new>
 #include <vector>
@@ -256,7 +257,11 @@ qrm_status qrm_adamw_step(qrm_ctx *c, qrm_adamw *o, const void *const *h_grads, 
         const uint32_t from = o->first_piece[i], to = o->first_piece[i + count];
         if (from == to) continue;
         hipError_t e = launch_adamw(o->types, o->tensors, o->pieces, from, to - from, i, h_grads + i, count, s, (hipStream_t)stream);
-        if (e != hipSuccess) return hip_fail(c, e, "adamw launch");
+        if (e != hipSuccess) {
+            char what[64];
+            snprintf(what, sizeof what, "adamw launch of tensor %d and those behind it", i);
+            return hip_fail(c, e, what);
+        }
     }
     return QRM_OK;
 }
