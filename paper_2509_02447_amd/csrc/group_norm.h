@@ -524,7 +524,6 @@ template <int V, int W, int ACT, typename FC, typename FG>
 __device__ __forceinline__ void sum_chunk(const NormArgs &a, const Tile &t, const Slopes<V, W, ACT> &c, const float (&b)[V], const float (&g)[V], float2 *lds, FC by_channel, FG by_group)
 {
     const int nch = t.cols * V, threads = blockDim.x;
-    __syncthreads(); // (who read the last call's sums is done)
     if (t.r < t.rpar) {
 #pragma unroll
         for (int v = 0; v < V; ++v) lds[t.r * nch + t.col * V + v] = make_float2(b[v], g[v] * c.rstd[v * W / V]);
@@ -802,7 +801,7 @@ NormArgs norm_args(const NormCall &c, const NormPlan &p, const NormCut &cut, voi
     a.mean = c.mean; a.rstd = c.rstd; a.dgamma = c.dgamma; a.dbeta = c.dbeta;
     a.N = c.d.N; a.P = c.d.P;
     a.xp = c.d.x_pixel; a.xn = c.d.x_image; a.yp = c.d.y_pixel; a.yn = c.d.y_image;
-    a.C = c.d.C; a.G = c.d.groups; a.D = c.d.C / c.d.groups; 
+    a.C = c.d.C; a.G = c.d.groups; a.D = c.d.C / c.d.groups;
     a.ct = cut.ct; a.tiles = cut.tiles; a.chunks = cut.chunks; a.rpar = cut.threads / (cut.ct / p.V);
     a.side = p.whole ? std::max(1, 128 / (cut.ct * type_bytes(c.d.type))) : 1;
     a.turned = a.side > 1 ? cut.blocks(a.N) / (kDies * a.side) * (kDies * a.side) : 0;

@@ -19,7 +19,6 @@ template <int BYTES> struct Raw {
 };
 template <> struct Raw<4> { typedef uint32_t type; };
 template <> struct Raw<2> { typedef uint16_t type; };
-template <> struct Raw<1> { typedef uint8_t type; };
 template <typename T, int V, bool STREAM = false> __device__ __forceinline__ Pack<T, V> load_pack(const T *p)
 {
     typedef typename Raw<sizeof(T) * V>::type R;
@@ -124,7 +123,7 @@ struct NormPlan {
     NormCut first, second;
     bool whole;        // one launch (`first`): a workgroup holds a whole tile of an image, up to `pixels` pieces a thread
     int pixels;
-    bool stream;       // two launches: outputs past the caches
+    bool stream;       // outputs past the caches
     bool channels;     // sums of the channels go through the workspace
     size_t part_words; // of the chunks' groups in the workspace, before the channels' sums
     size_t bytes;      // of workspace
