@@ -235,8 +235,8 @@ def _dptr_of(t, kinds, n: int) -> Optional[int]:
     """Device pointer of a contiguous tensor of one of the dtypes `kinds` and at least n elements (or None)."""
     if t is None:
         return None
-    assert t.dtype in kinds and t.numel() >= n, "a tensor has another type than the call takes, or too few elements"
-    assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous and on the GPU"
+    assert t.dtype in kinds and t.numel() >= n and t.is_cuda and t.is_contiguous(), \
+        "device tensors must be of the type and of at least the size that the call takes, contiguous and on the GPU"
     return t.data_ptr()
 
 
@@ -360,7 +360,7 @@ class Context:
             pass
 
     def _check(self, st: int):
-        if st:                                               # (QRM_OK is 0)
+        if st != QRM_OK:
             raise QrmError(st, self._lib.qrm_last_error(self._h).decode())
 
     def last_error(self) -> str:
@@ -507,9 +507,10 @@ class Context:
     def qrm_message_loss(self, d_logits, d_target, target_rows, N, n_bits, rs_weight, d_loss, d_grad=None, d_bit_errors=None,
                          d_symbol_errors=None, stream=None):
         N, n_bits, target_rows, k = int(N), int(n_bits), int(target_rows), _kinds()
-        self._check(self._lib.qrm_message_loss(self._h, _dptr_of(d_logits, k.f32, N * n_bits), _dptr_of(d_target, k.byte, target_rows * n_bits), target_rows,
-                                               N, n_bits, float(rs_weight), _dptr_of(d_loss, k.f32, 1), _dptr_of(d_grad, k.f32, N * n_bits),
-                                               _dptr_of(d_bit_errors, k.i32, N), _dptr_of(d_symbol_errors, k.i32, N), _stream_handle(stream)))
+        f32, i32, cells = k.f32, k.i32, N * n_bits
+        self._check(self._lib.qrm_message_loss(self._h, _dptr_of(d_logits, f32, cells), _dptr_of(d_target, k.byte, target_rows * n_bits), target_rows,
+                                               N, n_bits, float(rs_weight), _dptr_of(d_loss, f32, 1), _dptr_of(d_grad, f32, cells),
+                                               _dptr_of(d_bit_errors, i32, N), _dptr_of(d_symbol_errors, i32, N), _stream_handle(stream)))
 
 
 class AdamW:
