@@ -40,6 +40,20 @@ class _RsDesc(C.Structure):
 class _GroupNormDesc(C.Structure):
     _fields_ = [("N", C.c_int64), ("P", C.c_int64), ("C", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32), ("act", C.c_int32),
                 ("eps", C.c_float), ("x_pixel", C.c_int64), ("x_image", C.c_int64), ("y_pixel", C.c_int64), ("y_image", C.c_int64)]
+    _maps = None
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name != "_maps":
+            super().__setattr__("_maps", None)
+
+    def maps(self):
+        """What the call's tensors have to be: (dtype or None, shape of a map, strides of x, strides of y, statistics), read once."""
+        if self._maps is None:
+            N, P, C_ = self.N, self.P, self.C
+            strides = [(image or P * (pixel or C_), pixel or C_, 1) for pixel, image in ((self.x_pixel, self.x_image), (self.y_pixel, self.y_image))]
+            self._maps = (_kinds().dtypes.get(self.type), (N, P, C_), *strides, N * self.groups)
+        return self._maps
 
 
 class _AdamwTensor(C.Structure):
@@ -221,8 +235,9 @@ class _Kinds:
 
     def __init__(self):
         import torch
-        self.f32, self.i32, self.byte = (torch.float32,), (torch.int32,), (torch.uint8, torch.int8, torch.bool)
+        self.f32, self.i32 = torch.float32, torch.int32
         self.codes = {torch.float32: QRM_F32, torch.bfloat16: QRM_BF16, torch.float16: QRM_F16}
+        self.dtypes = {code: dtype for dtype, code in self.codes.items()}
 
 
 def _kinds() -> _Kinds:
@@ -231,25 +246,32 @@ def _kinds() -> _Kinds:
     return _Kinds._known
 
 
-def _dptr_of(t, kinds, n: int) -> Optional[int]:
-    """Device pointer of a contiguous tensor of one of the dtypes `kinds` and at least n elements (or None)."""
+def _dptr_of(t, dtype, n: int) -> Optional[int]:
+    """Device pointer of a contiguous tensor of at least n elements of a dtype (or None)."""
     if t is None:
         return None
-    assert t.dtype in kinds and t.numel() >= n and t.is_cuda and t.is_contiguous(), \
+    assert t.dtype is dtype and t.numel() >= n and t.is_cuda and t.is_contiguous(), \
         "device tensors must be of the type and of at least the size that the call takes, contiguous and on the GPU"
+    return t.data_ptr()
+
+
+def _dptr_bytes(t, n: int) -> Optional[int]:
+    """The same of elements of one byte, whatever they are called."""
+    if t is None:
+        return None
+    assert t.element_size() == 1 and t.numel() >= n and t.is_cuda and t.is_contiguous(), \
+        "device tensors must have one byte an element and at least the size that the call takes, be contiguous and on the GPU"
     return t.data_ptr()
 
 
 def _lies(t, N: int, P: int, C: int, pixel: int, image: int) -> bool:
     """Whether channel c of pixel p of image i of a map [..,C] lies i * image + p * pixel + c elements from its first one.  The tensor's
     channels may be more than C and its images more than N; pixels may have several dimensions."""
-    shape, stride = t.shape, t.stride()
-    if stride == (image, pixel, 1) and shape == (N, P, C):
-        return True
     if N < 1 or P < 1 or C < 1:                              # no images, or refused
         return True
     if pixel == C and (image == P * C or N == 1) and t.numel() == N * P * C and t.is_contiguous():
         return True
+    shape, stride = t.shape, t.stride()
     if len(shape) < 2:                                       # a buffer
         return t.is_contiguous() and t.numel() >= (N - 1) * image + (P - 1) * pixel + C
     if shape[-1] < C or (C > 1 and stride[-1] != 1):
@@ -265,13 +287,15 @@ def _lies(t, N: int, P: int, C: int, pixel: int, image: int) -> bool:
     return inside == left
 
 
-def _dptr_map(t, codes, code: int, N: int, P: int, C: int, pixel: int, image: int) -> Optional[int]:
-    """Device pointer of a map that lies as its descriptor says, strides in elements, 0 = dense (or None)."""
+def _dptr_map(t, dtype, shape, strides) -> Optional[int]:
+    """Device pointer of a map [N,P,C] that lies as its descriptor says (or None)."""
     if t is None:
         return None
-    pixel = pixel or C
+    if t.dtype is dtype and t.is_cuda and t.stride() == strides and t.shape == shape:
+        return t.data_ptr()
     assert t.is_cuda, "device tensors must be on the GPU"
-    assert codes.get(t.dtype, -1) == code and _lies(t, N, P, C, pixel, image or P * pixel), "a map has another type, size or strides than its descriptor"
+    # (a dtype of None: a descriptor that is refused)
+    assert (t.dtype is dtype or dtype is None) and _lies(t, *shape, strides[1], strides[0]), "a map has another type, size or strides than its descriptor"
     return t.data_ptr()
 
 
@@ -483,32 +507,33 @@ class Context:
                                                 _stream_handle(stream)))
 
     def qrm_group_norm(self, desc, d_x, d_gamma, d_beta, d_y, d_mean=None, d_rstd=None, stream=None):
-        k, N, C_ = _kinds(), desc.N, desc.C
-        f32, stats, lie = k.f32, N * desc.groups, (k.codes, desc.type, N, desc.P, C_)
-        self._check(self._lib.qrm_group_norm(self._h, C.byref(desc), _dptr_map(d_x, *lie, desc.x_pixel, desc.x_image), _dptr_of(d_gamma, f32, C_),
-                                             _dptr_of(d_beta, f32, C_), _dptr_map(d_y, *lie, desc.y_pixel, desc.y_image), _dptr_of(d_mean, f32, stats),
+        dtype, shape, x, y, stats = desc.maps()
+        f32, C_ = _kinds().f32, shape[2]
+        self._check(self._lib.qrm_group_norm(self._h, C.byref(desc), _dptr_map(d_x, dtype, shape, x), _dptr_of(d_gamma, f32, C_),
+                                             _dptr_of(d_beta, f32, C_), _dptr_map(d_y, dtype, shape, y), _dptr_of(d_mean, f32, stats),
                                              _dptr_of(d_rstd, f32, stats), _stream_handle(stream)))
 
     def qrm_group_norm_backward(self, desc, d_x, d_dy, d_gamma, d_beta, d_mean, d_rstd, d_dx, d_dgamma=None, d_dbeta=None,
                                 stream=None):
-        k, N, C_ = _kinds(), desc.N, desc.C
-        f32, stats, lie, x_pixel, x_image = k.f32, N * desc.groups, (k.codes, desc.type, N, desc.P, C_), desc.x_pixel, desc.x_image
-        self._check(self._lib.qrm_group_norm_backward(self._h, C.byref(desc), _dptr_map(d_x, *lie, x_pixel, x_image),
-                                                      _dptr_map(d_dy, *lie, desc.y_pixel, desc.y_image), _dptr_of(d_gamma, f32, C_),
-                                                      _dptr_of(d_beta, f32, C_), _dptr_of(d_mean, f32, stats), _dptr_of(d_rstd, f32, stats),
-                                                      _dptr_map(d_dx, *lie, x_pixel, x_image), _dptr_of(d_dgamma, f32, C_),
+        dtype, shape, x, y, stats = desc.maps()
+        f32, C_ = _kinds().f32, shape[2]
+        self._check(self._lib.qrm_group_norm_backward(self._h, C.byref(desc), _dptr_map(d_x, dtype, shape, x), _dptr_map(d_dy, dtype, shape, y),
+                                                      _dptr_of(d_gamma, f32, C_), _dptr_of(d_beta, f32, C_), _dptr_of(d_mean, f32, stats),
+                                                      _dptr_of(d_rstd, f32, stats), _dptr_map(d_dx, dtype, shape, x), _dptr_of(d_dgamma, f32, C_),
                                                       _dptr_of(d_dbeta, f32, C_), _stream_handle(stream)))
 
     def qrm_unpack_moment(self, moment: int, d_codes, d_scales, n, d_out, stream=None):
-        n, k = int(n), _kinds()
-        self._check(self._lib.qrm_unpack_moment(self._h, int(moment), _dptr_of(d_codes, k.byte, n), _dptr_of(d_scales, k.f32, -(-n // QRM_MOMENT_BLOCK)), n,
-                                                type_code(d_out.dtype), _dptr_of(d_out, k.codes, n), _stream_handle(stream)))
+        n = int(n)
+        code = type_code(d_out.dtype)
+        self._check(self._lib.qrm_unpack_moment(self._h, int(moment), _dptr_bytes(d_codes, n), _dptr_of(d_scales, _kinds().f32, -(-n // QRM_MOMENT_BLOCK)),
+                                                n, code, _dptr_of(d_out, d_out.dtype, n), _stream_handle(stream)))
 
     def qrm_message_loss(self, d_logits, d_target, target_rows, N, n_bits, rs_weight, d_loss, d_grad=None, d_bit_errors=None,
                          d_symbol_errors=None, stream=None):
-        N, n_bits, target_rows, k = int(N), int(n_bits), int(target_rows), _kinds()
-        f32, i32, cells = k.f32, k.i32, N * n_bits
-        self._check(self._lib.qrm_message_loss(self._h, _dptr_of(d_logits, f32, cells), _dptr_of(d_target, k.byte, target_rows * n_bits), target_rows,
+        N, n_bits, target_rows = int(N), int(n_bits), int(target_rows)
+        k, cells = _kinds(), N * n_bits
+        f32, i32 = k.f32, k.i32
+        self._check(self._lib.qrm_message_loss(self._h, _dptr_of(d_logits, f32, cells), _dptr_bytes(d_target, target_rows * n_bits), target_rows,
                                                N, n_bits, float(rs_weight), _dptr_of(d_loss, f32, 1), _dptr_of(d_grad, f32, cells),
                                                _dptr_of(d_bit_errors, i32, N), _dptr_of(d_symbol_errors, i32, N), _stream_handle(stream)))
 

@@ -60,3 +60,14 @@ def test_what_is_taken_lies_as_the_map_does(seed):
         elif mine.shape[0] == n * p:
             assert not right, (shape, stride, n, p, c, pixel, image)
     assert taken > 300
+
+
+def test_a_descriptor_that_is_changed_says_so():
+    d = binding.group_norm_desc(2, 10, 8, 4, torch.bfloat16, "silu")
+    assert d.maps() == (torch.bfloat16, (2, 10, 8), (80, 8, 1), (80, 8, 1), 8)
+    d.x_pixel, d.y_image, d.N = 12, 99, 3
+    assert d.maps() == (torch.bfloat16, (3, 10, 8), (120, 12, 1), (99, 8, 1), 12)
+    d.type = 7
+    assert d.maps()[0] is None and d.type == 7 and d.P == 10
+    d.groups, d.type = 2, binding.QRM_F32
+    assert d.maps() == (torch.float32, (3, 10, 8), (120, 12, 1), (99, 8, 1), 6)
