@@ -481,9 +481,7 @@ qrm_status get_counters(qrm_ctx *c, hipStream_t s, QrmSlot *slot)
 {
     if (slot->counters) return QRM_OK;
     // (a graph that clears them would do so at every replay)
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(s, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone)
-        return fail(c, QRM_E_INVALID, "a stream's first call of this kind cannot be recorded into a graph");
+    if (recording(s)) return fail(c, QRM_E_INVALID, "a stream's first call of this kind cannot be recorded into a graph");
     void *p = nullptr;
     if (hipMalloc(&p, kSlotCounters * sizeof(uint32_t)) != hipSuccess) {
         (void)hipGetLastError();
