@@ -6,8 +6,8 @@
 // registers.  Statistics need all of a group before the first output: a map whose tiles fit the registers of a workgroup each takes one launch and is read once;
 // all others take two, of which one leaves each chunk's part and the other joins the parts of its groups in a fixed order and reads the map again.
 //
-// Bound by memory where the map is large: 4 images of 256 x 256 pixels and 128 channels in bf16 take 37.4 us (15.6 + 22.3, 201 MB read and written at 5.4 TB/s; read
-// once, at the rate of a large copy, 26.2), their backward pass 59.9 us (29.7 + 32.5, 335 MB at 5.6 TB/s; 39.2).  The second reading comes from the memory-side cache in part.  Vector
+// Bound by memory where the map is large: 4 images of 256 x 256 pixels and 128 channels in bf16 take 37.6 us (15.6 + 22.5, 201 MB read and written at 5.4 TB/s; read
+// once, at the rate of a large copy, 26.2), their backward pass 60.2 us (30.3 + 32.3, 335 MB at 5.6 TB/s; 39.2).  The second reading comes from the memory-side cache in part.  Vector
 // instructions (silu: 20 slots an element forward, 43 backward, an exponential and an inverse four each) are 17 and 36 us of that and run beside the memory.  Bound
 // by latency where it is small: 4 images of 32 x 32 and 512 channels 7.9 us.
 //
@@ -356,7 +356,7 @@ template <int V, int W> struct Affine {
     }
 };
 
-// One launch: R pixels a thread, a whole tile a workgroup.  1 image of 256 pixels and 512 channels (bf16, silu) 5.7 us, of which 4 are launch and
+// One launch: R pixels a thread, a whole tile a workgroup.  1 image of 256 pixels and 512 channels (bf16, silu) 6.3 us, of which 4 are launch and
 // the first loads; two launches 9.7.
 template <typename T, int V, int W, int ACT, int R, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_whole_kernel(NormArgs a)
 {
@@ -413,7 +413,7 @@ template <typename T, int V, int W> __global__ __launch_bounds__(kMaxThreads) vo
     join_chunk<V, W>(a, t, mine, lds, [&](int g, float mean, float m2) { *part_at(a, t, g, t.s) = make_float2(mean, m2); });
 }
 
-// .. the second: joins the chunks' parts and writes the outputs.  134 MB in 22.3 us, 6.0 TB/s.
+// .. the second: joins the chunks' parts and writes the outputs.  134 MB in 22.5 us, 6.0 TB/s.
 template <typename T, int V, int W, int ACT, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_apply_kernel(NormArgs a)
 {
     constexpr int R = 4;
@@ -618,7 +618,7 @@ __global__ __launch_bounds__(kThreads) void norm_channels_kernel(NormArgs a)
 }
 
 // One launch (and one for the channels of several images): R pixels a thread, a whole tile a workgroup.  dz stays in registers beside the
-// input.  1 image of 256 pixels and 512 channels 7.0 us, two launches 11.5.
+// input.  1 image of 256 pixels and 512 channels 7.3 us, two launches 11.6.
 template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__(kMaxThreads / 2) void norm_grad_whole_kernel(NormArgs a)
 {
     extern __shared__ __align__(16) float2 lds[];
@@ -675,7 +675,7 @@ template <typename T, int V, int W, int ACT, int R> __global__ __launch_bounds__
         }
 }
 
-// Two launches, the first: sums of dz and dz h over the chunk, channel by channel and weighted with gamma group by group.  134 MB in 29.7 us, 4.5
+// Two launches, the first: sums of dz and dz h over the chunk, channel by channel and weighted with gamma group by group.  134 MB in 30.3 us, 4.4
 // TB/s, and 17 us of arithmetic, not all of it beside the loads.  A thread adds runs of kRun pixels, then their sums, of which kNormRow pixels leave 43: with
 // thousands of equal numbers one after the other, roundings that all go one way would grow to a thousand units in the last place.
 constexpr int kRun = 48;
@@ -729,7 +729,7 @@ template <typename T, int V, int W, int ACT> __global__ __launch_bounds__(kMaxTh
               [&](int k, float sa, float sb) { *part_at(a, t, k, t.s) = make_float2(sa, sb); });
 }
 
-// .. the second: dx, and in the workgroups behind those dgamma and dbeta of 16 channels each.  201 MB in 32.5 us, 6.2 TB/s.
+// .. the second: dx, and in the workgroups behind those dgamma and dbeta of 16 channels each.  201 MB in 32.3 us, 6.2 TB/s.
 template <typename T, int V, int W, int ACT, bool STREAM> __global__ __launch_bounds__(kMaxThreads) void norm_grad_apply_kernel(NormArgs a, uint32_t apply_blocks)
 {
     constexpr int R = 2;

@@ -49,9 +49,9 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
     // A tile for one launch is the narrowest, down to 16 channels (8 forward), of which there are not more than compute units: a line's tiles are numbered so that one
     // die's cache serves them all (find_tile).  One launch is taken where a tile fits a workgroup and is over before a second launch would have begun, or
     // where compute units are busy anyway and the map is read once.  Measured with silu and 512 channels in bf16 on one map again and again, one launch / two, us: 1 image
-    // of 256 / 1024 / 2048 pixels 5.7 / 9.7, 7.4 / 9.7, 10.1 / 9.9; 4 images of 1024 / 2048 / 4096 7.9 / 10.2, 11.1 / 12.2, 16.4 / 16.4 (tiles of a line, 1024 pixels: 12.8); 16 images
+    // of 256 / 1024 / 2048 pixels 6.3 / 9.7, 7.5 / 9.7, 10.1 / 9.9; 4 images of 1024 / 2048 / 4096 7.9 / 10.2, 11.1 / 12.2, 16.4 / 16.4 (tiles of a line, 1024 pixels: 12.8); 16 images
     // 11.7 / 16.3, 18.9 / 22.5, 28.8 / 34.6 (a line 14.7, 24.1); 64 images of 1024, on other maps in turn, 24.5 / 39.0; backward, 1 image of 256 / 1024 / 2048 pixels
-    // 6.4 / 11.6, 8.7 / 11.6, 14.8 / 11.8; 4 images 9.1 / 11.7, 11.8 / 12.3, 18.7 / 15.4; 16 images of 512 / 1024 11.7 / 15.3, 18.3 / 20.2.
+    // 7.3 / 11.6, 8.4 / 11.6, 14.8 / 11.8; 4 images 9.1 / 11.7, 11.8 / 12.3, 18.7 / 15.4; 16 images of 512 / 1024 11.7 / 15.3, 18.3 / 20.2.
     const int most_threads = p.W > 2 ? 256 : backward ? kNormMaxThreads / 2 : kNormMaxThreads;
     const int least = (backward ? 16 : 8) * size;
     auto fit = [&] { // pixels and threads of a tile
