@@ -444,7 +444,7 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
  * 1.  d_grad_scale f32 [1] on the device, read by the kernels (a clipping factor, the inverse of a loss scale), or NULL = 1.
  * A launch takes the gradients of several hundred tensors: after QRM_E_DEVICE the tensors before the one that qrm_last_error names have made
  * their step, which is not to be repeated for them.  Recorded into a graph, a step keeps its number, rates and gradients' addresses: a replay makes
- * the same step once more, not the next one.  qrm_adamw_destroy waits for the device; NULL is ignored.
+ * the same step once more, not the next one, and reads the plan, which has to be there.  qrm_adamw_destroy waits for the device; NULL is ignored.
  * Errors: QRM_E_INVALID (NULL pointer, n < 0, unknown type, state_bits not 8 or 32, a copy of other than 16 bits or beside parameters that are
  * not f32, a pointer not aligned to its elements, step < 1, lr, weight_decay, lr_scale or eps negative or not finite, a beta outside [0, 1), a plan of
  * another device), QRM_E_NOMEM, QRM_E_UNSUPPORTED (a plan of 2^24 and more pieces of 4096 elements; 2^36 codes

@@ -52,6 +52,9 @@ bool plan_norm(const qrm_group_norm_desc &d, int align_bytes, bool backward, boo
     // of 256 / 1024 / 2048 pixels 6.3 / 9.7, 7.5 / 9.7, 10.1 / 9.9; 4 images of 1024 / 2048 / 4096 7.9 / 10.2, 11.1 / 12.2, 16.4 / 16.4 (tiles of a line, 1024 pixels: 12.8); 16 images
     // 11.7 / 16.3, 18.9 / 22.5, 28.8 / 34.6 (a line 14.7, 24.1); 64 images of 1024, on other maps in turn, 24.5 / 39.0; backward, 1 image of 256 / 1024 / 2048 pixels
     // 7.3 / 11.6, 8.4 / 11.6, 14.8 / 11.8; 4 images 9.1 / 11.7, 11.8 / 12.3, 18.7 / 15.4; 16 images of 512 / 1024 11.7 / 15.3, 18.3 / 20.2.
+    // In f32 1 image of 1024 pixels 7.4 / 9.4, 4 of 2048 10.9 / 13.4, 16 of 2048 24.2 / 31.1, 64 of 1024 42.7 / 64.8; backward 1 of 1024 9.8 / 10.6, 16 and 64 of 256 9.7 / 11.9,
+    // 21.4 / 28.5.  128 channels, bf16 4 of 2048 8.2 / 10.5, 64 of 1024 11.2 / 16.9, backward 19.8 / 20.6; 320 channels, ten a group, bf16 16 of 256 8.6 / 12.6, backward 11.4 / 14.3. In
+    // f32 these last are the one family that the rule costs something: backward, 16 and 64 images of 256 pixels 12.0 / 11.4, 27.8 / 26.3.
     const int most_threads = p.W > 2 ? 256 : backward ? kNormMaxThreads / 2 : kNormMaxThreads;
     const int least = (backward ? 16 : 8) * size;
     auto fit = [&] { // pixels and threads of a tile
