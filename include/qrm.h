@@ -427,6 +427,46 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
                                            void *d_dx, float *d_dgamma, float *d_dbeta, void *stream);
 
 /*
+ * Attention over the rows of a map: an image's pixels look at each other, or at the rows of a prompt.  q, o [N,Lq,heads,D], k, v [N,Lk,kv_heads,D]: N images;
+ * heads / kv_heads query heads in a row share a key head (head h has key head h / (heads / kv_heads)).  Per image and head
+ *   S_ij = scale q_i . k_j where query i sees key j,  lse_i = log sum_j exp S_ij,  P_ij = exp(S_ij - lse_i),  o_i = sum_j P_ij v_j.
+ * d_q_len, d_k_len i32 [N] on the device, or NULL = Lq, Lk: only so many of an image's queries (keys) are there (less than zero counts as zero, more than Lq, Lk
+ * as that).  Rows behind them are not read (not as values: what they hold, NaNs too, reaches nothing).  causal: query i sees key j if
+ * j <= i + k_len - q_len: the queries are the last q_len of the k_len.  A row that sees nothing, or is not there, has o = 0 and lse = -inf.
+ * Scores, sums, lse and results are held in 32 bits; 16-bit types: P is rounded to the type, unsystematically, for the product with v; o is rounded once.
+ * f32: all in 32 bits.  d_lse f32 [N,heads,Lq], what the backward pass needs, or NULL.
+ * Elements of a row lie side by side; strides in elements of neighbouring rows, heads, images (0 = dense: D a head, heads * D a row): any order of the three,
+ * as long as rows do not overlap.  Rows that do not lie on 16 bytes, or whose D is not a multiple of them, are copied to the workspace first.
+ *
+ * Backward: with dP_ij = do_i . v_j, delta_i = do_i . o_i, dS_ij = P_ij (dP_ij - delta_i), P from S and the given lse
+ *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij do_i   (dk, dv over all heads that share the key head).
+ * do has o's strides, dq, dk and dv those of q, k and v; each of the three may be NULL (not wanted).  16-bit types: P and dS are rounded to the type (f16:
+ * with a factor that keeps a row's largest in range) for the second products.  Rows that are not there have gradients of zero, also where do is not finite.
+ * The same bits from call to call.  A value that is not finite in a row that is there reaches the outputs of its image and key head, no others.
+ * Errors: QRM_E_INVALID (NULL pointer, N, Lq or Lk < 0, kv_heads that do not divide heads, D < 1, an unknown type, causal not 0 or 1, scale not above
+ * zero, strides with which rows overlap, an output that is an input, two outputs that are one, no output, a pointer not aligned to its elements),
+ * QRM_E_UNSUPPORTED (D above QRM_ATTENTION_MAX_D; N, Lk or Lq * heads above 2^30, N * heads above 2^23, 2^32 threads and more for the rows of
+ * all images), QRM_E_NOMEM.
+ */
+#define QRM_ATTENTION_MAX_D 512
+typedef struct {
+    int64_t N, Lq, Lk;
+    int32_t heads, kv_heads, D;
+    int32_t type;   /* qrm_type of q, k, v, o and the gradients */
+    int32_t causal; /* 0 or 1 */
+    float scale;    /* usually 1 / sqrt(D) */
+    int64_t q_row, q_head, q_image; /* distance of neighbouring rows / heads / images of q and dq, in elements */
+    int64_t k_row, k_head, k_image; /* .. of k and dk */
+    int64_t v_row, v_head, v_image; /* .. of v and dv */
+    int64_t o_row, o_head, o_image; /* .. of o and do */
+} qrm_attention_desc;
+QRM_API qrm_status qrm_attention(qrm_ctx *ctx, const qrm_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v,
+                                 const int32_t *d_q_len, const int32_t *d_k_len, void *d_o, float *d_lse, void *stream);
+QRM_API qrm_status qrm_attention_backward(qrm_ctx *ctx, const qrm_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v,
+                                          const void *d_o, const void *d_do, const float *d_lse, const int32_t *d_q_len, const int32_t *d_k_len,
+                                          void *d_dq, void *d_dk, void *d_dv, void *stream);
+
+/*
  * AdamW over all tensors of a network in one call.  A plan (qrm_adamw) holds the addresses and sizes of the parameters and moments, which
  * stay the caller's and have to stay where they are while the plan is used; gradients are named at every step.  For each element
  *   g = grad * grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
@@ -451,6 +491,16 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
  * and more to unpack).
  *
  * qrm_unpack_moment: the values that 8-bit codes stand for, f32 or bf16 [n]: moment 0 = m, 1 = v.
+ *
+ * Clipping by the norm of all gradients of a step, h_grads as in qrm_adamw_step:
+ *   norm = u sqrt(sum g^2),  scale = u min(1, max_norm / norm),  u = *d_unscale (f32 [1] on the device: the inverse of a loss scale or of a number of
+ *   passes that were added up, read by the kernels), or 1 where it is NULL.
+ * qrm_adamw_grad_norm writes both, f32 [1] each (either may be NULL); d_scale is what qrm_adamw_step takes as d_grad_scale, which clips without another pass
+ * over the gradients.  Squares and sums in 64 bits: no gradient of 32 bits overflows there; a norm above 32 bits' largest is infinite in d_norm alone.
+ * A gradient that is not finite makes the norm inf or NaN and the scale u * 0 or NaN; without any gradient the norm is 0 and the scale u.  The same bits from call to call.
+ * qrm_adamw_scale_grads: out = grad * *d_scale, rounded once to grad_type, for other optimisers: h_outs HOST [n_tensors] of device pointers, each its
+ * gradient's own (in place) or a buffer that overlaps nothing; NULL where the gradient is NULL, and only there.
+ * Errors: as qrm_adamw_step where they apply, QRM_E_INVALID (max_norm not above zero (inf is: no clipping), d_norm and d_scale both NULL, an output at d_unscale, a missing output).
  */
 #define QRM_MOMENT_BLOCK 256
 typedef struct qrm_adamw qrm_adamw; /* opaque, library-owned */
@@ -471,6 +521,9 @@ QRM_API qrm_status qrm_adamw_create(qrm_ctx *ctx, const qrm_adamw_desc *desc, co
 QRM_API void qrm_adamw_destroy(qrm_adamw *opt);
 QRM_API qrm_status qrm_adamw_step(qrm_ctx *ctx, qrm_adamw *opt, const void *const *h_grads, int64_t step, double lr, double beta1, double beta2,
                                   double eps, const float *d_grad_scale, void *stream);
+QRM_API qrm_status qrm_adamw_grad_norm(qrm_ctx *ctx, qrm_adamw *opt, const void *const *h_grads, double max_norm, const float *d_unscale, float *d_norm,
+                                       float *d_scale, void *stream);
+QRM_API qrm_status qrm_adamw_scale_grads(qrm_ctx *ctx, qrm_adamw *opt, const void *const *h_grads, const float *d_scale, void *const *h_outs, void *stream);
 QRM_API qrm_status qrm_unpack_moment(qrm_ctx *ctx, int32_t moment, const void *d_codes, const float *d_scales, int64_t n, int32_t out_type,
                                      void *d_out, void *stream);
 

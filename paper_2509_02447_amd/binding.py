@@ -56,6 +56,29 @@ class _GroupNormDesc(C.Structure):
         return self._maps
 
 
+class _AttentionDesc(C.Structure):
+    _fields_ = [("N", C.c_int64), ("Lq", C.c_int64), ("Lk", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("D", C.c_int32),
+                ("type", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float)] + \
+               [(f"{t}_{s}", C.c_int64) for t in "qkvo" for s in ("row", "head", "image")]
+    _rows = None
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name != "_rows":
+            super().__setattr__("_rows", None)
+
+    def rows(self):
+        """What the call's tensors have to be: (dtype or None, {tensor: (shape, strides)} of q, k, v, o, numbers of lse), read once."""
+        if self._rows is None:
+            lie = {}
+            for t in "qkvo":
+                shape = (self.N, self.Lk, self.kv_heads, self.D) if t in "kv" else (self.N, self.Lq, self.heads, self.D)
+                row = getattr(self, t + "_row") or shape[2] * shape[3]
+                lie[t] = (shape, (getattr(self, t + "_image") or max(shape[1], 1) * row, row, getattr(self, t + "_head") or shape[3], 1))
+            self._rows = (_kinds().dtypes.get(self.type), lie, self.N * self.heads * self.Lq)
+        return self._rows
+
+
 class _AdamwTensor(C.Structure):
     _fields_ = [("n", C.c_int64), ("d_param", C.c_void_p), ("d_m", C.c_void_p), ("d_v", C.c_void_p), ("d_m_scale", C.c_void_p),
                 ("d_v_scale", C.c_void_p), ("d_copy", C.c_void_p), ("weight_decay", C.c_float), ("lr_scale", C.c_float)]
@@ -71,7 +94,7 @@ EXPORTS = ["qrm_create", "qrm_destroy", "qrm_last_error", "qrm_set_micro_batch",
            "qrm_detect_host", "qrm_plan_streams", "qrm_key_threshold", "qrm_set_key", "qrm_verify_key", "qrm_detect_verify",
            "qrm_profile_enable", "qrm_profile_read", "qrm_profile_read_chunks", "qrm_release_stream", "qrm_detect_static", "qrm_version",
            "qrm_group_norm", "qrm_group_norm_backward", "qrm_adamw_create", "qrm_adamw_destroy", "qrm_adamw_step", "qrm_unpack_moment",
-           "qrm_message_loss"]
+           "qrm_message_loss", "qrm_attention", "qrm_attention_backward", "qrm_adamw_grad_norm", "qrm_adamw_scale_grads"]
 DIAG_EXPORTS = ["qrm_diag_set_flags", "qrm_diag_matrix_rate", "qrm_diag_pair_split",
                 "qrm_diag_wide_schedule", "qrm_diag_last_lines", "qrm_diag_host_plan",
                 "qrm_diag_preprocess_strips", "qrm_diag_rs_lanes", "qrm_diag_chain_patience", "qrm_diag_chain_count",
@@ -81,6 +104,7 @@ QRM_MAX_STREAMS = 8   # include/qrm.h
 QRM_F32, QRM_BF16, QRM_F16 = 0, 1, 2
 QRM_ACT_NONE, QRM_ACT_RELU, QRM_ACT_SILU = 0, 1, 2
 QRM_MOMENT_BLOCK = 256
+QRM_ATTENTION_MAX_D = 512
 ACTIVATIONS = {"none": QRM_ACT_NONE, "relu": QRM_ACT_RELU, "silu": QRM_ACT_SILU}
 QRM_DIAG_NO_FUSED_PAIRS, QRM_DIAG_POISON_WORKSPACE, QRM_DIAG_FUSE_ALWAYS, QRM_DIAG_CHAIN_ALWAYS, QRM_DIAG_NO_CHAIN = 1, 2, 4, 8, 16
 (QRM_PROFILE_PAIR_FIRST, QRM_PROFILE_PAIR_MID, QRM_PROFILE_PAIR_LAST, QRM_PROFILE_BLOCK_FIRST, QRM_PROFILE_BLOCK_MID,
@@ -190,6 +214,14 @@ def load_library():
     lib.qrm_unpack_moment.restype = C.c_int
     lib.qrm_message_loss.argtypes = [vp, vp, vp, i64, i64, i32, C.c_float, vp, vp, vp, vp, vp]
     lib.qrm_message_loss.restype = C.c_int
+    lib.qrm_attention.argtypes = [vp, C.POINTER(_AttentionDesc)] + [vp] * 8
+    lib.qrm_attention.restype = C.c_int
+    lib.qrm_attention_backward.argtypes = [vp, C.POINTER(_AttentionDesc)] + [vp] * 12
+    lib.qrm_attention_backward.restype = C.c_int
+    lib.qrm_adamw_grad_norm.argtypes = [vp, vp, C.POINTER(vp), C.c_double, vp, vp, vp, vp]
+    lib.qrm_adamw_grad_norm.restype = C.c_int
+    lib.qrm_adamw_scale_grads.argtypes = [vp, vp, C.POINTER(vp), vp, C.POINTER(vp), vp]
+    lib.qrm_adamw_scale_grads.restype = C.c_int
     lib.qrm_version.argtypes = []
     lib.qrm_version.restype = C.c_char_p
     _lib = lib
@@ -309,6 +341,39 @@ def group_norm_desc(N: int, P: int, C: int, groups: int, dtype, act: str = "none
     """The qrm_group_norm_desc of maps [N,P,C] of `dtype`; act is "none", "relu" or "silu"; strides in elements, 0 = dense."""
     return _GroupNormDesc(int(N), int(P), int(C), int(groups), type_code(dtype), ACTIVATIONS[act], float(eps), int(x_pixel),
                           int(x_image), int(y_pixel), int(y_image))
+
+
+def _dptr_rows(t, dtype, lie) -> Optional[int]:
+    """Device pointer of rows [N,L,heads,D] that lie as their descriptor says (or None); a buffer of another shape has to be contiguous, as the rows."""
+    if t is None:
+        return None
+    shape, strides = lie
+    if t.dtype is dtype and t.is_cuda and t.shape == shape and t.stride() == strides:
+        return t.data_ptr()
+    assert t.is_cuda, "device tensors must be on the GPU"
+    # (a dtype of None, sizes below one: a descriptor that is refused, or nothing to read)
+    assert t.dtype is dtype or dtype is None, "a tensor has another type than its descriptor"
+    if min(shape) >= 1:
+        want = [(n, s) for n, s in zip(shape, strides) if n > 1]
+        if t.shape == shape:
+            assert [(n, s) for n, s in zip(t.shape, t.stride()) if n > 1] == want, "a tensor has other strides than its descriptor"
+        else:
+            dense, n = [], 1
+            for size in reversed(shape):
+                dense.append(n)
+                n *= size
+            assert t.is_contiguous() and t.numel() >= n and want == [(size, s) for size, s in zip(shape, reversed(dense)) if size > 1], \
+                "a tensor has another size or strides than its descriptor"
+    return t.data_ptr()
+
+
+def attention_desc(N: int, Lq: int, Lk: int, heads: int, kv_heads: int, D: int, dtype, causal: bool = False, scale: Optional[float] = None,
+                   q=(0, 0, 0), k=(0, 0, 0), v=(0, 0, 0), o=(0, 0, 0)):
+    """The qrm_attention_desc of queries [N,Lq,heads,D] and keys [N,Lk,kv_heads,D] of `dtype`; scale None is 1 / sqrt(D); q, k, v, o are the strides of
+    neighbouring rows, heads and images in elements, 0 = dense."""
+    scale = D ** -0.5 if scale is None and D > 0 else 1.0 if scale is None else scale
+    return _AttentionDesc(int(N), int(Lq), int(Lk), int(heads), int(kv_heads), int(D), type_code(dtype), int(causal), float(scale),
+                          *[int(x) for lie in (q, k, v, o) for x in lie])
 
 
 def _hptr(t) -> Optional[int]:
@@ -522,6 +587,21 @@ class Context:
                                                       _dptr_of(d_rstd, f32, stats), _dptr_map(d_dx, dtype, shape, x), _dptr_of(d_dgamma, f32, C_),
                                                       _dptr_of(d_dbeta, f32, C_), _stream_handle(stream)))
 
+    def qrm_attention(self, desc, d_q, d_k, d_v, d_o, d_lse=None, d_q_len=None, d_k_len=None, stream=None):
+        dtype, lie, sums = desc.rows()
+        k, N = _kinds(), desc.N
+        self._check(self._lib.qrm_attention(self._h, C.byref(desc), _dptr_rows(d_q, dtype, lie["q"]), _dptr_rows(d_k, dtype, lie["k"]),
+                                            _dptr_rows(d_v, dtype, lie["v"]), _dptr_of(d_q_len, k.i32, N), _dptr_of(d_k_len, k.i32, N),
+                                            _dptr_rows(d_o, dtype, lie["o"]), _dptr_of(d_lse, k.f32, sums), _stream_handle(stream)))
+
+    def qrm_attention_backward(self, desc, d_q, d_k, d_v, d_o, d_do, d_lse, d_dq, d_dk=None, d_dv=None, d_q_len=None, d_k_len=None, stream=None):
+        dtype, lie, sums = desc.rows()
+        k, N = _kinds(), desc.N
+        rows = lambda t, name: _dptr_rows(t, dtype, lie[name])
+        self._check(self._lib.qrm_attention_backward(self._h, C.byref(desc), rows(d_q, "q"), rows(d_k, "k"), rows(d_v, "v"), rows(d_o, "o"), rows(d_do, "o"),
+                                                     _dptr_of(d_lse, k.f32, sums), _dptr_of(d_q_len, k.i32, N), _dptr_of(d_k_len, k.i32, N),
+                                                     rows(d_dq, "q"), rows(d_dk, "k"), rows(d_dv, "v"), _stream_handle(stream)))
+
     def qrm_unpack_moment(self, moment: int, d_codes, d_scales, n, d_out, stream=None):
         n = int(n)
         code = type_code(d_out.dtype)
@@ -581,14 +661,29 @@ class AdamW:
     def _mixed(what):
         raise ValueError(f"all {what} of a plan have one type")
 
-    def qrm_adamw_step(self, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
-                       d_grad_scale=None, stream=None):
-        """grads: one device tensor of grad_type for each tensor of the plan, or None where it has no gradient."""
+    def _pointers(self, grads):
         assert len(grads) == self._n, "one gradient (or None) for each tensor"
         t = self._grad_type
         assert all([g is None or (g.dtype is t and g.numel() == n and g.is_cuda and g.is_contiguous()) for g, n in zip(grads, self._sizes)]), \
             "gradients must have the plan's type and sizes, be contiguous and on the GPU"
-        ptrs = self._array(*[None if g is None else g.data_ptr() for g in grads])
+        return self._array(*[None if g is None else g.data_ptr() for g in grads])
+
+    def qrm_adamw_grad_norm(self, grads, max_norm: float, d_norm, d_scale, d_unscale=None, stream=None):
+        """grads as in qrm_adamw_step; d_norm, d_scale, d_unscale: f32 [1] on the device (or None)."""
+        f32 = _kinds().f32
+        self._ctx._check(self._lib.qrm_adamw_grad_norm(self._ctx._h, self._h, self._pointers(grads), float(max_norm), _dptr_of(d_unscale, f32, 1),
+                                                       _dptr_of(d_norm, f32, 1), _dptr_of(d_scale, f32, 1), _stream_handle(stream)))
+
+    def qrm_adamw_scale_grads(self, grads, d_scale, outs=None, stream=None):
+        """outs: a tensor for each gradient, or None: in place."""
+        ptrs = self._pointers(grads)
+        self._ctx._check(self._lib.qrm_adamw_scale_grads(self._ctx._h, self._h, ptrs, _dptr_of(d_scale, _kinds().f32, 1),
+                                                         ptrs if outs is None else self._pointers(outs), _stream_handle(stream)))
+
+    def qrm_adamw_step(self, grads, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                       d_grad_scale=None, stream=None):
+        """grads: one device tensor of grad_type for each tensor of the plan, or None where it has no gradient."""
+        ptrs = self._pointers(grads)
         self._ctx._check(self._lib.qrm_adamw_step(self._ctx._h, self._h, ptrs, int(step), float(lr), float(beta1), float(beta2),
                                                   float(eps), _dptr_of(d_grad_scale, _kinds().f32, 1), _stream_handle(stream)))
 

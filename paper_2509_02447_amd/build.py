@@ -12,8 +12,9 @@ LIB = os.path.join(HERE, "libqrm.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["qrm_api.hip", "extractor.hip", "rs_decode.hip", "tiles.hip", "qrm_noalloc.hip", "qrm_diag.hip", "qrm_plan.hip",
            "qrm_train.hip", "group_norm.hip", "group_norm_f32.hip", "group_norm_bf16.hip",
-           "group_norm_f16.hip", "adamw.hip", "message_loss.hip"]
-HEADERS = ["qrm_internal.h", "qrm_ctx.h", "rs_lane.h", "qrm_train.h", "group_norm.h", os.path.join("..", "..", "include", "qrm.h"),
+           "group_norm_f16.hip", "attention.hip", "attention_f32.hip", "attention_bf16.hip", "attention_f16.hip", "adamw.hip",
+           "grad_norm.hip", "message_loss.hip"]
+HEADERS = ["qrm_internal.h", "qrm_ctx.h", "rs_lane.h", "qrm_train.h", "group_norm.h", "attention.h", os.path.join("..", "..", "include", "qrm.h"),
            os.path.join("..", "..", "include", "qrm_diag.h")]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -1,0 +1,639 @@
+// Attention over the rows of a map, forward and backward (qrm_attention, qrm_attention_backward): kernels, for one element type a source file.
+//
+// A column of matrix products belongs to a lane.  A wavefront holds M query rows (backward for keys: M key rows) as columns and walks down the other side's
+// rows in tiles that lie in LDS as they lie in memory.  Scores are computed with those rows as the products' rows, so that a lane has the scores of its
+// own column: maxima and sums stay in the lane but for one or two lane exchanges, and the scores go back into the next product as its column operand
+// without leaving their registers: the order of the summed index is the same on both sides, whichever it is (kappa below).  The other operand of that
+// product is the tile again, transposed by the LDS read.
+//
+// Heads that share keys: query rows are counted (position, head of the group), so a tile of keys is read once for all of them; gradients of shared keys
+// are summed over the group inside one workgroup.  No atomics anywhere: the backward pass computes the scores twice, once with queries as columns for dq
+// and once with keys as columns for dk and dv.
+#pragma once
+
+#include "qrm_train.h"
+
+namespace qrm {
+
+typedef __attribute__((address_space(3))) uint8_t *lds_t;
+
+// Products of M x 8 NG by 8 NG x M: `a` has row lane % M, `b` column lane % M, both elements 8 g + j of the summed index, g = lane / M.  The result's
+// column is lane % M, its rows those of row_of.
+template <typename T, int M> struct Mma {
+    static constexpr int NG = 64 / M, KK = 8 * NG, C = M * M / 64;
+    typedef T frag __attribute__((ext_vector_type(8)));
+    typedef float acc __attribute__((ext_vector_type(C)));
+    static __device__ __forceinline__ acc mul(frag a, frag b, acc c)
+    {
+        if constexpr (std::is_same<T, bf16_t>::value) {
+            if constexpr (M == 32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+            else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+        } else if constexpr (std::is_same<T, f16_t>::value) {
+            if constexpr (M == 32) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+            else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { // (any order of the summed index will do, as long as both sides have it)
+                if constexpr (M == 32) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+                else c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+            }
+            return c;
+        }
+    }
+    // Row of a lane's r-th result where blocks of M rows lie one below the other; also the summed index of element r % 8 of the r / 8 -th column operand
+    // that is made of them.
+    static __device__ __forceinline__ int row_of(int r, int g) { return r / 4 * (4 * NG) + 4 * g + r % 4; }
+};
+
+// A wavefront's load of 64 times 16 (4) bytes, at off (per lane) of the resource, to `to` and what follows.  In asm, so that the compiler, which cannot tell
+// the tiles apart, does not wait for the next one before every read of this one; whoever reads waits (wait_loads) and passes a barrier.
+__device__ __forceinline__ void load_to_lds16(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, uint8_t *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)(lds_t)to), "v"(off), "s"(rsrc) : "m0", "memory");
+}
+__device__ __forceinline__ void load_to_lds4(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, uint8_t *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)(lds_t)to), "v"(off), "s"(rsrc) : "m0", "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// .. of the loads that the compiler knows: said once before a loop, it does not wait for them inside, and for what is under way there.
+__device__ __forceinline__ void wait_known_loads() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
+
+// A tile in LDS: rows of PB bytes, a power of two, whose pieces of 16 bytes are swapped about within the row (swizzle) so that neither the reads of one
+// piece of 16 neighbouring rows nor those of 4 rows by 4 pieces meet in one of the 64 banks.
+template <typename T, int DP> struct Tile {
+    static constexpr int bytes_of(int n) { return n <= 128 ? 128 : n <= 256 ? 256 : n <= 512 ? 512 : n <= 1024 ? 1024 : 2048; }
+    static constexpr int PB = bytes_of(DP * (int)sizeof(T)), E = 16 / (int)sizeof(T), PIECES = PB / 16;
+    static __device__ __forceinline__ int swizzle(int row) { return PB == 128 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3); }
+
+    // Rows 0 .. ROWS-1 of `src` (row_bytes apart, `rows` of them there, D elements each) on their way into the tile; what is not there becomes zeros.
+    // WAVES * 64 threads; everything lies on 16 bytes.
+    template <int ROWS, int WAVES>
+    static __device__ __forceinline__ void load(const uint8_t *src, int row_bytes, int rows, int D, uint8_t *tile, int tid, int wave)
+    {
+        constexpr int COUNT = ROWS * PIECES;
+        static_assert(COUNT % (WAVES * 64) == 0, "whole wavefronts load a tile");
+        rows = max(0, min(rows, ROWS));
+        const int bytes = rows ? (rows - 1) * row_bytes + D * (int)sizeof(T) : 0;
+        __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(src), 0, bytes, 0x00020000);
+#pragma unroll
+        for (int k = 0; k < COUNT / (WAVES * 64); ++k) {
+            const int at = k * (WAVES * 64) + tid, row = at / PIECES, piece = (at % PIECES) ^ swizzle(row);
+            const uint32_t off = piece * E < D ? (uint32_t)(row * row_bytes + piece * 16) : 0x80000000u;
+            load_to_lds16(rsrc, off, tile + (k * (WAVES * 64) + wave * 64) * 16);
+        }
+    }
+
+    // Row operand of a product that sums over the row's elements: tile row `row`, whose swizzle is that of row % 16 (blocks of 16 rows and more).
+    template <int M> static __device__ __forceinline__ typename Mma<T, M>::frag along(const uint8_t *tile, int row, int step, int g)
+    {
+        typedef typename Mma<T, M>::frag frag;
+        const int sw = swizzle(row);
+        if constexpr (sizeof(T) == 2) {
+            return *(const frag *)(tile + row * PB + (((step * Mma<T, M>::NG + g) ^ sw) << 4));
+        } else {
+            const int piece = 2 * (step * Mma<T, M>::NG + g);
+            const f32x4 lo = *(const f32x4 *)(tile + row * PB + ((piece ^ sw) << 4)), hi = *(const f32x4 *)(tile + row * PB + (((piece + 1) ^ sw) << 4));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+
+    // Row operand of a product that sums over the tile's rows: its rows are elements d0 .. d0 + M - 1, element j of the summed index tile row
+    // first + row_of(j, g).
+    template <int M> static __device__ __forceinline__ typename Mma<T, M>::frag across(const uint8_t *tile, int first, int d0, int lane)
+    {
+        typedef Mma<T, M> X;
+        typedef typename X::frag frag;
+        const int g = lane / M;
+        if constexpr (sizeof(T) == 2) {
+            typedef short v4 __attribute__((ext_vector_type(4)));
+            typedef short v8 __attribute__((ext_vector_type(8)));
+            v4 part[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) { // 16 lanes read 4 rows of 16 elements and hold 16 columns of 4
+                const int row = first + u * 4 * X::NG + 4 * g + lane % 16 / 4, piece = d0 / 8 + lane % M / 16 * 2 + lane % 4 / 2;
+                part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)(tile + row * PB + ((piece ^ swizzle(row)) << 4) + lane % 2 * 8));
+            }
+            return __builtin_bit_cast(frag, (v8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int d = d0 + lane % M;
+            frag f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int row = first + X::row_of(j, g);
+                f[j] = *(const float *)(tile + row * PB + (((d / 4) ^ swizzle(row)) << 4) + d % 4 * 4);
+            }
+            return f;
+        }
+    }
+};
+
+// Eight elements of a row in memory from d on, zeros behind its end.
+template <typename T> __device__ __forceinline__ auto row_piece(const T *row, bool there, int d, int D)
+{
+    typedef T frag __attribute__((ext_vector_type(8)));
+    constexpr int E = 16 / (int)sizeof(T);
+    frag f = {};
+#pragma unroll
+    for (int h = 0; h < 8 / E; ++h)
+        if (there && d + h * E < D) {
+            const Pack<T, E> v = load_pack<T, E>(row + d + h * E);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[h * E + e] = v.e[e];
+        }
+    return f;
+}
+
+// Four results of a row, from element d on.
+template <typename T> __device__ __forceinline__ void store_four(T *row, int d, int D, float a, float b, float c, float e)
+{
+    if (d < D) store_pack<T, 4>(row + d, Pack<T, 4>{{(T)a, (T)b, (T)c, (T)e}});
+}
+
+// The barrier leaves loads into the other tile under way: it waits for lgkmcnt alone.
+constexpr int kAttnWaitLds = 15 | (3 << 14) | (7 << 4);
+__device__ __forceinline__ void attn_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kAttnWaitLds);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Largest and sum over the lanes of a column.
+template <int M> __device__ __forceinline__ float column_max(float v)
+{
+    if (M == 16) v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+template <int M> __device__ __forceinline__ float column_sum(float v)
+{
+    if (M == 16) v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// Where a workgroup is: workgroups of a group of heads that share keys follow each other, on one die where there are groups enough (their keys stay in
+// its cache).  false: behind the last one.
+struct AttnPlace {
+    int n, kv, part, split; // image, key head, tile of rows, split of the other side
+};
+__device__ __forceinline__ bool attn_place(const AttnArgs &a, int parts, int splits, int b, AttnPlace *p)
+{
+    const int per = parts * splits, groups = a.N * a.kv_heads;
+    if (groups >= 8) b = b % 8 * ((groups * per + 7) / 8) + b / 8;
+    if (b >= groups * per) return false;
+    const int group = b / per, rest = b % per;
+    p->n = group / a.kv_heads;
+    p->kv = group % a.kv_heads;
+    p->part = rest / splits;
+    p->split = rest % splits;
+    return true;
+}
+
+__device__ __forceinline__ int attn_length(const int32_t *lens, int n, int all) { return lens ? max(0, min(lens[n], all)) : all; }
+
+// ---------------------------------------------------------------- forward
+
+// Columns: query rows (position, head of the group).  Walks over the keys with a running maximum; the results are scaled down when it has grown by more
+// than 2^8, so that most tiles leave them alone.  Sums and results in 32 bits; probabilities are rounded to the type for the second product (16-bit types:
+// half a step relative to each, unsystematic, which is what the output's own rounding is).
+template <typename T, int DP, int M, int WAVES, int TK, int NBUF, int OCC>
+__global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
+{
+    typedef Mma<T, M> X;
+    typedef Tile<T, DP> L;
+    constexpr int R = TK / X::NG; // scores of a lane
+    __shared__ alignas(16) uint8_t lds[NBUF * 2 * TK * L::PB];
+    AttnPlace at;
+    if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
+    if (a.causal) at.part = a.parts - 1 - at.part; // (the longest first)
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
+    const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
+    const int row0 = (at.part * WAVES + wave) * M, rows = a.Lq * a.group;
+    const int row = row0 + col, pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
+    const bool here = row < rows, there = here && pos < q_len;
+    const int seen = there ? (a.causal ? max(0, min(k_len, pos + off + 1)) : k_len) : 0; // keys that the column sees
+    // .. and the most and the least in the wavefront, the most in the workgroup
+    auto last_seen = [&](int last_row) { const int p = min(last_row, rows - 1) / a.group; return a.causal ? max(0, min(k_len, min(p, q_len - 1) + off + 1)) : k_len; };
+    const bool any = row0 < rows && row0 / a.group < q_len;
+    const int most = any ? last_seen(row0 + M - 1) : 0;
+    const int least = row0 + M <= rows && (row0 + M - 1) / a.group < q_len ? (a.causal ? max(0, min(k_len, row0 / a.group + off + 1)) : k_len) : 0;
+    const int base = at.part * WAVES * M;
+    const int all = base / a.group < q_len ? last_seen(base + WAVES * M - 1) : 0;
+    const int tiles = (all + TK - 1) / TK, from = (int)((int64_t)tiles * at.split / a.splits), to = (int)((int64_t)tiles * (at.split + 1) / a.splits);
+
+    const uint8_t *const k = (const uint8_t *)a.k + (at.n * a.k_image + at.kv * a.k_head) * (int64_t)sizeof(T);
+    const uint8_t *const v = (const uint8_t *)a.v + (at.n * a.v_image + at.kv * a.v_head) * (int64_t)sizeof(T);
+    const int k_bytes = (int)a.k_row * (int)sizeof(T), v_bytes = (int)a.v_row * (int)sizeof(T);
+    auto load = [&](int t) {
+        uint8_t *const tile = lds + (t - from) % NBUF * (2 * TK * L::PB);
+        const int first = t * TK;
+        L::template load<TK, WAVES>(k + (int64_t)first * k_bytes, k_bytes, k_len - first, a.D, tile, tid, wave);
+        L::template load<TK, WAVES>(v + (int64_t)first * v_bytes, v_bytes, k_len - first, a.D, tile + TK * L::PB, tid, wave);
+    };
+    if (from < to) load(from);
+
+    typename X::frag q[DP / X::KK];
+    const T *const q_row = (const T *)a.q + at.n * a.q_image + pos * a.q_row + head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < DP / X::KK; ++s) q[s] = row_piece<T>(q_row, there, s * X::KK + 8 * g, a.D);
+
+    typename X::acc o[DP / M] = {};
+    wait_known_loads();
+    float top = -INFINITY, sum = 0.f; // of the raw scores; of this lane's probabilities
+    const float c = a.scale * kLog2E;
+    for (int t = from; t < to; ++t) {
+        wait_loads();
+        attn_barrier();
+        if (NBUF > 1 && t + 1 < to) load(t + 1);
+        const uint8_t *const kt = lds + (t - from) % NBUF * (2 * TK * L::PB), *const vt = kt + TK * L::PB;
+        const int first = t * TK;
+        if (first < most) {
+            typename X::acc s[TK / M];
+#pragma unroll
+            for (int b = 0; b < TK / M; ++b) {
+                s[b] = typename X::acc{};
+#pragma unroll
+                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(kt, b * M + col, i, g), q[i], s[b]);
+            }
+            auto score = [&](int r) -> float { return s[r / X::C][r % X::C]; };
+            if (first + TK > least) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (first + X::row_of(r, g) >= seen) s[r / X::C][r % X::C] = -INFINITY;
+            }
+            float high = score(0);
+#pragma unroll
+            for (int r = 1; r < R; ++r) high = fmaxf(high, score(r));
+            high = column_max<M>(high);
+            if (__any(high * c > top * c + 8.f)) {
+                const float now = fmaxf(top, high);
+                const float less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - now) * c);
+                top = now;
+                sum *= less;
+#pragma unroll
+                for (int d = 0; d < DP / M; ++d) o[d] *= less;
+            }
+            const float about = top == -INFINITY ? 0.f : top * c;
+            typename X::frag p[TK / X::KK];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score(r), c, -about));
+                sum += e;
+                p[r / 8][r % 8] = (T)e;
+            }
+#pragma unroll
+            for (int u = 0; u < TK / X::KK; ++u)
+#pragma unroll
+                for (int d = 0; d < DP / M; ++d) o[d] = X::mul(L::template across<M>(vt, u * X::KK, d * M, lane), p[u], o[d]);
+        }
+        if (NBUF == 1 && t + 1 < to) {
+            attn_barrier();
+            load(t + 1);
+        }
+    }
+    sum = column_sum<M>(sum);
+    if (!here) return;
+    const float about = top == -INFINITY ? 0.f : top * c;
+    const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
+    if (a.splits > 1) { // parts of a row: results and their sum about 2^about
+        const int64_t all_rows = (int64_t)a.N * a.heads * a.Lq;
+        float *const part = a.part + (at.split * all_rows + index) * a.D;
+        if (g == 0) ((float2 *)a.part_sums)[at.split * all_rows + index] = make_float2(sum > 0.f || sum != sum ? about : -INFINITY, sum);
+#pragma unroll
+        for (int d = 0; d < DP / M; ++d)
+#pragma unroll
+            for (int r = 0; r < X::C; r += 4) store_four<float>(part, d * M + X::row_of(r, g), a.D, o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+        return;
+    }
+    if (g == 0 && a.lse) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
+#pragma unroll
+    for (int d = 0; d < DP / M; ++d)
+#pragma unroll
+        for (int r = 0; r < X::C; r += 4)
+            store_four<T>(o_row, d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+}
+
+// ---------------------------------------------------------------- backward
+
+// f16 numbers reach from 2^-24 to 2^16 only.  A column's numbers are multiplied by a power of two that brings the largest so far to 2^14 .. 2^15 before
+// they are rounded; when a larger one comes, what has been summed is scaled down with the factor.  (bf16 and f32 need none.)  Probabilities, which are
+// not above one, are multiplied by 2^14.
+template <typename T> struct Lift {
+    static constexpr bool USED = std::is_same<T, f16_t>::value;
+    static constexpr float PROBABILITY = USED ? 0x1p14f : 1.f;
+    float by = USED ? 0x1p100f : 1.f;
+    __device__ __forceinline__ bool over(float high) const { return high * by > 0x1p15f; }
+    // For numbers of a column whose largest magnitude is `high`; returns what to multiply the column's sums by.
+    __device__ __forceinline__ float fit(float high)
+    {
+        if (!over(high)) return 1.f;
+        const float now = __builtin_ldexpf(1.f, 14 + 127 - (int)(__float_as_uint(high) >> 23)), less = now / by;
+        by = now;
+        return less;
+    }
+};
+
+// Columns: query rows, as above.  dq = scale sum over keys of dS k, dS = P (do v - delta), P = exp(score - lse).
+template <typename T, int DP, int M, int WAVES, int TK, int NBUF, int OCC>
+__global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs a)
+{
+    typedef Mma<T, M> X;
+    typedef Tile<T, DP> L;
+    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG; // keys at a time
+    __shared__ alignas(16) uint8_t lds[NBUF * 2 * TK * L::PB];
+    AttnPlace at;
+    if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
+    if (a.causal) at.part = a.parts - 1 - at.part;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
+    const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
+    const int row0 = (at.part * WAVES + wave) * M, rows = a.Lq * a.group;
+    const int row = row0 + col, pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
+    const bool here = row < rows, there = here && pos < q_len;
+    const int seen = there ? (a.causal ? max(0, min(k_len, pos + off + 1)) : k_len) : 0;
+    auto last_seen = [&](int last_row) { const int p = min(last_row, rows - 1) / a.group; return a.causal ? max(0, min(k_len, min(p, q_len - 1) + off + 1)) : k_len; };
+    const bool any = row0 < rows && row0 / a.group < q_len;
+    const int most = any ? last_seen(row0 + M - 1) : 0;
+    const int least = row0 + M <= rows && (row0 + M - 1) / a.group < q_len ? (a.causal ? max(0, min(k_len, row0 / a.group + off + 1)) : k_len) : 0;
+    const int base = at.part * WAVES * M;
+    const int all = base / a.group < q_len ? last_seen(base + WAVES * M - 1) : 0;
+    const int tiles = (all + TK - 1) / TK, from = (int)((int64_t)tiles * at.split / a.splits), to = (int)((int64_t)tiles * (at.split + 1) / a.splits);
+
+    const uint8_t *const k = (const uint8_t *)a.k + (at.n * a.k_image + at.kv * a.k_head) * (int64_t)sizeof(T);
+    const uint8_t *const v = (const uint8_t *)a.v + (at.n * a.v_image + at.kv * a.v_head) * (int64_t)sizeof(T);
+    const int k_bytes = (int)a.k_row * (int)sizeof(T), v_bytes = (int)a.v_row * (int)sizeof(T);
+    auto load = [&](int t) {
+        uint8_t *const tile = lds + (t - from) % NBUF * (2 * TK * L::PB);
+        const int first = t * TK;
+        L::template load<TK, WAVES>(k + (int64_t)first * k_bytes, k_bytes, k_len - first, a.D, tile, tid, wave);
+        L::template load<TK, WAVES>(v + (int64_t)first * v_bytes, v_bytes, k_len - first, a.D, tile + TK * L::PB, tid, wave);
+    };
+    if (from < to) load(from);
+
+    typename X::frag q[DP / X::KK], dy[DP / X::KK];
+    const T *const q_row = (const T *)a.q + at.n * a.q_image + pos * a.q_row + head * a.q_head;
+    const T *const dy_row = (const T *)a.dy + at.n * a.o_image + pos * a.o_row + head * a.o_head;
+#pragma unroll
+    for (int s = 0; s < DP / X::KK; ++s) {
+        q[s] = row_piece<T>(q_row, there, s * X::KK + 8 * g, a.D);
+        dy[s] = row_piece<T>(dy_row, there, s * X::KK + 8 * g, a.D);
+    }
+    const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
+    const float about = there ? a.row_lse[index] : INFINITY, delta = there ? a.row_delta[index] : 0.f;
+
+    wait_known_loads();
+    typename X::acc dq[DP / M] = {};
+    Lift<T> lift;
+    const float c = a.scale * kLog2E;
+    for (int t = from; t < to; ++t) {
+        wait_loads();
+        attn_barrier();
+        if (NBUF > 1 && t + 1 < to) load(t + 1);
+        const uint8_t *const kt = lds + (t - from) % NBUF * (2 * TK * L::PB), *const vt = kt + TK * L::PB;
+#pragma unroll
+        for (int h = 0; h < TK; h += STEP) {
+            const int first = t * TK + h;
+            if (first >= most) break;
+            typename X::acc s[BLOCKS], dp[BLOCKS];
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                s[b] = dp[b] = typename X::acc{};
+#pragma unroll
+                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(kt, h + b * M + col, i, g), q[i], s[b]);
+#pragma unroll
+                for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(vt, h + b * M + col, i, g), dy[i], dp[b]);
+            }
+            float ds[R], high = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / X::C][r % X::C], c, -about)) * (dp[r / X::C][r % X::C] - delta);
+            if (first + STEP > least) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) ds[r] = first + X::row_of(r, g) < seen ? ds[r] : 0.f;
+            }
+            if constexpr (Lift<T>::USED) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) high = fmaxf(high, fabsf(ds[r]));
+                high = column_max<M>(high);
+                if (__any(lift.over(high))) {
+                    const float less = lift.fit(high);
+#pragma unroll
+                    for (int d = 0; d < DP / M; ++d) dq[d] *= less;
+                }
+            }
+            typename X::frag p[STEP / X::KK];
+#pragma unroll
+            for (int r = 0; r < R; ++r) p[r / 8][r % 8] = (T)(Lift<T>::USED ? ds[r] * lift.by : ds[r]);
+#pragma unroll
+            for (int u = 0; u < STEP / X::KK; ++u)
+#pragma unroll
+                for (int d = 0; d < DP / M; ++d) dq[d] = X::mul(L::template across<M>(kt, h + u * X::KK, d * M, lane), p[u], dq[d]);
+        }
+        if (NBUF == 1 && t + 1 < to) {
+            attn_barrier();
+            load(t + 1);
+        }
+    }
+    if (!here) return;
+    const float by = a.scale / lift.by;
+    float *const part = a.splits > 1 ? a.part + (at.split * ((int64_t)a.N * a.heads * a.Lq) + index) * a.D : nullptr;
+    T *const out = (T *)a.dq + at.n * a.q_image + pos * a.q_row + head * a.q_head;
+#pragma unroll
+    for (int d = 0; d < DP / M; ++d)
+#pragma unroll
+        for (int r = 0; r < X::C; r += 4) {
+            const float w[4] = {dq[d][r] * by, dq[d][r + 1] * by, dq[d][r + 2] * by, dq[d][r + 3] * by};
+            if (part) store_four<float>(part, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+            else store_four<T>(out, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+        }
+}
+
+// Columns: key rows.  dv = sum over queries of P do, dk = scale sum of dS q, over all heads that share the keys.  DK, DV: which of the two (both where the
+// registers hold both).
+template <typename T, int DP, int M, int WAVES, int TQ, int NBUF, int OCC, bool DK, bool DV>
+__global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs a)
+{
+    typedef Mma<T, M> X;
+    typedef Tile<T, DP> L;
+    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG;
+    constexpr int BUF = 2 * TQ * L::PB + 512; // queries, gradients, 64 log-sums, 64 deltas
+    static_assert(TQ <= 64, "a wavefront loads a tile's log-sums at once");
+    __shared__ alignas(16) uint8_t lds[NBUF * BUF];
+    AttnPlace at;
+    if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
+    const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
+    const int base = at.part * WAVES * M, key0 = base + wave * M, key = key0 + col;
+    const bool here = key < a.Lk, there = key < k_len;
+    // tiles of a head's queries that see any of the workgroup's keys; all heads' one after the other
+    const int skip = a.causal ? max(0, base - off) / TQ : 0, each = base < k_len ? max(0, (q_len + TQ - 1) / TQ - skip) : 0;
+    const int tiles = each * a.group, from = (int)((int64_t)tiles * at.split / a.splits), to = (int)((int64_t)tiles * (at.split + 1) / a.splits);
+
+    const int q_bytes = (int)a.q_row * (int)sizeof(T), y_bytes = (int)a.o_row * (int)sizeof(T);
+    auto load = [&](int t) {
+        uint8_t *const tile = lds + (t - from) % NBUF * BUF;
+        const int h = t / each, first = (skip + t - h * each) * TQ, head = at.kv * a.group + h;
+        const uint8_t *const q = (const uint8_t *)a.q + (at.n * a.q_image + head * a.q_head + (int64_t)first * a.q_row) * (int64_t)sizeof(T);
+        const uint8_t *const y = (const uint8_t *)a.dy + (at.n * a.o_image + head * a.o_head + (int64_t)first * a.o_row) * (int64_t)sizeof(T);
+        L::template load<TQ, WAVES>(q, q_bytes, q_len - first, a.D, tile, tid, wave);
+        L::template load<TQ, WAVES>(y, y_bytes, q_len - first, a.D, tile + TQ * L::PB, tid, wave);
+        const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + first;
+        if (wave == 0) {
+            const int bytes = min(64, q_len - first) * 4;
+            __amdgpu_buffer_rsrc_t l = __builtin_amdgcn_make_buffer_rsrc((void *)(a.row_lse + index), 0, bytes, 0x00020000);
+            __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc((void *)(a.row_delta + index), 0, bytes, 0x00020000);
+            load_to_lds4(l, lane * 4, tile + 2 * TQ * L::PB);
+            load_to_lds4(d, lane * 4, tile + 2 * TQ * L::PB + 256);
+        }
+    };
+    if (from < to) load(from);
+
+    typename X::frag k[DP / X::KK], v[DK ? DP / X::KK : 1];
+    const T *const k_row = (const T *)a.k + at.n * a.k_image + key * a.k_row + at.kv * a.k_head;
+    const T *const v_row = (const T *)a.v + at.n * a.v_image + key * a.v_row + at.kv * a.v_head;
+#pragma unroll
+    for (int s = 0; s < DP / X::KK; ++s) {
+        k[s] = row_piece<T>(k_row, there, s * X::KK + 8 * g, a.D);
+        if constexpr (DK) v[s] = row_piece<T>(v_row, there, s * X::KK + 8 * g, a.D);
+    }
+
+    wait_known_loads();
+    typename X::acc dk[DK ? DP / M : 1] = {}, dv[DV ? DP / M : 1] = {};
+    Lift<T> lift;
+    const float c = a.scale * kLog2E;
+    for (int t = from; t < to; ++t) {
+        wait_loads();
+        attn_barrier();
+        if (NBUF > 1 && t + 1 < to) load(t + 1);
+        const uint8_t *const qt = lds + (t - from) % NBUF * BUF, *const yt = qt + TQ * L::PB;
+        const float *const lse = (const float *)(qt + 2 * TQ * L::PB), *const delta = lse + 64;
+        const int pos0 = (skip + t % each) * TQ;
+#pragma unroll
+        for (int h = 0; h < TQ; h += STEP) {
+            if (pos0 + h >= q_len) break;
+            const int behind = a.causal ? key0 - off - (pos0 + h) : 0; // query row r of these sees the wavefront's keys 0 .. r - behind
+            if (behind >= STEP) continue;
+            typename X::acc s[BLOCKS], dp[BLOCKS];
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                s[b] = dp[b] = typename X::acc{};
+#pragma unroll
+                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(qt, h + b * M + col, i, g), k[i], s[b]);
+                if constexpr (DK) {
+#pragma unroll
+                    for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(yt, h + b * M + col, i, g), v[i], dp[b]);
+                }
+            }
+            float pr[R], ds[R];
+#pragma unroll
+            for (int r = 0; r < R; r += 4) {
+                const f32x4 about = *(const f32x4 *)(lse + h + X::row_of(r, g)), mean = *(const f32x4 *)(delta + h + X::row_of(r, g));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    pr[r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[(r + e) / X::C][(r + e) % X::C], c, -about[e]));
+                    ds[r + e] = DK ? pr[r + e] * (dp[(r + e) / X::C][(r + e) % X::C] - mean[e]) : 0.f;
+                }
+            }
+            if (behind > 1 - M && a.causal) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (X::row_of(r, g) - behind < col) pr[r] = ds[r] = 0.f;
+            }
+            if constexpr (Lift<T>::USED && DK) {
+                float high = 0.f;
+#pragma unroll
+                for (int r = 0; r < R; ++r) high = fmaxf(high, fabsf(ds[r]));
+                high = column_max<M>(high);
+                if (__any(lift.over(high))) {
+                    const float less = lift.fit(high);
+#pragma unroll
+                    for (int d = 0; d < DP / M; ++d) dk[d] *= less;
+                }
+            }
+            typename X::frag p[STEP / X::KK], z[STEP / X::KK];
+#pragma unroll
+            for (int r = 0; r < R; ++r) p[r / 8][r % 8] = (T)(Lift<T>::USED ? pr[r] * Lift<T>::PROBABILITY : pr[r]), z[r / 8][r % 8] = (T)(Lift<T>::USED ? ds[r] * lift.by : ds[r]);
+#pragma unroll
+            for (int u = 0; u < STEP / X::KK; ++u)
+#pragma unroll
+                for (int d = 0; d < DP / M; ++d) {
+                    if constexpr (DV) dv[d] = X::mul(L::template across<M>(yt, h + u * X::KK, d * M, lane), p[u], dv[d]);
+                    if constexpr (DK) dk[d] = X::mul(L::template across<M>(qt, h + u * X::KK, d * M, lane), z[u], dk[d]);
+                }
+        }
+        if (NBUF == 1 && t + 1 < to) {
+            attn_barrier();
+            load(t + 1);
+        }
+    }
+    if (!here) return;
+    const float by_k = a.scale / lift.by, by_v = 1.f / Lift<T>::PROBABILITY;
+    auto value = [&](float sum, float by) { return there ? sum * by : 0.f; };
+    const int64_t index = ((int64_t)at.n * a.kv_heads + at.kv) * a.Lk + key, all_rows = (int64_t)a.N * a.kv_heads * a.Lk;
+    auto write = [&](const typename X::acc *sums, float by, T *out, float *part) {
+#pragma unroll
+        for (int d = 0; d < DP / M; ++d)
+#pragma unroll
+            for (int r = 0; r < X::C; r += 4) {
+                const float w[4] = {value(sums[d][r], by), value(sums[d][r + 1], by), value(sums[d][r + 2], by), value(sums[d][r + 3], by)};
+                if (part) store_four<float>(part, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+                else store_four<T>(out, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+            }
+    };
+    const int64_t part_at = (at.split * all_rows + index) * a.D;
+    if constexpr (DK)
+        if (a.dk) write(dk, by_k, (T *)a.dk + at.n * a.k_image + key * a.k_row + at.kv * a.k_head, a.splits > 1 ? a.part_k + part_at : nullptr);
+    if constexpr (DV)
+        if (a.dv) write(dv, by_v, (T *)a.dv + at.n * a.v_image + key * a.v_row + at.kv * a.v_head, a.splits > 1 ? a.part_v + part_at : nullptr);
+}
+
+// ---------------------------------------------------------------- launches
+
+template <typename T, int DP> hipError_t attention_launch_width(int kind, const AttnArgs &a, hipStream_t s)
+{
+    constexpr int size = sizeof(T);
+    const int64_t blocks = (int64_t)a.N * a.kv_heads * a.parts * a.splits;
+    const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
+    switch (kind) {
+    case ATTN_FORWARD: {
+        constexpr AttnShape h = attn_shape(size, DP, ATTN_FORWARD);
+        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
+        break;
+    }
+    case ATTN_FEW: {
+        constexpr AttnShape h = attn_shape(size, DP, ATTN_FEW);
+        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
+        break;
+    }
+    case ATTN_DQ: {
+        constexpr AttnShape h = attn_shape(size, DP, ATTN_DQ);
+        hipLaunchKernelGGL((attention_dq_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
+        break;
+    }
+    default: {
+        constexpr AttnShape h = attn_shape(size, DP, ATTN_DKV);
+        if constexpr (attn_dk_dv_at_once(size, DP)) {
+            hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy, true, true>), grid, dim3(h.waves * 64), 0, s, a);
+        } else {
+            if (a.dk) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy, true, false>), grid, dim3(h.waves * 64), 0, s, a);
+            if (a.dv) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy, false, true>), grid, dim3(h.waves * 64), 0, s, a);
+        }
+    }
+    }
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t attention_launch(int kind, const AttnArgs &a, hipStream_t s)
+{
+    switch (attn_width(a.D)) {
+    case 64: return attention_launch_width<T, 64>(kind, a, s);
+    case 128: return attention_launch_width<T, 128>(kind, a, s);
+    case 256: return attention_launch_width<T, 256>(kind, a, s);
+    default: return attention_launch_width<T, 512>(kind, a, s);
+    }
+}
+
+} // namespace qrm

@@ -164,6 +164,78 @@ hipError_t launch_adamw(const AdamwTypes &t, const AdamwTensor *tensors, const u
                         const void *const *grads, int n_grads, const AdamwStep &step, hipStream_t s);
 hipError_t launch_unpack_moment(int moment, const void *codes, const float *scales, int64_t n, int out_type, void *out, hipStream_t s);
 
+// ---- norm of the gradients
+
+struct NormParts {
+    double *sums;         // of the workgroups of all launches
+    uint32_t *done;       // counters, all zero
+    uint32_t first, total; // this launch's first one, all of them
+    bool ends;            // this is the last launch
+    double max_norm;
+    const float *unscale; // or null
+    float *norm, *scale;  // either may be null
+};
+constexpr int kScaleGrads = kAdamwGrads / 2; // gradients named to one launch that has outputs too
+uint32_t norm_blocks(uint32_t pieces);
+// Pieces and gradients as launch_adamw; no pieces: one workgroup.
+hipError_t launch_grad_norm(int type, const AdamwTensor *tensors, const uint2 *pieces, uint32_t first, uint32_t count, uint32_t t0, const void *const *grads, int n_grads,
+                            const NormParts &parts, hipStream_t s);
+hipError_t launch_scale_grads(int type, const AdamwTensor *tensors, const uint2 *pieces, uint32_t first, uint32_t count, uint32_t t0, const void *const *grads, void *const *outs, int n_grads,
+                              const float *scale, hipStream_t s);
+
+// ---- attention
+
+struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie on 16 bytes and are a multiple of them (launch_attention_copy)
+    const void *q, *k, *v, *dy;
+    void *o, *dq, *dk, *dv;
+    float *lse;                        // [N,heads,Lq]
+    const float *row_lse, *row_delta;  // backward, [N,heads,Lq]: log-sums in powers of two (+inf: the row sees nothing), sums of dy o
+    float *part, *part_sums;           // splits > 1: their results, f32 [splits][rows][D], and forward (power of two, sum) of each row
+    float *part_k, *part_v;
+    const int32_t *q_len, *k_len;      // [N] or null
+    int64_t q_row, q_head, q_image, k_row, k_head, k_image, v_row, v_head, v_image, o_row, o_head, o_image;
+    int N, Lq, Lk, heads, kv_heads, group, D;
+    int parts, splits;                 // of the launch: tiles of the columns' rows, splits of the other side
+    float scale;
+    bool causal;
+};
+// How a kernel cuts its work: M columns to a wavefront (the matrix products' side), wavefronts of a workgroup, rows of the other side in a tile, tiles
+// in LDS, wavefronts to a SIMD that the registers are kept for.
+struct AttnShape {
+    int m, waves, tile, buffers, occupancy;
+    constexpr int rows() const { return m * waves; }
+};
+enum { ATTN_FORWARD, ATTN_FEW, ATTN_DQ, ATTN_DKV }; // ATTN_FEW: forward with few query rows
+constexpr int attn_width(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 256 ? 256 : 512; }
+constexpr AttnShape attn_shape(int size, int width, int kind)
+{
+    const int bytes = size * width;
+    if (kind == ATTN_FEW) return bytes <= 256 ? AttnShape{32, 1, 64, 2, 1} : AttnShape{16, 1, 32, bytes <= 1024 ? 2 : 1, 1};
+    if (kind == ATTN_FORWARD)
+        return bytes <= 256 ? AttnShape{32, 4, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 32, 2, size == 2 ? 1 : 2} : bytes == 1024 ? AttnShape{size == 2 ? 32 : 16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
+    if (kind == ATTN_DQ)
+        return bytes <= 256 ? AttnShape{32, 4, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 32, 2, 1} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
+    return bytes <= 128 ? AttnShape{32, 4, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 32, 2, 1} : bytes == 512 ? AttnShape{32, 4, 32, 2, 1} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
+}
+// The registers hold the sums of dk and dv beside the keys and values, or they are two launches.
+constexpr bool attn_dk_dv_at_once(int size, int width) { return size * width <= 1024; }
+struct AttnRows { // where rows [N,L,heads,D] lie
+    int64_t row, head, image;
+};
+struct AttnCut {
+    int kind, parts, splits;
+};
+// width: D rounded up to 16 bytes.
+AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num_cu);
+hipError_t launch_attention(int type, int kind, const AttnArgs &a, hipStream_t s); // kind ATTN_DKV: dk, dv, whichever is not null
+// Backward, before all else: row_lse and row_delta of lse, o and dy.
+hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, const void *dy, const float *lse, const int32_t *q_len, float *row_lse, float *row_delta, hipStream_t s);
+// Behind launches with splits: the forward's parts into o and lse; the sums of gradient parts [splits][N,heads,L,D] into rows.
+hipError_t launch_attention_join(int type, const AttnArgs &a, hipStream_t s);
+hipError_t launch_attention_add(int type, const float *part, int splits, void *out, const AttnRows &r, int64_t N, int64_t L, int heads, int D, hipStream_t s);
+// Rows of any alignment into rows [N,heads,L,wide] that the kernels take, or (out) back.
+hipError_t launch_attention_copy(int type, bool out, const AttnRows &r, void *there, void *here, int64_t N, int64_t L, int heads, int D, int wide, hipStream_t s);
+
 // ---- message loss
 
 struct LossCall {

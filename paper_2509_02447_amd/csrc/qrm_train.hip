@@ -4,6 +4,7 @@
 #include <math.h>
 #include <stdio.h>
 
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -79,6 +80,126 @@ qrm_status plan(qrm_ctx *c, const qrm_group_norm_desc &d, int align, bool backwa
     auto fits = [&](const NormCut &cut) { return ((double)d.N * cut.tiles * cut.chunks + 8192.0) * cut.threads < 4294967296.0; };
     if (!fits(p->first) || (!p->whole && !fits(p->second))) return fail(c, QRM_E_UNSUPPORTED, "the tiles of all images need 2^32 threads and more");
     return QRM_OK;
+}
+
+// The gradients of a plan's tensors.
+qrm_status check_grads(qrm_ctx *c, const qrm_adamw *o, const void *const *h_grads)
+{
+    const int n = (int)o->first_piece.size() - 1;
+    if (n > 0 && !h_grads) return fail(c, QRM_E_INVALID, "h_grads is NULL");
+    const size_t bytes = type_bytes(o->types.grad);
+    for (int i = 0; i < n; ++i)
+        if (!aligned_to(h_grads[i], bytes)) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
+    return QRM_OK;
+}
+
+// Where a tensor of an attention call lies: dense strides filled in; rows overlap nowhere.
+qrm_status check_rows(qrm_ctx *c, AttnRows *r, int64_t N, int64_t L, int heads, int D)
+{
+    constexpr int64_t far = (int64_t)1 << 46; // (addresses stay in 64 bits)
+    if (!r->head) r->head = D;
+    if (!r->row) r->row = (int64_t)heads * D;
+    if (!r->image) r->image = std::max<int64_t>(L, 1) * r->row;
+    if (L <= 1) r->row = D; // (there is no next one)
+    if (heads <= 1) r->head = D;
+    if (N <= 1) r->image = D;
+    std::pair<int64_t, int64_t> dims[3] = {{r->row, L}, {r->head, heads}, {r->image, N}};
+    std::sort(dims, dims + 3);
+    int64_t extent = D;
+    for (auto &d : dims) {
+        if (d.second <= 1) continue;
+        if (d.first < extent) return fail(c, QRM_E_INVALID, "rows, heads or images overlap: a stride is too short");
+        if (d.first > far / d.second) return fail(c, QRM_E_INVALID, "a stride is out of range");
+        extent += d.first * (d.second - 1);
+    }
+    return QRM_OK;
+}
+
+struct AttnCheck {
+    qrm_attention_desc d; // strides filled in
+    AttnRows q, k, v, o;
+    int wide;             // D rounded up to 16 bytes
+};
+
+qrm_status check_attention(qrm_ctx *c, const qrm_attention_desc *desc, AttnCheck *out)
+{
+    if (!desc) return fail(c, QRM_E_INVALID, "desc is NULL");
+    qrm_attention_desc &d = out->d = *desc;
+    if (d.N < 0 || d.Lq < 0 || d.Lk < 0) return fail(c, QRM_E_INVALID, "N, Lq and Lk must not be negative");
+    if (d.heads < 1 || d.kv_heads < 1 || d.heads % d.kv_heads) return fail(c, QRM_E_INVALID, "kv_heads must divide heads");
+    if (d.D < 1) return fail(c, QRM_E_INVALID, "D < 1");
+    if (!known_type(d.type)) return fail(c, QRM_E_INVALID, "unknown type");
+    if (d.causal != 0 && d.causal != 1) return fail(c, QRM_E_INVALID, "causal is 0 or 1");
+    if (!(d.scale > 0.f) || !std::isfinite(d.scale)) return fail(c, QRM_E_INVALID, "scale must be above zero");
+    constexpr int64_t most = (int64_t)1 << 30;
+    if (d.D > QRM_ATTENTION_MAX_D) return fail(c, QRM_E_UNSUPPORTED, "D above 512");
+    if (d.N > most || d.Lq > most || d.Lk > most || d.Lq * d.heads > most) return fail(c, QRM_E_UNSUPPORTED, "N, Lk, or query rows of all heads of an image above 2^30");
+    if (d.N * d.heads > most / 128) return fail(c, QRM_E_UNSUPPORTED, "heads of all images above 2^23");
+    // (a launch has less than 2^32 threads; a thread has at least four elements, a workgroup of 64 sixteen rows and more)
+    const double rows = (double)d.N * std::max((double)d.Lq * d.heads, (double)d.Lk * d.kv_heads);
+    if (rows * ((d.D + 7) / 4) >= 4294967296.0 || rows * 16 >= 4294967296.0) return fail(c, QRM_E_UNSUPPORTED, "the rows of all images need 2^32 threads and more");
+    const int size = type_bytes(d.type), e = 16 / size;
+    out->wide = (d.D + e - 1) / e * e;
+    out->q = {d.q_row, d.q_head, d.q_image};
+    out->k = {d.k_row, d.k_head, d.k_image};
+    out->v = {d.v_row, d.v_head, d.v_image};
+    out->o = {d.o_row, d.o_head, d.o_image};
+    qrm_status st;
+    for (AttnRows *r : {&out->q, &out->o})
+        if ((st = check_rows(c, r, d.N, d.Lq, d.heads, d.D)) != QRM_OK) return st;
+    for (AttnRows *r : {&out->k, &out->v})
+        if ((st = check_rows(c, r, d.N, d.Lk, d.kv_heads, d.D)) != QRM_OK) return st;
+    d.q_row = out->q.row, d.q_head = out->q.head, d.q_image = out->q.image;
+    d.k_row = out->k.row, d.k_head = out->k.head, d.k_image = out->k.image;
+    d.v_row = out->v.row, d.v_head = out->v.head, d.v_image = out->v.image;
+    d.o_row = out->o.row, d.o_head = out->o.head, d.o_image = out->o.image;
+    return QRM_OK;
+}
+
+// A tensor as the kernels see it: where it is, or rows of the workspace that it is copied to (and, an output, from) where it does not lie on 16 bytes.
+struct AttnTensor {
+    AttnRows rows;
+    size_t at = 0; // in the workspace, where `copied`
+    bool copied = false;
+};
+
+// Parts of a workspace, one behind the other.
+struct Workspace {
+    size_t bytes = 0;
+    size_t take(size_t n)
+    {
+        const size_t at = bytes;
+        bytes += (n + 255) / 256 * 256;
+        return at;
+    }
+};
+
+AttnTensor place(const AttnCheck &a, const AttnRows &r, int64_t L, int heads, std::initializer_list<const void *> list, int copies, Workspace *w)
+{
+    const int size = type_bytes(a.d.type), e = 16 / size;
+    AttnTensor t;
+    t.rows = r;
+    // (a tile's rows are less than 2^31 bytes apart)
+    t.copied = a.wide != a.d.D || common_alignment(list) < 16 || r.row % e || r.head % e || r.image % e || r.row * size > (1 << 24);
+    if (t.copied) {
+        t.at = w->take((size_t)copies * a.d.N * heads * L * a.wide * size);
+        t.rows = {a.wide, L * a.wide, heads * L * a.wide};
+    }
+    return t;
+}
+
+AttnArgs attention_args(const AttnCheck &a, const AttnTensor &q, const AttnTensor &k, const AttnTensor &v, const AttnTensor &o, const int32_t *q_len, const int32_t *k_len)
+{
+    const qrm_attention_desc &d = a.d;
+    AttnArgs g{};
+    g.q_len = q_len, g.k_len = k_len;
+    g.q_row = q.rows.row, g.q_head = q.rows.head, g.q_image = q.rows.image;
+    g.k_row = k.rows.row, g.k_head = k.rows.head, g.k_image = k.rows.image;
+    g.v_row = v.rows.row, g.v_head = v.rows.head, g.v_image = v.rows.image;
+    g.o_row = o.rows.row, g.o_head = o.rows.head, g.o_image = o.rows.image;
+    g.N = (int)d.N, g.Lq = (int)d.Lq, g.Lk = (int)d.Lk, g.heads = d.heads, g.kv_heads = d.kv_heads, g.group = d.heads / d.kv_heads, g.D = a.wide;
+    g.scale = d.scale, g.causal = d.causal != 0;
+    return g;
 }
 
 } // namespace
@@ -243,12 +364,8 @@ qrm_status qrm_adamw_step(qrm_ctx *c, qrm_adamw *o, const void *const *h_grads, 
     if (!aligned_to(d_grad_scale, 4)) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
     const int n = (int)o->first_piece.size() - 1;
     if (n <= 0) return QRM_OK;
-    if (!h_grads) return fail(c, QRM_E_INVALID, "h_grads is NULL");
-    const size_t gb = type_bytes(o->types.grad);
-    for (int i = 0; i < n; ++i)
-        if (!aligned_to(h_grads[i], gb)) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
-    qrm_status st = start(c);
-    if (st != QRM_OK) return st;
+    qrm_status st = check_grads(c, o, h_grads);
+    if (st != QRM_OK || (st = start(c)) != QRM_OK) return st;
     // (1 - beta from the caller's 64 bits: from a beta of 32 it would be off by 1e-5)
     AdamwStep s{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, (float)lr, (float)(lr / (1.0 - pow(beta1, (double)step))),
                 (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step))), d_grad_scale};
@@ -260,6 +377,71 @@ qrm_status qrm_adamw_step(qrm_ctx *c, qrm_adamw *o, const void *const *h_grads, 
         if (e != hipSuccess) {
             char what[64];
             snprintf(what, sizeof what, "adamw launch of tensor %d and those behind it", i);
+            return hip_fail(c, e, what);
+        }
+    }
+    return QRM_OK;
+}
+
+qrm_status qrm_adamw_grad_norm(qrm_ctx *c, qrm_adamw *o, const void *const *h_grads, double max_norm, const float *d_unscale, float *d_norm, float *d_scale, void *stream)
+{
+    if (!c) return QRM_E_INVALID;
+    if (!o) return fail(c, QRM_E_INVALID, "opt is NULL");
+    if (o->device != c->device) return fail(c, QRM_E_INVALID, "the plan belongs to another device");
+    if (!(max_norm > 0.0)) return fail(c, QRM_E_INVALID, "max_norm must be above zero");
+    if (!d_norm && !d_scale) return fail(c, QRM_E_INVALID, "no output is asked for");
+    if (d_norm == d_scale || (d_unscale && (d_unscale == d_norm || d_unscale == d_scale))) return fail(c, QRM_E_INVALID, "an output is an input or the other output");
+    if (!aligned_to(d_unscale, 4) || !aligned_to(d_norm, 4) || !aligned_to(d_scale, 4)) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
+    qrm_status st = check_grads(c, o, h_grads);
+    if (st != QRM_OK || (st = start(c)) != QRM_OK) return st;
+    const int n = (int)o->first_piece.size() - 1;
+    auto pieces = [&](int i) { return o->first_piece[std::min(n, i + kAdamwGrads)] - o->first_piece[i]; };
+    NormParts parts{};
+    for (int i = 0; i == 0 || i < n; i += kAdamwGrads) parts.total += n ? norm_blocks(pieces(i)) : 1;
+    parts.max_norm = max_norm;
+    parts.unscale = d_unscale, parts.norm = d_norm, parts.scale = d_scale;
+    QrmSlot *slot = nullptr;
+    const hipStream_t s = (hipStream_t)stream;
+    if (parts.total > 1) {
+        if ((st = get_slot(c, s, parts.total * sizeof(double), &slot)) != QRM_OK || (st = get_counters(c, s, slot)) != QRM_OK) return st;
+        parts.sums = (double *)slot->ws;
+        parts.done = slot->counters;
+    }
+    hipError_t e = hipSuccess;
+    for (int i = 0; e == hipSuccess && (i == 0 || i < n); i += kAdamwGrads) {
+        const uint32_t count = n ? pieces(i) : 0;
+        parts.ends = i + kAdamwGrads >= n;
+        e = launch_grad_norm(o->types.grad, o->tensors, o->pieces, n ? o->first_piece[i] : 0, count, i, n ? h_grads + i : nullptr, std::min(n - i, kAdamwGrads), parts, s);
+        parts.first += norm_blocks(count);
+    }
+    if (slot) st = slot_done(c, slot, s, true);
+    return e == hipSuccess ? st : hip_fail(c, e, "grad_norm launch");
+}
+
+qrm_status qrm_adamw_scale_grads(qrm_ctx *c, qrm_adamw *o, const void *const *h_grads, const float *d_scale, void *const *h_outs, void *stream)
+{
+    if (!c) return QRM_E_INVALID;
+    if (!o) return fail(c, QRM_E_INVALID, "opt is NULL");
+    if (o->device != c->device) return fail(c, QRM_E_INVALID, "the plan belongs to another device");
+    if (!d_scale || !aligned_to(d_scale, 4)) return fail(c, QRM_E_INVALID, "d_scale is NULL or not aligned to its elements");
+    qrm_status st = check_grads(c, o, h_grads);
+    if (st != QRM_OK) return st;
+    const int n = (int)o->first_piece.size() - 1;
+    if (n <= 0) return QRM_OK;
+    if (!h_outs) return fail(c, QRM_E_INVALID, "h_outs is NULL");
+    for (int i = 0; i < n; ++i) {
+        if (!h_grads[i] != !h_outs[i]) return fail(c, QRM_E_INVALID, "a gradient without an output, or the reverse");
+        if (!aligned_to(h_outs[i], type_bytes(o->types.grad))) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
+    }
+    if ((st = start(c)) != QRM_OK) return st;
+    for (int i = 0; i < n; i += kScaleGrads) {
+        const int count = std::min(n - i, kScaleGrads);
+        const uint32_t from = o->first_piece[i], to = o->first_piece[i + count];
+        if (from == to) continue;
+        hipError_t e = launch_scale_grads(o->types.grad, o->tensors, o->pieces, from, to - from, i, h_grads + i, h_outs + i, count, d_scale, (hipStream_t)stream);
+        if (e != hipSuccess) {
+            char what[64];
+            snprintf(what, sizeof what, "scale_grads launch of tensor %d and those behind it", i);
             return hip_fail(c, e, what);
         }
     }
@@ -307,6 +489,125 @@ qrm_status qrm_message_loss(qrm_ctx *c, const float *d_logits, const uint8_t *d_
     hipError_t e = launch_message_loss(call, slot ? (double *)slot->ws : nullptr, slot ? slot->counters : nullptr, (hipStream_t)stream);
     if (slot) st = slot_done(c, slot, (hipStream_t)stream, true);
     return e == hipSuccess ? st : hip_fail(c, e, "message_loss launch");
+}
+
+qrm_status qrm_attention(qrm_ctx *c, const qrm_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v, const int32_t *d_q_len, const int32_t *d_k_len,
+                         void *d_o, float *d_lse, void *stream)
+{
+    if (!c) return QRM_E_INVALID;
+    AttnCheck a;
+    qrm_status st = check_attention(c, desc, &a);
+    if (st != QRM_OK) return st;
+    const qrm_attention_desc &d = a.d;
+    if (d.N == 0 || d.Lq == 0) return QRM_OK;
+    if (!d_q || !d_o || (d.Lk && (!d_k || !d_v))) return fail(c, QRM_E_INVALID, "d_q / d_k / d_v / d_o is NULL");
+    if (d_o == d_q || d_o == d_k || d_o == d_v) return fail(c, QRM_E_INVALID, "d_o is an input");
+    const int size = type_bytes(d.type);
+    if (common_alignment({d_q, d_k, d_v, d_o}) < size || !aligned_to(d_lse, 4) || !aligned_to(d_q_len, 4) || !aligned_to(d_k_len, 4))
+        return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
+    const AttnCut cut = plan_attention(d, a.wide, ATTN_FORWARD, c->num_cu);
+    Workspace w;
+    const AttnTensor q = place(a, a.q, d.Lq, d.heads, {d_q}, 1, &w), k = place(a, a.k, d.Lk, d.kv_heads, {d_k}, 1, &w), v = place(a, a.v, d.Lk, d.kv_heads, {d_v}, 1, &w),
+                     o = place(a, a.o, d.Lq, d.heads, {d_o}, 1, &w);
+    const size_t rows = (size_t)d.N * d.heads * d.Lq;
+    const size_t part = cut.splits > 1 ? w.take(cut.splits * rows * a.wide * 4) : 0, sums = cut.splits > 1 ? w.take(cut.splits * rows * 8) : 0;
+    if ((st = start(c)) != QRM_OK) return st;
+    QrmSlot *slot = nullptr;
+    const hipStream_t s = (hipStream_t)stream;
+    if (w.bytes && (st = get_slot(c, s, w.bytes, &slot)) != QRM_OK) return st;
+    uint8_t *const ws = slot ? (uint8_t *)slot->ws : nullptr;
+    AttnArgs g = attention_args(a, q, k, v, o, d_q_len, d_k_len);
+    g.parts = cut.parts, g.splits = cut.splits;
+    g.lse = d_lse;
+    g.part = (float *)(ws + part), g.part_sums = (float *)(ws + sums);
+    hipError_t e = hipSuccess;
+    auto in = [&](const AttnTensor &t, const AttnRows &r, const void *p, int64_t L, int heads) -> const void * {
+        if (!t.copied) return p;
+        if (e == hipSuccess && L) e = launch_attention_copy(d.type, false, r, const_cast<void *>(p), ws + t.at, d.N, L, heads, d.D, a.wide, s);
+        return ws + t.at;
+    };
+    g.q = in(q, a.q, d_q, d.Lq, d.heads);
+    g.k = in(k, a.k, d_k, d.Lk, d.kv_heads);
+    g.v = in(v, a.v, d_v, d.Lk, d.kv_heads);
+    g.o = o.copied ? ws + o.at : d_o;
+    if (e == hipSuccess) e = launch_attention(d.type, cut.kind, g, s);
+    if (e == hipSuccess && cut.splits > 1) e = launch_attention_join(d.type, g, s);
+    if (e == hipSuccess && o.copied) e = launch_attention_copy(d.type, true, a.o, d_o, g.o, d.N, d.Lq, d.heads, d.D, a.wide, s);
+    if (slot) st = slot_done(c, slot, s, true);
+    return e == hipSuccess ? st : hip_fail(c, e, "attention launch");
+}
+
+qrm_status qrm_attention_backward(qrm_ctx *c, const qrm_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v, const void *d_o, const void *d_do,
+                                  const float *d_lse, const int32_t *d_q_len, const int32_t *d_k_len, void *d_dq, void *d_dk, void *d_dv, void *stream)
+{
+    if (!c) return QRM_E_INVALID;
+    AttnCheck a;
+    qrm_status st = check_attention(c, desc, &a);
+    if (st != QRM_OK) return st;
+    const qrm_attention_desc &d = a.d;
+    if (!d_dq && !d_dk && !d_dv) return fail(c, QRM_E_INVALID, "no output is asked for");
+    if (d.Lq == 0) d_dq = nullptr;
+    if (d.Lk == 0) d_dk = d_dv = nullptr;
+    if (d.N == 0 || (!d_dq && !d_dk && !d_dv)) return QRM_OK;
+    if ((d.Lq && (!d_q || !d_o || !d_do || !d_lse)) || (d.Lk && (!d_k || !d_v))) return fail(c, QRM_E_INVALID, "d_q / d_k / d_v / d_o / d_do / d_lse is NULL");
+    const void *const inputs[] = {d_q, d_k, d_v, d_o, d_do}, *const outputs[] = {d_dq, d_dk, d_dv};
+    for (int i = 0; i < 3; ++i) {
+        for (const void *p : inputs)
+            if (outputs[i] && outputs[i] == p) return fail(c, QRM_E_INVALID, "an output is an input");
+        if (outputs[i] && outputs[i] == outputs[(i + 1) % 3]) return fail(c, QRM_E_INVALID, "two outputs are one");
+    }
+    const int size = type_bytes(d.type);
+    if (common_alignment({d_q, d_k, d_v, d_o, d_do, d_dq, d_dk, d_dv}) < size || !aligned_to(d_lse, 4) || !aligned_to(d_q_len, 4) || !aligned_to(d_k_len, 4))
+        return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
+    const AttnCut by_q = plan_attention(d, a.wide, ATTN_DQ, c->num_cu), by_k = plan_attention(d, a.wide, ATTN_DKV, c->num_cu);
+    Workspace w;
+    const size_t q_rows = (size_t)d.N * d.heads * d.Lq, k_rows = (size_t)d.N * d.kv_heads * d.Lk;
+    // (a copied tensor's gradient is written behind its copy)
+    const AttnTensor q = place(a, a.q, d.Lq, d.heads, {d_q, d_dq}, 2, &w), k = place(a, a.k, d.Lk, d.kv_heads, {d_k, d_dk}, 2, &w),
+                     v = place(a, a.v, d.Lk, d.kv_heads, {d_v, d_dv}, 2, &w), y = place(a, a.o, d.Lq, d.heads, {d_do}, 1, &w);
+    const size_t row_lse = w.take(q_rows * 4), row_delta = w.take(q_rows * 4);
+    const size_t part_q = d_dq && by_q.splits > 1 ? w.take(by_q.splits * q_rows * a.wide * 4) : 0, part_k = d_dk && by_k.splits > 1 ? w.take(by_k.splits * k_rows * a.wide * 4) : 0,
+                 part_v = d_dv && by_k.splits > 1 ? w.take(by_k.splits * k_rows * a.wide * 4) : 0;
+    if ((st = start(c)) != QRM_OK) return st;
+    QrmSlot *slot = nullptr;
+    const hipStream_t s = (hipStream_t)stream;
+    if ((st = get_slot(c, s, w.bytes, &slot)) != QRM_OK) return st;
+    uint8_t *const ws = (uint8_t *)slot->ws;
+    AttnArgs g = attention_args(a, q, k, v, y, d_q_len, d_k_len);
+    hipError_t e = hipSuccess;
+    auto in = [&](const AttnTensor &t, const AttnRows &r, const void *p, int64_t L, int heads) -> const void * {
+        if (!t.copied) return p;
+        if (e == hipSuccess && L) e = launch_attention_copy(d.type, false, r, const_cast<void *>(p), ws + t.at, d.N, L, heads, d.D, a.wide, s);
+        return ws + t.at;
+    };
+    auto out = [&](const AttnTensor &t, void *p, size_t rows) -> void * { return !p ? nullptr : t.copied ? ws + t.at + rows * a.wide * size : p; };
+    auto back = [&](const AttnTensor &t, const AttnRows &r, void *p, void *from, int64_t L, int heads) {
+        if (e == hipSuccess && p && t.copied) e = launch_attention_copy(d.type, true, r, p, from, d.N, L, heads, d.D, a.wide, s);
+    };
+    g.q = in(q, a.q, d_q, d.Lq, d.heads);
+    g.k = in(k, a.k, d_k, d.Lk, d.kv_heads);
+    g.v = in(v, a.v, d_v, d.Lk, d.kv_heads);
+    g.dy = in(y, a.o, d_do, d.Lq, d.heads);
+    g.dq = out(q, d_dq, q_rows), g.dk = out(k, d_dk, k_rows), g.dv = out(v, d_dv, k_rows);
+    g.row_lse = (float *)(ws + row_lse), g.row_delta = (float *)(ws + row_delta);
+    g.part = (float *)(ws + part_q), g.part_k = (float *)(ws + part_k), g.part_v = (float *)(ws + part_v);
+    if (e == hipSuccess && d.Lq) e = launch_attention_rows(d, d_o, d_do, d_lse, d_q_len, (float *)(ws + row_lse), (float *)(ws + row_delta), s);
+    if (d_dq) {
+        g.parts = by_q.parts, g.splits = by_q.splits;
+        if (e == hipSuccess) e = launch_attention(d.type, ATTN_DQ, g, s);
+        if (e == hipSuccess && g.splits > 1) e = launch_attention_add(d.type, g.part, g.splits, g.dq, q.rows, d.N, d.Lq, d.heads, a.wide, s);
+        back(q, a.q, d_dq, g.dq, d.Lq, d.heads);
+    }
+    if (d_dk || d_dv) {
+        g.parts = by_k.parts, g.splits = by_k.splits;
+        if (e == hipSuccess) e = launch_attention(d.type, ATTN_DKV, g, s);
+        if (e == hipSuccess && g.splits > 1 && d_dk) e = launch_attention_add(d.type, g.part_k, g.splits, g.dk, k.rows, d.N, d.Lk, d.kv_heads, a.wide, s);
+        if (e == hipSuccess && g.splits > 1 && d_dv) e = launch_attention_add(d.type, g.part_v, g.splits, g.dv, v.rows, d.N, d.Lk, d.kv_heads, a.wide, s);
+        back(k, a.k, d_dk, g.dk, d.Lk, d.kv_heads);
+        back(v, a.v, d_dv, g.dv, d.Lk, d.kv_heads);
+    }
+    st = slot_done(c, slot, s, true);
+    return e == hipSuccess ? st : hip_fail(c, e, "attention_backward launch");
 }
 
 } // extern "C"
