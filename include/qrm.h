@@ -445,7 +445,7 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
  * The same bits from call to call.  A value that is not finite in a row that is there reaches the outputs of its image and key head, no others.
  * Errors: QRM_E_INVALID (NULL pointer, N, Lq or Lk < 0, kv_heads that do not divide heads, D < 1, an unknown type, causal not 0 or 1, scale not above
  * zero, strides with which rows overlap, an output that is an input, two outputs that are one, no output, a pointer not aligned to its elements),
- * QRM_E_UNSUPPORTED (D above QRM_ATTENTION_MAX_D; N, Lk or Lq * heads above 2^30, N * heads above 2^23, 2^32 threads and more for the rows of
+ * QRM_E_UNSUPPORTED (D above QRM_ATTENTION_MAX_D; scale outside 2^-64 .. 2^64; N, Lk or Lq * heads above 2^30, N * heads above 2^23, 2^32 threads and more for the rows of
  * all images), QRM_E_NOMEM.
  */
 #define QRM_ATTENTION_MAX_D 512

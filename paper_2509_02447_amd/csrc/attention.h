@@ -46,14 +46,15 @@ template <typename T, int M> struct Mma {
 };
 
 // A wavefront's load of 64 times 16 (4) bytes, at off (per lane) of the resource, to `to` and what follows.  In asm, so that the compiler, which cannot tell
-// the tiles apart, does not wait for the next one before every read of this one; whoever reads waits (wait_loads) and passes a barrier.
+// the tiles apart, does not wait for the next one before every read of this one; whoever reads waits (wait_loads) and passes a barrier.  (m0 holds nothing
+// else in these kernels: it is set where it is used.)
 __device__ __forceinline__ void load_to_lds16(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, uint8_t *to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)(lds_t)to), "v"(off), "s"(rsrc) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)(lds_t)to), "v"(off), "s"(rsrc) : "memory");
 }
 __device__ __forceinline__ void load_to_lds4(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, uint8_t *to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)(lds_t)to), "v"(off), "s"(rsrc) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)(lds_t)to), "v"(off), "s"(rsrc) : "memory");
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // .. of the loads that the compiler knows: said once before a loop, it does not wait for them inside, and for what is under way there.
@@ -84,45 +85,51 @@ template <typename T, int DP> struct Tile {
         }
     }
 
-    // Row operand of a product that sums over the row's elements: tile row `row`, whose swizzle is that of row % 16 (blocks of 16 rows and more).
-    template <int M> static __device__ __forceinline__ typename Mma<T, M>::frag along(const uint8_t *tile, int row, int step, int g)
+    // An LDS address of a tile's operand is one address of the lane, whose piece is changed by a constant, plus a constant: MASK is what the swizzle reaches.
+    static constexpr int MASK = PB == 128 ? 7 : 15;
+    static __device__ __forceinline__ uint32_t piece_at(uint32_t at, int piece, int add) { return (at ^ (uint32_t)(piece & MASK) << 4) + (uint32_t)((piece & ~MASK) * 16 + add); }
+    template <typename V> static __device__ __forceinline__ V read(uint32_t at) { return *(const __attribute__((address_space(3))) V *)(uintptr_t)at; }
+
+    // Row operand of a product that sums over the row's elements, steps of 8 NG: the lane's address for row `row` of the tile, and the operand of a
+    // step from the tile and the block of 16 rows (or a multiple) that lie `add` bytes behind.
+    template <int M> static __device__ __forceinline__ uint32_t along_at(int row, int g) { return row * PB + (((sizeof(T) / 2 * g) ^ swizzle(row)) << 4); }
+    template <int M> static __device__ __forceinline__ typename Mma<T, M>::frag along(uint32_t at, int step, int add)
     {
         typedef typename Mma<T, M>::frag frag;
-        const int sw = swizzle(row);
         if constexpr (sizeof(T) == 2) {
-            return *(const frag *)(tile + row * PB + (((step * Mma<T, M>::NG + g) ^ sw) << 4));
+            return read<frag>(piece_at(at, step * Mma<T, M>::NG, add));
         } else {
-            const int piece = 2 * (step * Mma<T, M>::NG + g);
-            const f32x4 lo = *(const f32x4 *)(tile + row * PB + ((piece ^ sw) << 4)), hi = *(const f32x4 *)(tile + row * PB + (((piece + 1) ^ sw) << 4));
+            const f32x4 lo = read<f32x4>(piece_at(at, 2 * step * Mma<T, M>::NG, add)), hi = read<f32x4>(piece_at(at, 2 * step * Mma<T, M>::NG + 1, add));
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
 
     // Row operand of a product that sums over the tile's rows: its rows are elements d0 .. d0 + M - 1, element j of the summed index tile row
-    // first + row_of(j, g).
-    template <int M> static __device__ __forceinline__ typename Mma<T, M>::frag across(const uint8_t *tile, int first, int d0, int lane)
+    // first + row_of(j, g), `first` a multiple of 8 NG.  16-bit types: 16 lanes read 4 rows of 16 elements and hold 16 columns of 4.
+    template <int M> static __device__ __forceinline__ uint32_t across_at(int lane)
+    {
+        const int g = lane / M, row = 4 * g + (sizeof(T) == 2 ? lane % 16 / 4 : 0);
+        if (sizeof(T) == 2) return row * PB + (((lane % M / 16 * 2 + lane % 4 / 2) ^ swizzle(row)) << 4) + lane % 2 * 8;
+        return row * PB + ((lane % M / 4 ^ swizzle(row)) << 4) + lane % 4 * 4;
+    }
+    template <int M> static __device__ __forceinline__ typename Mma<T, M>::frag across(uint32_t at, int first, int d0, int add)
     {
         typedef Mma<T, M> X;
         typedef typename X::frag frag;
-        const int g = lane / M;
         if constexpr (sizeof(T) == 2) {
             typedef short v4 __attribute__((ext_vector_type(4)));
             typedef short v8 __attribute__((ext_vector_type(8)));
             v4 part[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) { // 16 lanes read 4 rows of 16 elements and hold 16 columns of 4
-                const int row = first + u * 4 * X::NG + 4 * g + lane % 16 / 4, piece = d0 / 8 + lane % M / 16 * 2 + lane % 4 / 2;
-                part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)(tile + row * PB + ((piece ^ swizzle(row)) << 4) + lane % 2 * 8));
+            for (int u = 0; u < 2; ++u) { // (eight rows further on the swizzle is another by 2, sixteen further on the same)
+                const uint32_t from = piece_at(at, d0 / 8 ^ (M == 32 ? 2 * u : 0), (first + u * 4 * X::NG) * PB + add);
+                part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)(uintptr_t)from);
             }
             return __builtin_bit_cast(frag, (v8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const int d = d0 + lane % M;
             frag f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int row = first + X::row_of(j, g);
-                f[j] = *(const float *)(tile + row * PB + (((d / 4) ^ swizzle(row)) << 4) + d % 4 * 4);
-            }
+            for (int j = 0; j < 8; ++j) f[j] = read<float>(piece_at(at, d0 / 4 ^ (j % 4) << 2 ^ (M == 32 ? j / 4 * 2 : 0), (first + X::row_of(j, 0)) * PB + add));
             return f;
         }
     }
@@ -205,7 +212,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
     constexpr int R = TK / X::NG; // scores of a lane
-    __shared__ alignas(16) uint8_t lds[NBUF * 2 * TK * L::PB];
+    __shared__ alignas(256) uint8_t lds[NBUF * 2 * TK * L::PB];
     AttnPlace at;
     if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
     if (a.causal) at.part = a.parts - 1 - at.part; // (the longest first)
@@ -242,13 +249,14 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 
     typename X::acc o[DP / M] = {};
     wait_known_loads();
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, along0 = lds0 + L::template along_at<M>(col, g), across0 = lds0 + L::template across_at<M>(lane);
     float top = -INFINITY, sum = 0.f; // of the raw scores; of this lane's probabilities
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
         wait_loads();
         attn_barrier();
         if (NBUF > 1 && t + 1 < to) load(t + 1);
-        const uint8_t *const kt = lds + (t - from) % NBUF * (2 * TK * L::PB), *const vt = kt + TK * L::PB;
+        const uint32_t tile = (t - from) % NBUF * (2 * TK * L::PB), along = along0 + tile, across = across0 + tile; // keys; values behind them
         const int first = t * TK;
         if (first < most) {
             typename X::acc s[TK / M];
@@ -256,7 +264,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
             for (int b = 0; b < TK / M; ++b) {
                 s[b] = typename X::acc{};
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(kt, b * M + col, i, g), q[i], s[b]);
+                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(along, i, b * M * L::PB), q[i], s[b]);
             }
             auto score = [&](int r) -> float { return s[r / X::C][r % X::C]; };
             if (first + TK > least) {
@@ -287,7 +295,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 #pragma unroll
             for (int u = 0; u < TK / X::KK; ++u)
 #pragma unroll
-                for (int d = 0; d < DP / M; ++d) o[d] = X::mul(L::template across<M>(vt, u * X::KK, d * M, lane), p[u], o[d]);
+                for (int d = 0; d < DP / M; ++d) o[d] = X::mul(L::template across<M>(across, u * X::KK, d * M, TK * L::PB), p[u], o[d]);
         }
         if (NBUF == 1 && t + 1 < to) {
             attn_barrier();
@@ -345,7 +353,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
     constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG; // keys at a time
-    __shared__ alignas(16) uint8_t lds[NBUF * 2 * TK * L::PB];
+    __shared__ alignas(256) uint8_t lds[NBUF * 2 * TK * L::PB];
     AttnPlace at;
     if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
     if (a.causal) at.part = a.parts - 1 - at.part;
@@ -383,9 +391,10 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
         dy[s] = row_piece<T>(dy_row, there, s * X::KK + 8 * g, a.D);
     }
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
-    const float about = there ? a.row_lse[index] : INFINITY, delta = there ? a.row_delta[index] : 0.f;
+    const float less = there ? a.row_lse[index] * a.scale * kLog2E : -INFINITY, delta = there ? a.row_delta[index] : 0.f;
 
     wait_known_loads();
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, along0 = lds0 + L::template along_at<M>(col, g), across0 = lds0 + L::template across_at<M>(lane);
     typename X::acc dq[DP / M] = {};
     Lift<T> lift;
     const float c = a.scale * kLog2E;
@@ -393,7 +402,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
         wait_loads();
         attn_barrier();
         if (NBUF > 1 && t + 1 < to) load(t + 1);
-        const uint8_t *const kt = lds + (t - from) % NBUF * (2 * TK * L::PB), *const vt = kt + TK * L::PB;
+        const uint32_t tile = (t - from) % NBUF * (2 * TK * L::PB), along = along0 + tile, across = across0 + tile;
 #pragma unroll
         for (int h = 0; h < TK; h += STEP) {
             const int first = t * TK + h;
@@ -403,13 +412,13 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
             for (int b = 0; b < BLOCKS; ++b) {
                 s[b] = dp[b] = typename X::acc{};
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(kt, h + b * M + col, i, g), q[i], s[b]);
+                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), q[i], s[b]);
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(vt, h + b * M + col, i, g), dy[i], dp[b]);
+                for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(along, i, (TK + h + b * M) * L::PB), dy[i], dp[b]);
             }
             float ds[R], high = 0.f;
 #pragma unroll
-            for (int r = 0; r < R; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / X::C][r % X::C], c, -about)) * (dp[r / X::C][r % X::C] - delta);
+            for (int r = 0; r < R; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / X::C][r % X::C], c, less)) * (dp[r / X::C][r % X::C] + delta);
             if (first + STEP > least) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) ds[r] = first + X::row_of(r, g) < seen ? ds[r] : 0.f;
@@ -430,7 +439,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
 #pragma unroll
             for (int u = 0; u < STEP / X::KK; ++u)
 #pragma unroll
-                for (int d = 0; d < DP / M; ++d) dq[d] = X::mul(L::template across<M>(kt, h + u * X::KK, d * M, lane), p[u], dq[d]);
+                for (int d = 0; d < DP / M; ++d) dq[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, 0), p[u], dq[d]);
         }
         if (NBUF == 1 && t + 1 < to) {
             attn_barrier();
@@ -461,7 +470,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG;
     constexpr int BUF = 2 * TQ * L::PB + 512; // queries, gradients, 64 log-sums, 64 deltas
     static_assert(TQ <= 64, "a wavefront loads a tile's log-sums at once");
-    __shared__ alignas(16) uint8_t lds[NBUF * BUF];
+    __shared__ alignas(256) uint8_t lds[NBUF * BUF];
     AttnPlace at;
     if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
@@ -501,6 +510,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     }
 
     wait_known_loads();
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, along0 = lds0 + L::template along_at<M>(col, g), across0 = lds0 + L::template across_at<M>(lane);
     typename X::acc dk[DK ? DP / M : 1] = {}, dv[DV ? DP / M : 1] = {};
     Lift<T> lift;
     const float c = a.scale * kLog2E;
@@ -508,33 +518,42 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
         wait_loads();
         attn_barrier();
         if (NBUF > 1 && t + 1 < to) load(t + 1);
-        const uint8_t *const qt = lds + (t - from) % NBUF * BUF, *const yt = qt + TQ * L::PB;
-        const float *const lse = (const float *)(qt + 2 * TQ * L::PB), *const delta = lse + 64;
+        const uint32_t tile = (t - from) % NBUF * BUF, along = along0 + tile, across = across0 + tile, sums = lds0 + tile + 2 * TQ * L::PB + 16 * g; // queries; gradients behind them
         const int pos0 = (skip + t % each) * TQ;
 #pragma unroll
         for (int h = 0; h < TQ; h += STEP) {
             if (pos0 + h >= q_len) break;
             const int behind = a.causal ? key0 - off - (pos0 + h) : 0; // query row r of these sees the wavefront's keys 0 .. r - behind
             if (behind >= STEP) continue;
+            // The sums begin with what is subtracted from them: minus delta, and minus lse / scale (f32: afterwards, for its 24 bits' sake).
+            constexpr bool AFTER = sizeof(T) == 4;
+            auto row_sums = [&](int r, int which) { return L::template read<f32x4>(sums + which * 256 + (h + X::row_of(r, 0)) * 4); };
             typename X::acc s[BLOCKS], dp[BLOCKS];
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 s[b] = dp[b] = typename X::acc{};
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(qt, h + b * M + col, i, g), k[i], s[b]);
+                for (int r = 0; r < X::C; r += 4) {
+                    const f32x4 less = AFTER ? f32x4{} : row_sums(b * X::C + r, 0), mean = row_sums(b * X::C + r, 1);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][r + e] = less[e], dp[b][r + e] = mean[e];
+                }
+#pragma unroll
+                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), k[i], s[b]);
                 if constexpr (DK) {
 #pragma unroll
-                    for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(yt, h + b * M + col, i, g), v[i], dp[b]);
+                    for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(along, i, (TQ + h + b * M) * L::PB), v[i], dp[b]);
                 }
             }
             float pr[R], ds[R];
 #pragma unroll
             for (int r = 0; r < R; r += 4) {
-                const f32x4 about = *(const f32x4 *)(lse + h + X::row_of(r, g)), mean = *(const f32x4 *)(delta + h + X::row_of(r, g));
+                const f32x4 less = AFTER ? row_sums(r, 0) : f32x4{};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    pr[r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[(r + e) / X::C][(r + e) % X::C], c, -about[e]));
-                    ds[r + e] = DK ? pr[r + e] * (dp[(r + e) / X::C][(r + e) % X::C] - mean[e]) : 0.f;
+                    const float score = s[(r + e) / X::C][(r + e) % X::C];
+                    pr[r + e] = __builtin_amdgcn_exp2f(AFTER ? __builtin_fmaf(score, c, less[e] * c) : score * c);
+                    ds[r + e] = DK ? pr[r + e] * dp[(r + e) / X::C][(r + e) % X::C] : 0.f;
                 }
             }
             if (behind > 1 - M && a.causal) {
@@ -560,8 +579,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
             for (int u = 0; u < STEP / X::KK; ++u)
 #pragma unroll
                 for (int d = 0; d < DP / M; ++d) {
-                    if constexpr (DV) dv[d] = X::mul(L::template across<M>(yt, h + u * X::KK, d * M, lane), p[u], dv[d]);
-                    if constexpr (DK) dk[d] = X::mul(L::template across<M>(qt, h + u * X::KK, d * M, lane), z[u], dk[d]);
+                    if constexpr (DV) dv[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, TQ * L::PB), p[u], dv[d]);
+                    if constexpr (DK) dk[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, 0), z[u], dk[d]);
                 }
         }
         if (NBUF == 1 && t + 1 < to) {

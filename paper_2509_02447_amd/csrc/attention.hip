@@ -13,16 +13,16 @@ hipError_t launch_attention_f16(int kind, const AttnArgs &a, hipStream_t s);
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLn2 = 0.693147180559945309f;
 
 uint32_t blocks_of(int64_t items) { return (uint32_t)((items + kThreads - 1) / kThreads); }
 
-// Sixteen lanes a row: sum of dy o, and the log-sum in powers of two (a row that sees nothing: +inf, so that its probabilities are zeros).  Rows behind
-// an image's queries are not read.
+// Sixteen lanes a row: minus the sum of dy o, and minus the log-sum over the scale (a row that sees nothing: -inf, so that its probabilities are zeros).
+// Rows behind an image's queries are not read.
 constexpr int kRowLanes = 16;
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, const T *dy, int64_t row, int64_t head, int64_t image, const float *lse, const int32_t *q_len,
-                                                                  int64_t all, int Lq, int heads, int D, float *row_lse, float *row_delta)
+                                                                  int64_t all, int Lq, int heads, int D, float scale, float *row_lse, float *row_delta)
 {
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kRowLanes;
     const int lane = threadIdx.x % kRowLanes;
@@ -42,8 +42,8 @@ __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, co
     for (int apart = kRowLanes / 2; apart; apart /= 2) sum += __shfl_xor(sum, apart);
     if (lane == 0) {
         const float l = there ? lse[i] : -INFINITY;
-        row_lse[i] = l == -INFINITY ? INFINITY : l * kLog2E;
-        row_delta[i] = l == -INFINITY ? 0.f : sum;
+        row_lse[i] = l == -INFINITY ? -INFINITY : -l / scale;
+        row_delta[i] = l == -INFINITY ? 0.f : -sum;
     }
 }
 
@@ -139,7 +139,7 @@ hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, con
         using T = std::remove_pointer_t<decltype(p)>;
         auto run = [&](auto width) {
             hipLaunchKernelGGL((attention_rows_kernel<T, decltype(width)::value>), grid, dim3(kThreads), 0, s, (const T *)o, (const T *)dy, d.o_row, d.o_head, d.o_image, lse, q_len,
-                               all, (int)d.Lq, d.heads, d.D, row_lse, row_delta);
+                               all, (int)d.Lq, d.heads, d.D, d.scale, row_lse, row_delta);
         };
         wide ? run(std::integral_constant<int, 16 / sizeof(T)>()) : run(std::integral_constant<int, 1>());
         return hipGetLastError();

@@ -189,7 +189,7 @@ struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie
     const void *q, *k, *v, *dy;
     void *o, *dq, *dk, *dv;
     float *lse;                        // [N,heads,Lq]
-    const float *row_lse, *row_delta;  // backward, [N,heads,Lq]: log-sums in powers of two (+inf: the row sees nothing), sums of dy o
+    const float *row_lse, *row_delta;  // backward, [N,heads,Lq]: minus log-sums over the scale (-inf: the row sees nothing), minus sums of dy o
     float *part, *part_sums;           // splits > 1: their results, f32 [splits][rows][D], and forward (power of two, sum) of each row
     float *part_k, *part_v;
     const int32_t *q_len, *k_len;      // [N] or null
@@ -212,10 +212,10 @@ constexpr AttnShape attn_shape(int size, int width, int kind)
     const int bytes = size * width;
     if (kind == ATTN_FEW) return bytes <= 256 ? AttnShape{32, 1, 64, 2, 1} : AttnShape{16, 1, 32, bytes <= 1024 ? 2 : 1, 1};
     if (kind == ATTN_FORWARD)
-        return bytes <= 256 ? AttnShape{32, 4, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 32, 2, size == 2 ? 1 : 2} : bytes == 1024 ? AttnShape{size == 2 ? 32 : 16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
+        return bytes <= 256 ? AttnShape{32, 4, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 32, 2, size == 2 ? 1 : 2} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
     if (kind == ATTN_DQ)
         return bytes <= 256 ? AttnShape{32, 4, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 32, 2, 1} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
-    return bytes <= 128 ? AttnShape{32, 4, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 32, 2, 1} : bytes == 512 ? AttnShape{32, 4, 32, 2, 1} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
+    return bytes <= 128 ? AttnShape{32, 4, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 32, 2, 2} : bytes == 512 ? AttnShape{16, 4, 32, 2, 2} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
 }
 // The registers hold the sums of dk and dv beside the keys and values, or they are two launches.
 constexpr bool attn_dk_dv_at_once(int size, int width) { return size * width <= 1024; }

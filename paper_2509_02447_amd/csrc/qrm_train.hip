@@ -131,6 +131,7 @@ qrm_status check_attention(qrm_ctx *c, const qrm_attention_desc *desc, AttnCheck
     if (!known_type(d.type)) return fail(c, QRM_E_INVALID, "unknown type");
     if (d.causal != 0 && d.causal != 1) return fail(c, QRM_E_INVALID, "causal is 0 or 1");
     if (!(d.scale > 0.f) || !std::isfinite(d.scale)) return fail(c, QRM_E_INVALID, "scale must be above zero");
+    if (d.scale < 0x1p-64f || d.scale > 0x1p64f) return fail(c, QRM_E_UNSUPPORTED, "scale outside 2^-64 .. 2^64");
     constexpr int64_t most = (int64_t)1 << 30;
     if (d.D > QRM_ATTENTION_MAX_D) return fail(c, QRM_E_UNSUPPORTED, "D above 512");
     if (d.N > most || d.Lq > most || d.Lk > most || d.Lq * d.heads > most) return fail(c, QRM_E_UNSUPPORTED, "N, Lk, or query rows of all heads of an image above 2^30");
