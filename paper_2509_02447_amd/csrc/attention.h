@@ -6,6 +6,9 @@
 // without leaving their registers: the order of the summed index is the same on both sides, whichever it is (kappa below).  The other operand of that
 // product is the tile again, transposed by the LDS read.
 //
+// Rows of 1 KB and more would not leave the registers two wavefronts to a SIMD.  There two wavefronts share a set of columns: each has half of the elements of
+// the rows and of the results, computes half of every score's sum, and they exchange these halves through LDS.
+//
 // Heads that share keys: query rows are counted (position, head of the group), so a tile of keys is read once for all of them; gradients of shared keys
 // are summed over the group inside one workgroup.  No atomics anywhere: the backward pass computes the scores twice, once with queries as columns for dq
 // and once with keys as columns for dk and dv.
@@ -60,6 +63,13 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)"
 // .. of the loads that the compiler knows: said once before a loop, it does not wait for them inside, and for what is under way there.
 __device__ __forceinline__ void wait_known_loads() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
 
+// A value that what follows is computed from anew, instead of being kept in registers from before.
+__device__ __forceinline__ int again(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // A tile in LDS: rows of PB bytes, a power of two, whose pieces of 16 bytes are swapped about within the row (swizzle) so that neither the reads of one
 // piece of 16 neighbouring rows nor those of 4 rows by 4 pieces meet in one of the 64 banks.
 template <typename T, int DP> struct Tile {
@@ -77,17 +87,21 @@ template <typename T, int DP> struct Tile {
         rows = max(0, min(rows, ROWS));
         const int bytes = rows ? (rows - 1) * row_bytes + D * (int)sizeof(T) : 0;
         __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(src), 0, bytes, 0x00020000);
+        // (rows of 1 KB and more: a row to a wavefront, whose offsets take four instructions; they are computed anew, as their registers are needed)
+        const int lane = PIECES >= 64 ? again(tid & 63) : 0;
 #pragma unroll
         for (int k = 0; k < COUNT / (WAVES * 64); ++k) {
-            const int at = k * (WAVES * 64) + tid, row = at / PIECES, piece = (at % PIECES) ^ swizzle(row);
+            const int first = (k * WAVES + wave) * 64, at = k * (WAVES * 64) + tid;
+            const int row = PIECES >= 64 ? first / PIECES : at / PIECES, piece = (PIECES >= 64 ? first % PIECES + lane : at % PIECES) ^ swizzle(row);
             const uint32_t off = piece * E < D ? (uint32_t)(row * row_bytes + piece * 16) : 0x80000000u;
-            load_to_lds16(rsrc, off, tile + (k * (WAVES * 64) + wave * 64) * 16);
+            load_to_lds16(rsrc, off, tile + first * 16);
         }
     }
 
     // An LDS address of a tile's operand is one address of the lane, whose piece is changed by a constant, plus a constant: MASK is what the swizzle reaches.
     static constexpr int MASK = PB == 128 ? 7 : 15;
     static __device__ __forceinline__ uint32_t piece_at(uint32_t at, int piece, int add) { return (at ^ (uint32_t)(piece & MASK) << 4) + (uint32_t)((piece & ~MASK) * 16 + add); }
+    template <typename V> static __device__ __forceinline__ void write(uint32_t at, V v) { *(__attribute__((address_space(3))) V *)(uintptr_t)at = v; }
     template <typename V> static __device__ __forceinline__ V read(uint32_t at) { return *(const __attribute__((address_space(3))) V *)(uintptr_t)at; }
 
     // Row operand of a product that sums over the row's elements, steps of 8 NG: the lane's address for row `row` of the tile, and the operand of a
@@ -167,6 +181,13 @@ __device__ __forceinline__ void attn_barrier()
     asm volatile("" ::: "memory");
 }
 
+// f32: an operand's eight loads are not on their way before the operand before it has been used, or there would be no registers for the sums; its eight products
+// take 256 cycles and more.
+template <typename T> __device__ __forceinline__ void one_by_one()
+{
+    if (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);
+}
+
 // Largest and sum over the lanes of a column.
 template <int M> __device__ __forceinline__ float column_max(float v)
 {
@@ -199,72 +220,99 @@ __device__ __forceinline__ bool attn_place(const AttnArgs &a, int parts, int spl
     return true;
 }
 
-__device__ __forceinline__ int attn_length(const int32_t *lens, int n, int all) { return lens ? max(0, min(lens[n], all)) : all; }
-
 // ---------------------------------------------------------------- forward
 
 // Columns: query rows (position, head of the group).  Walks over the keys with a running maximum; the results are scaled down when it has grown by more
 // than 2^8, so that most tiles leave them alone.  Sums and results in 32 bits; probabilities are rounded to the type for the second product (16-bit types:
 // half a step relative to each, unsystematic, which is what the output's own rounding is).
-template <typename T, int DP, int M, int WAVES, int TK, int NBUF, int OCC>
+template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF, int OCC>
 __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
-    constexpr int R = TK / X::NG; // scores of a lane
-    __shared__ alignas(256) uint8_t lds[NBUF * 2 * TK * L::PB];
+    constexpr int R = TK / X::NG, DH = DP / SHARE; // scores of a lane, elements of a wavefront
+    constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = R * 256; // exchanged: a wavefront's scores
+    static_assert(SHARE == 1 || NBUF == 1, "keys and values take turns");
+    __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
     AttnPlace at;
     if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
     if (a.causal) at.part = a.parts - 1 - at.part; // (the longest first)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
-    const int row0 = (at.part * WAVES + wave) * M, rows = a.Lq * a.group;
-    const int row = row0 + col, pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
-    const bool here = row < rows, there = here && pos < q_len;
+    const int half = SHARE > 1 ? wave % SHARE : 0, e0 = half * DH; // which elements
+    const int row0 = (at.part * (WAVES / SHARE) + wave / SHARE) * M, rows = a.Lq * a.group;
+    int row = row0 + col, pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
+    const bool there = row < rows && pos < q_len;
     const int seen = there ? (a.causal ? max(0, min(k_len, pos + off + 1)) : k_len) : 0; // keys that the column sees
-    // .. and the most and the least in the wavefront, the most in the workgroup
+    // .. and the most and the least in the wavefront
     auto last_seen = [&](int last_row) { const int p = min(last_row, rows - 1) / a.group; return a.causal ? max(0, min(k_len, min(p, q_len - 1) + off + 1)) : k_len; };
     const bool any = row0 < rows && row0 / a.group < q_len;
     const int most = any ? last_seen(row0 + M - 1) : 0;
     const int least = row0 + M <= rows && (row0 + M - 1) / a.group < q_len ? (a.causal ? max(0, min(k_len, row0 / a.group + off + 1)) : k_len) : 0;
-    const int base = at.part * WAVES * M;
-    const int all = base / a.group < q_len ? last_seen(base + WAVES * M - 1) : 0;
-    const int tiles = (all + TK - 1) / TK, from = (int)((int64_t)tiles * at.split / a.splits), to = (int)((int64_t)tiles * (at.split + 1) / a.splits);
+    const AttnSplit split = attn_split(attn_key_tiles(a, q_len, k_len, at.part), a.per, at.split);
+    if (at.split >= split.count) return;
+    const int from = split.from, to = split.to;
 
     const uint8_t *const k = (const uint8_t *)a.k + (at.n * a.k_image + at.kv * a.k_head) * (int64_t)sizeof(T);
     const uint8_t *const v = (const uint8_t *)a.v + (at.n * a.v_image + at.kv * a.v_head) * (int64_t)sizeof(T);
     const int k_bytes = (int)a.k_row * (int)sizeof(T), v_bytes = (int)a.v_row * (int)sizeof(T);
-    auto load = [&](int t) {
-        uint8_t *const tile = lds + (t - from) % NBUF * (2 * TK * L::PB);
-        const int first = t * TK;
-        L::template load<TK, WAVES>(k + (int64_t)first * k_bytes, k_bytes, k_len - first, a.D, tile, tid, wave);
-        L::template load<TK, WAVES>(v + (int64_t)first * v_bytes, v_bytes, k_len - first, a.D, tile + TK * L::PB, tid, wave);
+    auto load_k = [&](int t) {
+        L::template load<TK, WAVES>(k + (int64_t)t * TK * k_bytes, k_bytes, k_len - t * TK, a.D, lds + (t - from) % NBUF * (2 * TK * L::PB), tid, wave);
     };
-    if (from < to) load(from);
+    auto load_v = [&](int t) {
+        L::template load<TK, WAVES>(v + (int64_t)t * TK * v_bytes, v_bytes, k_len - t * TK, a.D, lds + (t - from) % NBUF * (2 * TK * L::PB) + TK * L::PB, tid, wave);
+    };
+    if (from < to) {
+        load_k(from);
+        if (SHARE == 1) load_v(from);
+    }
 
-    typename X::frag q[DP / X::KK];
+    typename X::frag q[DH / X::KK];
     const T *const q_row = (const T *)a.q + at.n * a.q_image + pos * a.q_row + head * a.q_head;
 #pragma unroll
-    for (int s = 0; s < DP / X::KK; ++s) q[s] = row_piece<T>(q_row, there, s * X::KK + 8 * g, a.D);
+    for (int s = 0; s < DH / X::KK; ++s) q[s] = row_piece<T>(q_row, there, e0 + s * X::KK + 8 * g, a.D);
 
-    typename X::acc o[DP / M] = {};
+    typename X::acc o[DH / M] = {};
     wait_known_loads();
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, along0 = lds0 + L::template along_at<M>(col, g), across0 = lds0 + L::template across_at<M>(lane);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, mine = lds0 + e0 * (int)sizeof(T);
+    const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
     float top = -INFINITY, sum = 0.f; // of the raw scores; of this lane's probabilities
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
         wait_loads();
         attn_barrier();
-        if (NBUF > 1 && t + 1 < to) load(t + 1);
+        if (SHARE > 1) {
+            load_v(t);
+        } else if (t + 1 < to) {
+            load_k(t + 1);
+            load_v(t + 1);
+        }
         const uint32_t tile = (t - from) % NBUF * (2 * TK * L::PB), along = along0 + tile, across = across0 + tile; // keys; values behind them
         const int first = t * TK;
-        if (first < most) {
+        if (SHARE > 1 || first < most) { // (wavefronts that exchange halves wait for each other)
             typename X::acc s[TK / M];
 #pragma unroll
             for (int b = 0; b < TK / M; ++b) {
                 s[b] = typename X::acc{};
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(along, i, b * M * L::PB), q[i], s[b]);
+                for (int i = 0; i < DH / X::KK; ++i) {
+                    s[b] = X::mul(L::template along<M>(along, i, b * M * L::PB), q[i], s[b]);
+                    one_by_one<T>();
+                }
+            }
+            if constexpr (SHARE > 1) {
+                const uint32_t to_other = lds0 + TILES + wave * SWAP + lane * 16, from_other = lds0 + TILES + (wave ^ 1) * SWAP + lane * 16;
+#pragma unroll
+                for (int r = 0; r < R; r += 4) L::write(to_other + r * 256, f32x4{s[r / X::C][r % X::C], s[r / X::C][r % X::C + 1], s[r / X::C][r % X::C + 2], s[r / X::C][r % X::C + 3]});
+                wait_loads();   // the values are there
+                attn_barrier(); // .. everybody's, and everybody has read the keys
+                if (t + 1 < to) load_k(t + 1);
+#pragma unroll
+                for (int r = 0; r < R; r += 4) {
+                    const f32x4 other = L::template read<f32x4>(from_other + r * 256);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[r / X::C][r % X::C + e] += other[e];
+                }
             }
             auto score = [&](int r) -> float { return s[r / X::C][r % X::C]; };
             if (first + TK > least) {
@@ -282,7 +330,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
                 top = now;
                 sum *= less;
 #pragma unroll
-                for (int d = 0; d < DP / M; ++d) o[d] *= less;
+                for (int d = 0; d < DH / M; ++d) o[d] *= less;
             }
             const float about = top == -INFINITY ? 0.f : top * c;
             typename X::frag p[TK / X::KK];
@@ -295,35 +343,35 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 #pragma unroll
             for (int u = 0; u < TK / X::KK; ++u)
 #pragma unroll
-                for (int d = 0; d < DP / M; ++d) o[d] = X::mul(L::template across<M>(across, u * X::KK, d * M, TK * L::PB), p[u], o[d]);
-        }
-        if (NBUF == 1 && t + 1 < to) {
-            attn_barrier();
-            load(t + 1);
+                for (int d = 0; d < DH / M; ++d) {
+                    o[d] = X::mul(L::template across<M>(across, u * X::KK, d * M, TK * L::PB), p[u], o[d]);
+                    one_by_one<T>();
+                }
         }
     }
     sum = column_sum<M>(sum);
-    if (!here) return;
+    row = row0 + again(col), pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
+    if (row >= rows) return;
     const float about = top == -INFINITY ? 0.f : top * c;
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
-    if (a.splits > 1) { // parts of a row: results and their sum about 2^about
+    if (split.count > 1) { // parts of a row: results and their sum about 2^about
         const int64_t all_rows = (int64_t)a.N * a.heads * a.Lq;
         float *const part = a.part + (at.split * all_rows + index) * a.D;
-        if (g == 0) ((float2 *)a.part_sums)[at.split * all_rows + index] = make_float2(sum > 0.f || sum != sum ? about : -INFINITY, sum);
+        if (g == 0 && half == 0) ((float2 *)a.part_sums)[at.split * all_rows + index] = make_float2(sum > 0.f || sum != sum ? about : -INFINITY, sum);
 #pragma unroll
-        for (int d = 0; d < DP / M; ++d)
+        for (int d = 0; d < DH / M; ++d)
 #pragma unroll
-            for (int r = 0; r < X::C; r += 4) store_four<float>(part, d * M + X::row_of(r, g), a.D, o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+            for (int r = 0; r < X::C; r += 4) store_four<float>(part, e0 + d * M + X::row_of(r, g), a.D, o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
         return;
     }
-    if (g == 0 && a.lse) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    if (g == 0 && half == 0 && a.lse) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
 #pragma unroll
-    for (int d = 0; d < DP / M; ++d)
+    for (int d = 0; d < DH / M; ++d)
 #pragma unroll
         for (int r = 0; r < X::C; r += 4)
-            store_four<T>(o_row, d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+            store_four<T>(o_row, e0 + d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
 }
 
 // ---------------------------------------------------------------- backward
@@ -346,20 +394,49 @@ template <typename T> struct Lift {
     }
 };
 
+// Two wavefronts that have halves of the scores' and products' sums of two blocks: each finishes one (the second one's is the second), in `inbox` + wave * 2 KB,
+// where the other one's half comes and where what it made of the block (with `make`: four scores and products to four numbers, and whatever else) stays for the
+// other to read.
+template <typename T, int M, typename L, typename ACC, typename F>
+__device__ __forceinline__ f32x4 finish_block(bool second, const ACC (&s)[2], const ACC (&dp)[2], uint32_t inbox, int wave, F &&make)
+{
+    const uint32_t mine = inbox + wave * 2048, others = inbox + (wave ^ 1) * 2048;
+    f32x4 score, product, give_s, give_p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        score[e] = second ? s[1][e] : s[0][e], give_s[e] = second ? s[0][e] : s[1][e];
+        product[e] = second ? dp[1][e] : dp[0][e], give_p[e] = second ? dp[0][e] : dp[1][e];
+    }
+    L::write(others, give_s);
+    L::write(others + 1024, give_p);
+    attn_barrier();
+    score += L::template read<f32x4>(mine);
+    product += L::template read<f32x4>(mine + 1024);
+    f32x4 made;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) made[e] = make(e, score[e], product[e]);
+    L::write(mine, made);
+    attn_barrier();
+    return made;
+}
+
 // Columns: query rows, as above.  dq = scale sum over keys of dS k, dS = P (do v - delta), P = exp(score - lse).
-template <typename T, int DP, int M, int WAVES, int TK, int NBUF, int OCC>
+template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF, int OCC>
 __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs a)
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
-    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG; // keys at a time
-    __shared__ alignas(256) uint8_t lds[NBUF * 2 * TK * L::PB];
+    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE; // keys at a time, elements of a wavefront
+    constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = 2048;
+    static_assert(SHARE == 1 || (BLOCKS == SHARE && X::C == 4 && TK == STEP), "of two wavefronts each finishes the scores of one block, once a tile");
+    __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
     AttnPlace at;
     if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
     if (a.causal) at.part = a.parts - 1 - at.part;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
-    const int row0 = (at.part * WAVES + wave) * M, rows = a.Lq * a.group;
+    const int half = SHARE > 1 ? wave % SHARE : 0, e0 = half * DH; // which elements
+    const int row0 = (at.part * (WAVES / SHARE) + wave / SHARE) * M, rows = a.Lq * a.group;
     const int row = row0 + col, pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
     const bool here = row < rows, there = here && pos < q_len;
     const int seen = there ? (a.causal ? max(0, min(k_len, pos + off + 1)) : k_len) : 0;
@@ -367,9 +444,9 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
     const bool any = row0 < rows && row0 / a.group < q_len;
     const int most = any ? last_seen(row0 + M - 1) : 0;
     const int least = row0 + M <= rows && (row0 + M - 1) / a.group < q_len ? (a.causal ? max(0, min(k_len, row0 / a.group + off + 1)) : k_len) : 0;
-    const int base = at.part * WAVES * M;
-    const int all = base / a.group < q_len ? last_seen(base + WAVES * M - 1) : 0;
-    const int tiles = (all + TK - 1) / TK, from = (int)((int64_t)tiles * at.split / a.splits), to = (int)((int64_t)tiles * (at.split + 1) / a.splits);
+    const AttnSplit split = attn_split(attn_key_tiles(a, q_len, k_len, at.part), a.per, at.split);
+    if (at.split >= split.count) return;
+    const int from = split.from, to = split.to;
 
     const uint8_t *const k = (const uint8_t *)a.k + (at.n * a.k_image + at.kv * a.k_head) * (int64_t)sizeof(T);
     const uint8_t *const v = (const uint8_t *)a.v + (at.n * a.v_image + at.kv * a.v_head) * (int64_t)sizeof(T);
@@ -382,20 +459,21 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
     };
     if (from < to) load(from);
 
-    typename X::frag q[DP / X::KK], dy[DP / X::KK];
+    typename X::frag q[DH / X::KK], dy[DH / X::KK];
     const T *const q_row = (const T *)a.q + at.n * a.q_image + pos * a.q_row + head * a.q_head;
     const T *const dy_row = (const T *)a.dy + at.n * a.o_image + pos * a.o_row + head * a.o_head;
 #pragma unroll
-    for (int s = 0; s < DP / X::KK; ++s) {
-        q[s] = row_piece<T>(q_row, there, s * X::KK + 8 * g, a.D);
-        dy[s] = row_piece<T>(dy_row, there, s * X::KK + 8 * g, a.D);
+    for (int s = 0; s < DH / X::KK; ++s) {
+        q[s] = row_piece<T>(q_row, there, e0 + s * X::KK + 8 * g, a.D);
+        dy[s] = row_piece<T>(dy_row, there, e0 + s * X::KK + 8 * g, a.D);
     }
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
     const float less = there ? a.row_lse[index] * a.scale * kLog2E : -INFINITY, delta = there ? a.row_delta[index] : 0.f;
 
     wait_known_loads();
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, along0 = lds0 + L::template along_at<M>(col, g), across0 = lds0 + L::template across_at<M>(lane);
-    typename X::acc dq[DP / M] = {};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, mine = lds0 + e0 * (int)sizeof(T);
+    const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
+    typename X::acc dq[DH / M] = {};
     Lift<T> lift;
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
@@ -406,22 +484,39 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
 #pragma unroll
         for (int h = 0; h < TK; h += STEP) {
             const int first = t * TK + h;
-            if (first >= most) break;
+            if (SHARE == 1 && first >= most) break;
             typename X::acc s[BLOCKS], dp[BLOCKS];
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 s[b] = dp[b] = typename X::acc{};
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), q[i], s[b]);
+                for (int i = 0; i < DH / X::KK; ++i) {
+                    s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), q[i], s[b]);
+                    one_by_one<T>();
+                }
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(along, i, (TK + h + b * M) * L::PB), dy[i], dp[b]);
+                for (int i = 0; i < DH / X::KK; ++i) {
+                    dp[b] = X::mul(L::template along<M>(along, i, (TK + h + b * M) * L::PB), dy[i], dp[b]);
+                    one_by_one<T>();
+                }
             }
             float ds[R], high = 0.f;
+            if constexpr (SHARE == 1) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / X::C][r % X::C], c, less)) * (dp[r / X::C][r % X::C] + delta);
-            if (first + STEP > least) {
+                for (int r = 0; r < R; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / X::C][r % X::C], c, less)) * (dp[r / X::C][r % X::C] + delta);
+                if (first + STEP > least) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) ds[r] = first + X::row_of(r, g) < seen ? ds[r] : 0.f;
+                    for (int r = 0; r < R; ++r) ds[r] = first + X::row_of(r, g) < seen ? ds[r] : 0.f;
+                }
+            } else {
+                const bool second = half != 0;
+                const f32x4 own = finish_block<T, M, L>(second, s, dp, lds0 + TILES + lane * 16, wave, [&](int e, float score, float product) {
+                    const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(score, c, less)) * (product + delta);
+                    return first + (second ? M : 0) + X::row_of(e, g) < seen ? z : 0.f;
+                });
+                const f32x4 other = L::template read<f32x4>(lds0 + TILES + lane * 16 + (wave ^ 1) * SWAP);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ds[e] = second ? other[e] : own[e], ds[4 + e] = second ? own[e] : other[e];
             }
             if constexpr (Lift<T>::USED) {
 #pragma unroll
@@ -430,7 +525,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
                 if (__any(lift.over(high))) {
                     const float less = lift.fit(high);
 #pragma unroll
-                    for (int d = 0; d < DP / M; ++d) dq[d] *= less;
+                    for (int d = 0; d < DH / M; ++d) dq[d] *= less;
                 }
             }
             typename X::frag p[STEP / X::KK];
@@ -439,7 +534,10 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
 #pragma unroll
             for (int u = 0; u < STEP / X::KK; ++u)
 #pragma unroll
-                for (int d = 0; d < DP / M; ++d) dq[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, 0), p[u], dq[d]);
+                for (int d = 0; d < DH / M; ++d) {
+                    dq[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, 0), p[u], dq[d]);
+                    one_by_one<T>();
+                }
         }
         if (NBUF == 1 && t + 1 < to) {
             attn_barrier();
@@ -448,38 +546,44 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
     }
     if (!here) return;
     const float by = a.scale / lift.by;
-    float *const part = a.splits > 1 ? a.part + (at.split * ((int64_t)a.N * a.heads * a.Lq) + index) * a.D : nullptr;
+    float *const part = split.count > 1 ? a.part + (at.split * ((int64_t)a.N * a.heads * a.Lq) + index) * a.D : nullptr;
     T *const out = (T *)a.dq + at.n * a.q_image + pos * a.q_row + head * a.q_head;
 #pragma unroll
-    for (int d = 0; d < DP / M; ++d)
+    for (int d = 0; d < DH / M; ++d)
 #pragma unroll
         for (int r = 0; r < X::C; r += 4) {
             const float w[4] = {dq[d][r] * by, dq[d][r + 1] * by, dq[d][r + 2] * by, dq[d][r + 3] * by};
-            if (part) store_four<float>(part, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
-            else store_four<T>(out, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+            if (part) store_four<float>(part, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+            else store_four<T>(out, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
         }
 }
 
 // Columns: key rows.  dv = sum over queries of P do, dk = scale sum of dS q, over all heads that share the keys.  DK, DV: which of the two (both where the
 // registers hold both).
-template <typename T, int DP, int M, int WAVES, int TQ, int NBUF, int OCC, bool DK, bool DV>
+template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, int OCC, bool DK, bool DV>
 __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs a)
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
-    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG;
+    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE;
     constexpr int BUF = 2 * TQ * L::PB + 512; // queries, gradients, 64 log-sums, 64 deltas
+    constexpr int TILES = NBUF * BUF, SWAP = 2048;
     static_assert(TQ <= 64, "a wavefront loads a tile's log-sums at once");
-    __shared__ alignas(256) uint8_t lds[NBUF * BUF];
+    static_assert(SHARE == 1 || (BLOCKS == SHARE && X::C == 4 && TQ == STEP), "of two wavefronts each finishes the scores of one block, once a tile");
+    __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
     AttnPlace at;
     if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
-    const int base = at.part * WAVES * M, key0 = base + wave * M, key = key0 + col;
+    const int half = SHARE > 1 ? wave % SHARE : 0, e0 = half * DH;
+    const int key0 = (at.part * (WAVES / SHARE) + wave / SHARE) * M, key = key0 + col;
     const bool here = key < a.Lk, there = key < k_len;
-    // tiles of a head's queries that see any of the workgroup's keys; all heads' one after the other
-    const int skip = a.causal ? max(0, base - off) / TQ : 0, each = base < k_len ? max(0, (q_len + TQ - 1) / TQ - skip) : 0;
-    const int tiles = each * a.group, from = (int)((int64_t)tiles * at.split / a.splits), to = (int)((int64_t)tiles * (at.split + 1) / a.splits);
+    // all heads' queries one after the other
+    int skip;
+    const int each = attn_query_tiles(a, q_len, k_len, at.part, &skip);
+    const AttnSplit split = attn_split(each * a.group, a.per, at.split);
+    if (at.split >= split.count) return;
+    const int from = split.from, to = split.to;
 
     const int q_bytes = (int)a.q_row * (int)sizeof(T), y_bytes = (int)a.o_row * (int)sizeof(T);
     auto load = [&](int t) {
@@ -500,18 +604,19 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     };
     if (from < to) load(from);
 
-    typename X::frag k[DP / X::KK], v[DK ? DP / X::KK : 1];
+    typename X::frag k[DH / X::KK], v[DK ? DH / X::KK : 1];
     const T *const k_row = (const T *)a.k + at.n * a.k_image + key * a.k_row + at.kv * a.k_head;
     const T *const v_row = (const T *)a.v + at.n * a.v_image + key * a.v_row + at.kv * a.v_head;
 #pragma unroll
-    for (int s = 0; s < DP / X::KK; ++s) {
-        k[s] = row_piece<T>(k_row, there, s * X::KK + 8 * g, a.D);
-        if constexpr (DK) v[s] = row_piece<T>(v_row, there, s * X::KK + 8 * g, a.D);
+    for (int s = 0; s < DH / X::KK; ++s) {
+        k[s] = row_piece<T>(k_row, there, e0 + s * X::KK + 8 * g, a.D);
+        if constexpr (DK) v[s] = row_piece<T>(v_row, there, e0 + s * X::KK + 8 * g, a.D);
     }
 
     wait_known_loads();
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, along0 = lds0 + L::template along_at<M>(col, g), across0 = lds0 + L::template across_at<M>(lane);
-    typename X::acc dk[DK ? DP / M : 1] = {}, dv[DV ? DP / M : 1] = {};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, mine = lds0 + e0 * (int)sizeof(T);
+    const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
+    typename X::acc dk[DK ? DH / M : 1] = {}, dv[DV ? DH / M : 1] = {};
     Lift<T> lift;
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
@@ -522,11 +627,11 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
         const int pos0 = (skip + t % each) * TQ;
 #pragma unroll
         for (int h = 0; h < TQ; h += STEP) {
-            if (pos0 + h >= q_len) break;
+            if (SHARE == 1 && pos0 + h >= q_len) break;
             const int behind = a.causal ? key0 - off - (pos0 + h) : 0; // query row r of these sees the wavefront's keys 0 .. r - behind
-            if (behind >= STEP) continue;
-            // The sums begin with what is subtracted from them: minus delta, and minus lse / scale (f32: afterwards, for its 24 bits' sake).
-            constexpr bool AFTER = sizeof(T) == 4;
+            if (SHARE == 1 && behind >= STEP) continue;
+            // The sums begin with what is subtracted from them: minus delta, and minus lse / scale (f32: that one afterwards, for its 24 bits' sake).
+            constexpr bool AFTER = sizeof(T) == 4 || SHARE > 1;
             auto row_sums = [&](int r, int which) { return L::template read<f32x4>(sums + which * 256 + (h + X::row_of(r, 0)) * 4); };
             typename X::acc s[BLOCKS], dp[BLOCKS];
 #pragma unroll
@@ -534,32 +639,58 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
                 s[b] = dp[b] = typename X::acc{};
 #pragma unroll
                 for (int r = 0; r < X::C; r += 4) {
-                    const f32x4 less = AFTER ? f32x4{} : row_sums(b * X::C + r, 0), mean = row_sums(b * X::C + r, 1);
+                    const f32x4 less = AFTER ? f32x4{} : row_sums(b * X::C + r, 0), mean = SHARE > 1 ? f32x4{} : row_sums(b * X::C + r, 1);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][r + e] = less[e], dp[b][r + e] = mean[e];
                 }
 #pragma unroll
-                for (int i = 0; i < DP / X::KK; ++i) s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), k[i], s[b]);
+                for (int i = 0; i < DH / X::KK; ++i) {
+                    s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), k[i], s[b]);
+                    one_by_one<T>();
+                }
                 if constexpr (DK) {
 #pragma unroll
-                    for (int i = 0; i < DP / X::KK; ++i) dp[b] = X::mul(L::template along<M>(along, i, (TQ + h + b * M) * L::PB), v[i], dp[b]);
+                    for (int i = 0; i < DH / X::KK; ++i) {
+                        dp[b] = X::mul(L::template along<M>(along, i, (TQ + h + b * M) * L::PB), v[i], dp[b]);
+                        one_by_one<T>();
+                    }
                 }
             }
             float pr[R], ds[R];
+            if constexpr (SHARE == 1) {
 #pragma unroll
-            for (int r = 0; r < R; r += 4) {
-                const f32x4 less = AFTER ? row_sums(r, 0) : f32x4{};
+                for (int r = 0; r < R; r += 4) {
+                    const f32x4 less = AFTER ? row_sums(r, 0) : f32x4{};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float score = s[(r + e) / X::C][(r + e) % X::C];
+                        pr[r + e] = __builtin_amdgcn_exp2f(AFTER ? __builtin_fmaf(score, c, less[e] * c) : score * c);
+                        ds[r + e] = DK ? pr[r + e] * dp[(r + e) / X::C][(r + e) % X::C] : 0.f;
+                    }
+                }
+                if (behind > 1 - M && a.causal) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+                        if (X::row_of(r, g) - behind < col) pr[r] = ds[r] = 0.f;
+                }
+            } else {
+                const bool second = half != 0;
+                const uint32_t swap = lds0 + TILES + lane * 16, block = sums + (h + (second ? M : 0)) * 4;
+                const f32x4 less = L::template read<f32x4>(block), mean = L::template read<f32x4>(block + 256);
+                f32x4 chance;
+                const f32x4 own = finish_block<T, M, L>(second, s, dp, swap, wave, [&](int e, float score, float product) {
+                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(score, c, less[e] * c)), z = p * (product + mean[e]);
+                    if (a.causal && X::row_of(e, g) + (second ? M : 0) - behind < col) p = z = 0.f;
+                    chance[e] = p;
+                    if (e == 3) L::write(swap + wave * SWAP + 1024, chance);
+                    return z;
+                });
+                const f32x4 other = L::template read<f32x4>(swap + (wave ^ 1) * SWAP), other_chance = L::template read<f32x4>(swap + (wave ^ 1) * SWAP + 1024);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float score = s[(r + e) / X::C][(r + e) % X::C];
-                    pr[r + e] = __builtin_amdgcn_exp2f(AFTER ? __builtin_fmaf(score, c, less[e] * c) : score * c);
-                    ds[r + e] = DK ? pr[r + e] * dp[(r + e) / X::C][(r + e) % X::C] : 0.f;
+                    ds[e] = second ? other[e] : own[e], ds[4 + e] = second ? own[e] : other[e];
+                    pr[e] = second ? other_chance[e] : chance[e], pr[4 + e] = second ? chance[e] : other_chance[e];
                 }
-            }
-            if (behind > 1 - M && a.causal) {
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-                    if (X::row_of(r, g) - behind < col) pr[r] = ds[r] = 0.f;
             }
             if constexpr (Lift<T>::USED && DK) {
                 float high = 0.f;
@@ -569,7 +700,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
                 if (__any(lift.over(high))) {
                     const float less = lift.fit(high);
 #pragma unroll
-                    for (int d = 0; d < DP / M; ++d) dk[d] *= less;
+                    for (int d = 0; d < DH / M; ++d) dk[d] *= less;
                 }
             }
             typename X::frag p[STEP / X::KK], z[STEP / X::KK];
@@ -578,9 +709,10 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
 #pragma unroll
             for (int u = 0; u < STEP / X::KK; ++u)
 #pragma unroll
-                for (int d = 0; d < DP / M; ++d) {
+                for (int d = 0; d < DH / M; ++d) {
                     if constexpr (DV) dv[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, TQ * L::PB), p[u], dv[d]);
                     if constexpr (DK) dk[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, 0), z[u], dk[d]);
+                    one_by_one<T>();
                 }
         }
         if (NBUF == 1 && t + 1 < to) {
@@ -594,19 +726,19 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     const int64_t index = ((int64_t)at.n * a.kv_heads + at.kv) * a.Lk + key, all_rows = (int64_t)a.N * a.kv_heads * a.Lk;
     auto write = [&](const typename X::acc *sums, float by, T *out, float *part) {
 #pragma unroll
-        for (int d = 0; d < DP / M; ++d)
+        for (int d = 0; d < DH / M; ++d)
 #pragma unroll
             for (int r = 0; r < X::C; r += 4) {
                 const float w[4] = {value(sums[d][r], by), value(sums[d][r + 1], by), value(sums[d][r + 2], by), value(sums[d][r + 3], by)};
-                if (part) store_four<float>(part, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
-                else store_four<T>(out, d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+                if (part) store_four<float>(part, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+                else store_four<T>(out, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
             }
     };
     const int64_t part_at = (at.split * all_rows + index) * a.D;
     if constexpr (DK)
-        if (a.dk) write(dk, by_k, (T *)a.dk + at.n * a.k_image + key * a.k_row + at.kv * a.k_head, a.splits > 1 ? a.part_k + part_at : nullptr);
+        if (a.dk) write(dk, by_k, (T *)a.dk + at.n * a.k_image + key * a.k_row + at.kv * a.k_head, split.count > 1 ? a.part_k + part_at : nullptr);
     if constexpr (DV)
-        if (a.dv) write(dv, by_v, (T *)a.dv + at.n * a.v_image + key * a.v_row + at.kv * a.v_head, a.splits > 1 ? a.part_v + part_at : nullptr);
+        if (a.dv) write(dv, by_v, (T *)a.dv + at.n * a.v_image + key * a.v_row + at.kv * a.v_head, split.count > 1 ? a.part_v + part_at : nullptr);
 }
 
 // ---------------------------------------------------------------- launches
@@ -619,26 +751,26 @@ template <typename T, int DP> hipError_t attention_launch_width(int kind, const 
     switch (kind) {
     case ATTN_FORWARD: {
         constexpr AttnShape h = attn_shape(size, DP, ATTN_FORWARD);
-        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
+        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
         break;
     }
     case ATTN_FEW: {
         constexpr AttnShape h = attn_shape(size, DP, ATTN_FEW);
-        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
+        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
         break;
     }
     case ATTN_DQ: {
         constexpr AttnShape h = attn_shape(size, DP, ATTN_DQ);
-        hipLaunchKernelGGL((attention_dq_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
+        hipLaunchKernelGGL((attention_dq_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
         break;
     }
     default: {
         constexpr AttnShape h = attn_shape(size, DP, ATTN_DKV);
         if constexpr (attn_dk_dv_at_once(size, DP)) {
-            hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy, true, true>), grid, dim3(h.waves * 64), 0, s, a);
+            hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy, true, true>), grid, dim3(h.waves * 64), 0, s, a);
         } else {
-            if (a.dk) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy, true, false>), grid, dim3(h.waves * 64), 0, s, a);
-            if (a.dv) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.tile, h.buffers, h.occupancy, false, true>), grid, dim3(h.waves * 64), 0, s, a);
+            if (a.dk) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy, true, false>), grid, dim3(h.waves * 64), 0, s, a);
+            if (a.dv) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy, false, true>), grid, dim3(h.waves * 64), 0, s, a);
         }
     }
     }

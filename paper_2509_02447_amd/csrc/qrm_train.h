@@ -195,27 +195,32 @@ struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie
     const int32_t *q_len, *k_len;      // [N] or null
     int64_t q_row, q_head, q_image, k_row, k_head, k_image, v_row, v_head, v_image, o_row, o_head, o_image;
     int N, Lq, Lk, heads, kv_heads, group, D;
-    int parts, splits;                 // of the launch: tiles of the columns' rows, splits of the other side
+    int parts, splits, per;            // of the launch: tiles of the columns' rows, the most splits of the other side, and its tiles in one
+    int columns, tile;                 // rows of a part, of a tile of the other side
     float scale;
     bool causal;
 };
-// How a kernel cuts its work: M columns to a wavefront (the matrix products' side), wavefronts of a workgroup, rows of the other side in a tile, tiles
-// in LDS, wavefronts to a SIMD that the registers are kept for.
+// How a kernel cuts its work: columns of a wavefront (the matrix products' side), wavefronts of a workgroup, how many of them share a set of columns, rows of
+// the other side in a tile, tiles in LDS, wavefronts to a SIMD that the registers are kept for.
 struct AttnShape {
-    int m, waves, tile, buffers, occupancy;
-    constexpr int rows() const { return m * waves; }
+    int m, waves, share, tile, buffers, occupancy;
+    constexpr int rows() const { return m * waves / share; }
 };
 enum { ATTN_FORWARD, ATTN_FEW, ATTN_DQ, ATTN_DKV }; // ATTN_FEW: forward with few query rows
 constexpr int attn_width(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 256 ? 256 : 512; }
 constexpr AttnShape attn_shape(int size, int width, int kind)
 {
-    const int bytes = size * width;
-    if (kind == ATTN_FEW) return bytes <= 256 ? AttnShape{32, 1, 64, 2, 1} : AttnShape{16, 1, 32, bytes <= 1024 ? 2 : 1, 1};
-    if (kind == ATTN_FORWARD)
-        return bytes <= 256 ? AttnShape{32, 4, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 32, 2, size == 2 ? 1 : 2} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
-    if (kind == ATTN_DQ)
-        return bytes <= 256 ? AttnShape{32, 4, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 32, 2, 1} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
-    return bytes <= 128 ? AttnShape{32, 4, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 32, 2, 2} : bytes == 512 ? AttnShape{16, 4, 32, 2, 2} : bytes == 1024 ? AttnShape{16, 4, 32, 2, 1} : AttnShape{16, 4, 32, 1, 1};
+    const int bytes = size * width; // of a row
+    switch (kind) {
+    case ATTN_FEW:
+        return bytes <= 256 ? AttnShape{32, 1, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 1, 1, 32, 2, 1} : AttnShape{16, 2, 2, 32, 1, 1};
+    case ATTN_FORWARD:
+        return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 1024 ? AttnShape{32, 8, 2, 32, 1, 2} : AttnShape{16, 8, 2, 32, 1, 2};
+    case ATTN_DQ:
+        return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
+    default:
+        return bytes <= 128 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
+    }
 }
 // The registers hold the sums of dk and dv beside the keys and values, or they are two launches.
 constexpr bool attn_dk_dv_at_once(int size, int width) { return size * width <= 1024; }
@@ -223,16 +228,43 @@ struct AttnRows { // where rows [N,L,heads,D] lie
     int64_t row, head, image;
 };
 struct AttnCut {
-    int kind, parts, splits;
+    int kind, parts, splits, per;
+    AttnShape shape;
 };
+// A part's splits: a workgroup walks down `per` tiles at most; a part of no more is written at once, the results of others are joined.  Both here and there
+// as many as are walked down at all: tiles of an image's length, not of Lk.
+struct AttnSplit {
+    int count, from, to;
+};
+__device__ __forceinline__ AttnSplit attn_split(int tiles, int per, int which)
+{
+    const int count = tiles <= per ? 1 : (tiles + per - 1) / per, each = (tiles + count - 1) / count;
+    return AttnSplit{count, which * each, min(tiles, (which + 1) * each)};
+}
+__device__ __forceinline__ int attn_length(const int32_t *lens, int n, int all) { return lens ? max(0, min(lens[n], all)) : all; }
+// Tiles of keys that any of a part's query rows sees; tiles of a head's queries (behind `skip`) that see any of a part's keys.
+__device__ __forceinline__ int attn_key_tiles(const AttnArgs &a, int q_len, int k_len, int part)
+{
+    const int first = part * a.columns / a.group;
+    if (first >= q_len) return 0;
+    const int last = min((part * a.columns + a.columns - 1) / a.group, q_len - 1);
+    return ((a.causal ? max(0, min(k_len, last + k_len - q_len + 1)) : k_len) + a.tile - 1) / a.tile;
+}
+__device__ __forceinline__ int attn_query_tiles(const AttnArgs &a, int q_len, int k_len, int part, int *skip)
+{
+    const int base = part * a.columns;
+    *skip = a.causal ? max(0, base - (k_len - q_len)) / a.tile : 0;
+    return base < k_len ? max(0, (q_len + a.tile - 1) / a.tile - *skip) : 0;
+}
 // width: D rounded up to 16 bytes.
 AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num_cu);
 hipError_t launch_attention(int type, int kind, const AttnArgs &a, hipStream_t s); // kind ATTN_DKV: dk, dv, whichever is not null
 // Backward, before all else: row_lse and row_delta of lse, o and dy.
 hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, const void *dy, const float *lse, const int32_t *q_len, float *row_lse, float *row_delta, hipStream_t s);
-// Behind launches with splits: the forward's parts into o and lse; the sums of gradient parts [splits][N,heads,L,D] into rows.
+// Behind launches with splits: the forward's parts into o and lse; the sums of gradient parts, [splits][N,heads,Lq,D] into dq (by_q.splits > 1) and
+// [splits][N,kv_heads,Lk,D] into dk and dv (by_k.splits > 1).
 hipError_t launch_attention_join(int type, const AttnArgs &a, hipStream_t s);
-hipError_t launch_attention_add(int type, const float *part, int splits, void *out, const AttnRows &r, int64_t N, int64_t L, int heads, int D, hipStream_t s);
+hipError_t launch_attention_add(int type, const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s);
 // Rows of any alignment into rows [N,heads,L,wide] that the kernels take, or (out) back.
 hipError_t launch_attention_copy(int type, bool out, const AttnRows &r, void *there, void *here, int64_t N, int64_t L, int heads, int D, int wide, hipStream_t s);
 

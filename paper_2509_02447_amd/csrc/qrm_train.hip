@@ -203,6 +203,12 @@ AttnArgs attention_args(const AttnCheck &a, const AttnTensor &q, const AttnTenso
     return g;
 }
 
+void cut_to(AttnArgs *g, const AttnCut &cut)
+{
+    g->parts = cut.parts, g->splits = cut.splits, g->per = cut.per;
+    g->columns = cut.shape.rows(), g->tile = cut.shape.tile;
+}
+
 } // namespace
 
 extern "C" {
@@ -518,7 +524,7 @@ qrm_status qrm_attention(qrm_ctx *c, const qrm_attention_desc *desc, const void 
     if (w.bytes && (st = get_slot(c, s, w.bytes, &slot)) != QRM_OK) return st;
     uint8_t *const ws = slot ? (uint8_t *)slot->ws : nullptr;
     AttnArgs g = attention_args(a, q, k, v, o, d_q_len, d_k_len);
-    g.parts = cut.parts, g.splits = cut.splits;
+    cut_to(&g, cut);
     g.lse = d_lse;
     g.part = (float *)(ws + part), g.part_sums = (float *)(ws + sums);
     hipError_t e = hipSuccess;
@@ -593,20 +599,15 @@ qrm_status qrm_attention_backward(qrm_ctx *c, const qrm_attention_desc *desc, co
     g.row_lse = (float *)(ws + row_lse), g.row_delta = (float *)(ws + row_delta);
     g.part = (float *)(ws + part_q), g.part_k = (float *)(ws + part_k), g.part_v = (float *)(ws + part_v);
     if (e == hipSuccess && d.Lq) e = launch_attention_rows(d, d_o, d_do, d_lse, d_q_len, (float *)(ws + row_lse), (float *)(ws + row_delta), s);
-    if (d_dq) {
-        g.parts = by_q.parts, g.splits = by_q.splits;
-        if (e == hipSuccess) e = launch_attention(d.type, ATTN_DQ, g, s);
-        if (e == hipSuccess && g.splits > 1) e = launch_attention_add(d.type, g.part, g.splits, g.dq, q.rows, d.N, d.Lq, d.heads, a.wide, s);
-        back(q, a.q, d_dq, g.dq, d.Lq, d.heads);
-    }
-    if (d_dk || d_dv) {
-        g.parts = by_k.parts, g.splits = by_k.splits;
-        if (e == hipSuccess) e = launch_attention(d.type, ATTN_DKV, g, s);
-        if (e == hipSuccess && g.splits > 1 && d_dk) e = launch_attention_add(d.type, g.part_k, g.splits, g.dk, k.rows, d.N, d.Lk, d.kv_heads, a.wide, s);
-        if (e == hipSuccess && g.splits > 1 && d_dv) e = launch_attention_add(d.type, g.part_v, g.splits, g.dv, v.rows, d.N, d.Lk, d.kv_heads, a.wide, s);
-        back(k, a.k, d_dk, g.dk, d.Lk, d.kv_heads);
-        back(v, a.v, d_dv, g.dv, d.Lk, d.kv_heads);
-    }
+    AttnArgs gq = g, gk = g;
+    cut_to(&gq, by_q);
+    cut_to(&gk, by_k);
+    if (e == hipSuccess && d_dq) e = launch_attention(d.type, ATTN_DQ, gq, s);
+    if (e == hipSuccess && (d_dk || d_dv)) e = launch_attention(d.type, ATTN_DKV, gk, s);
+    if (e == hipSuccess) e = launch_attention_add(d.type, gq, gk, s);
+    back(q, a.q, d_dq, g.dq, d.Lq, d.heads);
+    back(k, a.k, d_dk, g.dk, d.Lk, d.kv_heads);
+    back(v, a.v, d_dv, g.dv, d.Lk, d.kv_heads);
     st = slot_done(c, slot, s, true);
     return e == hipSuccess ? st : hip_fail(c, e, "attention_backward launch");
 }
