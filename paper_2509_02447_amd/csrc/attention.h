@@ -75,7 +75,11 @@ __device__ __forceinline__ int again(int v)
 template <typename T, int DP> struct Tile {
     static constexpr int bytes_of(int n) { return n <= 128 ? 128 : n <= 256 ? 256 : n <= 512 ? 512 : n <= 1024 ? 1024 : 2048; }
     static constexpr int PB = bytes_of(DP * (int)sizeof(T)), E = 16 / (int)sizeof(T), PIECES = PB / 16;
-    static __device__ __forceinline__ int swizzle(int row) { return PB == 128 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3); }
+    static __device__ __forceinline__ int swizzle(int row)
+    {
+        const int four = (row >> 2 & 3) ^ (row >> 2 & 1) << 1; // 0, 3, 2, 1
+        return PB == 128 ? (row >> 1 & 1) << 2 | four : (row & 3) << 2 | four;
+    }
 
     // Rows 0 .. ROWS-1 of `src` (row_bytes apart, `rows` of them there, D elements each) on their way into the tile; what is not there becomes zeros.
     // WAVES * 64 threads; everything lies on 16 bytes.
@@ -188,6 +192,21 @@ template <typename T> __device__ __forceinline__ void one_by_one()
     if (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);
 }
 
+// Order of a block of COUNT products with READS LDS reads each (and FIRST reads before them): the reads of AHEAD products are on their way before the first
+// product, and each product is followed by the reads of another.  Left to itself the compiler reads just ahead of the use, and the products wait.
+template <typename T, int COUNT, int READS, int AHEAD, int FIRST = 0> __device__ __forceinline__ void in_turn()
+{
+    if (sizeof(T) == 4) return;
+    constexpr int DS = 0x100, MFMA = 0x8, A = AHEAD < COUNT ? AHEAD : COUNT;
+    __builtin_amdgcn_sched_group_barrier(DS, FIRST + A * READS, 0);
+#pragma unroll
+    for (int i = 0; i < COUNT - A; ++i) {
+        __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(DS, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(MFMA, A, 0);
+}
+
 // Largest and sum over the lanes of a column.
 template <int M> __device__ __forceinline__ float column_max(float v)
 {
@@ -202,21 +221,30 @@ template <int M> __device__ __forceinline__ float column_sum(float v)
 
 constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
-// Where a workgroup is: workgroups of a group of heads that share keys follow each other, on one die where there are groups enough (their keys stay in
-// its cache).  false: behind the last one.
+// Where a workgroup is.  Workgroups that walk down the same keys are on one die, whose cache then serves them all, where there are eight groups of heads that
+// share keys and more (consecutive workgroups are dealt to the eight dies in turn), or a number of them that divides eight; of a group's, those of one split
+// follow each other.  false: behind the last one.
 struct AttnPlace {
     int n, kv, part, split; // image, key head, tile of rows, split of the other side
 };
 __device__ __forceinline__ bool attn_place(const AttnArgs &a, int parts, int splits, int b, AttnPlace *p)
 {
     const int per = parts * splits, groups = a.N * a.kv_heads;
-    if (groups >= 8) b = b % 8 * ((groups * per + 7) / 8) + b / 8;
-    if (b >= groups * per) return false;
-    const int group = b / per, rest = b % per;
+    int group, rest;
+    if (groups < 8 && 8 % groups == 0) {
+        group = b % 8 % groups;
+        rest = b / 8 * (8 / groups) + b % 8 / groups;
+        if (rest >= per) return false;
+    } else {
+        if (groups >= 8) b = b % 8 * ((groups * per + 7) / 8) + b / 8;
+        if (b >= groups * per) return false;
+        group = b / per;
+        rest = b % per;
+    }
     p->n = group / a.kv_heads;
     p->kv = group % a.kv_heads;
-    p->part = rest / splits;
-    p->split = rest % splits;
+    p->part = rest % parts;
+    p->split = rest / parts;
     return true;
 }
 
@@ -230,7 +258,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
-    constexpr int R = TK / X::NG, DH = DP / SHARE; // scores of a lane, elements of a wavefront
+    constexpr int R = TK / X::NG, DH = DP / SHARE, AHEAD = 6; // scores of a lane, elements of a wavefront
     constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = R * 256; // exchanged: a wavefront's scores
     static_assert(SHARE == 1 || NBUF == 1, "keys and values take turns");
     __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
@@ -292,14 +320,15 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         if (SHARE > 1 || first < most) { // (wavefronts that exchange halves wait for each other)
             typename X::acc s[TK / M];
 #pragma unroll
-            for (int b = 0; b < TK / M; ++b) {
-                s[b] = typename X::acc{};
+            for (int b = 0; b < TK / M; ++b) s[b] = typename X::acc{};
 #pragma unroll
-                for (int i = 0; i < DH / X::KK; ++i) {
+            for (int i = 0; i < DH / X::KK; ++i)
+#pragma unroll
+                for (int b = 0; b < TK / M; ++b) { // (one after the other on other sums)
                     s[b] = X::mul(L::template along<M>(along, i, b * M * L::PB), q[i], s[b]);
                     one_by_one<T>();
                 }
-            }
+            in_turn<T, TK / M * (DH / X::KK), 1, AHEAD>();
             if constexpr (SHARE > 1) {
                 const uint32_t to_other = lds0 + TILES + wave * SWAP + lane * 16, from_other = lds0 + TILES + (wave ^ 1) * SWAP + lane * 16;
 #pragma unroll
@@ -347,6 +376,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
                     o[d] = X::mul(L::template across<M>(across, u * X::KK, d * M, TK * L::PB), p[u], o[d]);
                     one_by_one<T>();
                 }
+            in_turn<T, TK / X::KK * (DH / M), 2, AHEAD>();
         }
     }
     sum = column_sum<M>(sum);
@@ -426,7 +456,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
-    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE; // keys at a time, elements of a wavefront
+    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE, AHEAD = 6; // keys at a time, elements of a wavefront
     constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = 2048;
     static_assert(SHARE == 1 || (BLOCKS == SHARE && X::C == 4 && TK == STEP), "of two wavefronts each finishes the scores of one block, once a tile");
     __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
@@ -487,19 +517,17 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
             if (SHARE == 1 && first >= most) break;
             typename X::acc s[BLOCKS], dp[BLOCKS];
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                s[b] = dp[b] = typename X::acc{};
+            for (int b = 0; b < BLOCKS; ++b) s[b] = dp[b] = typename X::acc{};
 #pragma unroll
-                for (int i = 0; i < DH / X::KK; ++i) {
+            for (int i = 0; i < DH / X::KK; ++i)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
                     s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), q[i], s[b]);
                     one_by_one<T>();
-                }
-#pragma unroll
-                for (int i = 0; i < DH / X::KK; ++i) {
                     dp[b] = X::mul(L::template along<M>(along, i, (TK + h + b * M) * L::PB), dy[i], dp[b]);
                     one_by_one<T>();
                 }
-            }
+            in_turn<T, 2 * BLOCKS * (DH / X::KK), 1, AHEAD>();
             float ds[R], high = 0.f;
             if constexpr (SHARE == 1) {
 #pragma unroll
@@ -538,6 +566,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
                     dq[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, 0), p[u], dq[d]);
                     one_by_one<T>();
                 }
+            in_turn<T, STEP / X::KK * (DH / M), 2, AHEAD>();
         }
         if (NBUF == 1 && t + 1 < to) {
             attn_barrier();
@@ -565,7 +594,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
-    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE;
+    constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE, AHEAD = 4;
     constexpr int BUF = 2 * TQ * L::PB + 512; // queries, gradients, 64 log-sums, 64 deltas
     constexpr int TILES = NBUF * BUF, SWAP = 2048;
     static_assert(TQ <= 64, "a wavefront loads a tile's log-sums at once");
@@ -643,19 +672,19 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][r + e] = less[e], dp[b][r + e] = mean[e];
                 }
+            }
 #pragma unroll
-                for (int i = 0; i < DH / X::KK; ++i) {
+            for (int i = 0; i < DH / X::KK; ++i)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
                     s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), k[i], s[b]);
                     one_by_one<T>();
-                }
-                if constexpr (DK) {
-#pragma unroll
-                    for (int i = 0; i < DH / X::KK; ++i) {
+                    if constexpr (DK) {
                         dp[b] = X::mul(L::template along<M>(along, i, (TQ + h + b * M) * L::PB), v[i], dp[b]);
                         one_by_one<T>();
                     }
                 }
-            }
+            in_turn<T, 2 * BLOCKS * (DH / X::KK), 1, AHEAD, SHARE == 1 ? R / 2 : 0>();
             float pr[R], ds[R];
             if constexpr (SHARE == 1) {
 #pragma unroll
@@ -714,6 +743,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
                     if constexpr (DK) dk[d] = X::mul(L::template across<M>(across, h + u * X::KK, d * M, 0), z[u], dk[d]);
                     one_by_one<T>();
                 }
+            in_turn<T, 2 * (STEP / X::KK) * (DH / M), 2, AHEAD>();
         }
         if (NBUF == 1 && t + 1 < to) {
             attn_barrier();
@@ -746,8 +776,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
 template <typename T, int DP> hipError_t attention_launch_width(int kind, const AttnArgs &a, hipStream_t s)
 {
     constexpr int size = sizeof(T);
-    const int64_t blocks = (int64_t)a.N * a.kv_heads * a.parts * a.splits;
-    const dim3 grid((uint32_t)((blocks + 7) / 8 * 8));
+    const int64_t groups = (int64_t)a.N * a.kv_heads, per = (int64_t)a.parts * a.splits;
+    const dim3 grid((uint32_t)((groups * per + 7) / 8 * 8)); // (attn_place)
     switch (kind) {
     case ATTN_FORWARD: {
         constexpr AttnShape h = attn_shape(size, DP, ATTN_FORWARD);

@@ -3,6 +3,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
+#include <cstdlib>
 
 namespace qrm {
 
@@ -276,6 +278,13 @@ AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num
         const double us = rounds * (std::min(per * 1.0, tiles * share) * tile_us * h.occupancy + 3.0) + (n > 1 ? 5.0 + part_us * n * share : 0.0);
         if (n == 1 || us < best) best = us, c.splits = (int)n, c.per = (int)per;
     }
+    const char *env = getenv(kind == ATTN_DKV ? "SPL_K" : kind == ATTN_DQ ? "SPL_Q" : "SPL_F");
+    if (env) {
+        const int64_t n = std::min<int64_t>(atoi(env), tiles);
+        c.per = (int)((tiles + n - 1) / n);
+        c.splits = (int)((tiles + c.per - 1) / c.per);
+    }
+    if (getenv("SPL_SAY")) printf("kind %d blocks %ld tiles %ld splits %d per %d tile_us %.2f\n", c.kind, (long)blocks, (long)tiles, c.splits, c.per, tile_us);
     return c;
 }
 

@@ -215,11 +215,11 @@ constexpr AttnShape attn_shape(int size, int width, int kind)
     case ATTN_FEW:
         return bytes <= 256 ? AttnShape{32, 1, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 1, 1, 32, 2, 1} : AttnShape{16, 2, 2, 32, 1, 1};
     case ATTN_FORWARD:
-        return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 1024 ? AttnShape{32, 8, 2, 32, 1, 2} : AttnShape{16, 8, 2, 32, 1, 2};
+        return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 1024 ? AttnShape{size == 2 ? 16 : 32, 8, size == 2 ? 1 : 2, 32, size == 2 ? 2 : 1, 2} : AttnShape{16, 8, 2, 32, 1, 2};
     case ATTN_DQ:
         return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
     default:
-        return bytes <= 128 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
+        return bytes <= 128 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 1, size == 2 ? 64 : 32, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
     }
 }
 // The registers hold the sums of dk and dv beside the keys and values, or they are two launches.
