@@ -248,6 +248,22 @@ __device__ __forceinline__ bool attn_place(const AttnArgs &a, int parts, int spl
     return true;
 }
 
+// Where a split's results wait for those of others: as the lanes hold them, four results of a lane beside those of the next lane, so that a wavefront
+// writes and reads 1 KB at a time.  attention_join_kernel knows which row's they are.
+__device__ __forceinline__ int64_t attn_slot(const AttnArgs &a, const AttnPlace &at)
+{
+    return ((int64_t)at.split * a.N * a.kv_heads + at.n * a.kv_heads + at.kv) * a.parts + at.part;
+}
+template <int M, int WAVES, typename ACC, int COUNT> __device__ __forceinline__ void store_part(float *part, int64_t slot, int wave, int lane, float by, const ACC (&sums)[COUNT])
+{
+    constexpr int QUADS = M * M / 256;
+    f32x4 *const to = (f32x4 *)part + ((slot * WAVES + wave) * COUNT * QUADS) * 64 + lane;
+#pragma unroll
+    for (int d = 0; d < COUNT; ++d)
+#pragma unroll
+        for (int r = 0; r < QUADS; ++r) to[(d * QUADS + r) * 64] = f32x4{sums[d][4 * r] * by, sums[d][4 * r + 1] * by, sums[d][4 * r + 2] * by, sums[d][4 * r + 3] * by};
+}
+
 // ---------------------------------------------------------------- forward
 
 // Columns: query rows (position, head of the group).  Walks over the keys with a running maximum; the results are scaled down when it has grown by more
@@ -260,7 +276,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     typedef Tile<T, DP> L;
     constexpr int R = TK / X::NG, DH = DP / SHARE, AHEAD = 6; // scores of a lane, elements of a wavefront
     constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = R * 256; // exchanged: a wavefront's scores
-    static_assert(SHARE == 1 || NBUF == 1, "keys and values take turns");
+    constexpr bool TURNS = NBUF == 1; // keys and values take turns: the one is on its way while the other is used
+    static_assert(SHARE > 1 || !TURNS, "in turns there is a barrier between keys and values");
     __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
     AttnPlace at;
     if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
@@ -292,7 +309,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     };
     if (from < to) {
         load_k(from);
-        if (SHARE == 1) load_v(from);
+        if (!TURNS) load_v(from);
     }
 
     typename X::frag q[DH / X::KK];
@@ -304,12 +321,12 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     wait_known_loads();
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, mine = lds0 + e0 * (int)sizeof(T);
     const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
-    float top = -INFINITY, sum = 0.f; // of the raw scores; of this lane's probabilities
+    float top = -INFINITY, limit = -INFINITY, sums[4] = {}; // of the raw scores; 2^8 above, in powers of two; of this lane's probabilities
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
         wait_loads();
         attn_barrier();
-        if (SHARE > 1) {
+        if (TURNS) {
             load_v(t);
         } else if (t + 1 < to) {
             load_k(t + 1);
@@ -333,9 +350,9 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
                 const uint32_t to_other = lds0 + TILES + wave * SWAP + lane * 16, from_other = lds0 + TILES + (wave ^ 1) * SWAP + lane * 16;
 #pragma unroll
                 for (int r = 0; r < R; r += 4) L::write(to_other + r * 256, f32x4{s[r / X::C][r % X::C], s[r / X::C][r % X::C + 1], s[r / X::C][r % X::C + 2], s[r / X::C][r % X::C + 3]});
-                wait_loads();   // the values are there
-                attn_barrier(); // .. everybody's, and everybody has read the keys
-                if (t + 1 < to) load_k(t + 1);
+                if (TURNS) wait_loads(); // the values are there
+                attn_barrier();          // .. everybody's, and everybody has read the keys
+                if (TURNS && t + 1 < to) load_k(t + 1);
 #pragma unroll
                 for (int r = 0; r < R; r += 4) {
                     const f32x4 other = L::template read<f32x4>(from_other + r * 256);
@@ -349,15 +366,17 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
                 for (int r = 0; r < R; ++r)
                     if (first + X::row_of(r, g) >= seen) s[r / X::C][r % X::C] = -INFINITY;
             }
+            // The largest of the lane's own scores says whether the column's has grown: only then do its lanes ask each other.
             float high = score(0);
 #pragma unroll
             for (int r = 1; r < R; ++r) high = fmaxf(high, score(r));
-            high = column_max<M>(high);
-            if (__any(high * c > top * c + 8.f)) {
-                const float now = fmaxf(top, high);
+            if (__any(high * c > limit)) {
+                const float now = fmaxf(top, column_max<M>(high));
                 const float less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - now) * c);
                 top = now;
-                sum *= less;
+                limit = __builtin_fmaf(now, c, 8.f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums[e] *= less;
 #pragma unroll
                 for (int d = 0; d < DH / M; ++d) o[d] *= less;
             }
@@ -366,7 +385,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score(r), c, -about));
-                sum += e;
+                sums[r % 4] += e;
                 p[r / 8][r % 8] = (T)e;
             }
 #pragma unroll
@@ -379,21 +398,17 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
             in_turn<T, TK / X::KK * (DH / M), 2, AHEAD>();
         }
     }
-    sum = column_sum<M>(sum);
+    const float sum = column_sum<M>(sums[0] + sums[1] + (sums[2] + sums[3]));
     row = row0 + again(col), pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
-    if (row >= rows) return;
     const float about = top == -INFINITY ? 0.f : top * c;
-    const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
-    if (split.count > 1) { // parts of a row: results and their sum about 2^about
-        const int64_t all_rows = (int64_t)a.N * a.heads * a.Lq;
-        float *const part = a.part + (at.split * all_rows + index) * a.D;
-        if (g == 0 && half == 0) ((float2 *)a.part_sums)[at.split * all_rows + index] = make_float2(sum > 0.f || sum != sum ? about : -INFINITY, sum);
-#pragma unroll
-        for (int d = 0; d < DH / M; ++d)
-#pragma unroll
-            for (int r = 0; r < X::C; r += 4) store_four<float>(part, e0 + d * M + X::row_of(r, g), a.D, o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+    if (split.count > 1) { // a part of a row: results, and their sum about 2^about
+        const int64_t slot = attn_slot(a, at);
+        if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(sum > 0.f || sum != sum ? about : -INFINITY, sum);
+        store_part<M, WAVES>(a.part, slot, wave, lane, 1.f, o);
         return;
     }
+    if (row >= rows) return;
+    const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
     if (g == 0 && half == 0 && a.lse) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
@@ -573,18 +588,17 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
             load(t + 1);
         }
     }
-    if (!here) return;
     const float by = a.scale / lift.by;
-    float *const part = split.count > 1 ? a.part + (at.split * ((int64_t)a.N * a.heads * a.Lq) + index) * a.D : nullptr;
+    if (split.count > 1) {
+        store_part<M, WAVES>(a.part, attn_slot(a, at), wave, lane, by, dq);
+        return;
+    }
+    if (!here) return;
     T *const out = (T *)a.dq + at.n * a.q_image + pos * a.q_row + head * a.q_head;
 #pragma unroll
     for (int d = 0; d < DH / M; ++d)
 #pragma unroll
-        for (int r = 0; r < X::C; r += 4) {
-            const float w[4] = {dq[d][r] * by, dq[d][r + 1] * by, dq[d][r + 2] * by, dq[d][r + 3] * by};
-            if (part) store_four<float>(part, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
-            else store_four<T>(out, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
-        }
+        for (int r = 0; r < X::C; r += 4) store_four<T>(out, e0 + d * M + X::row_of(r, g), a.D, dq[d][r] * by, dq[d][r + 1] * by, dq[d][r + 2] * by, dq[d][r + 3] * by);
 }
 
 // Columns: key rows.  dv = sum over queries of P do, dk = scale sum of dS q, over all heads that share the keys.  DK, DV: which of the two (both where the
@@ -750,25 +764,29 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
             load(t + 1);
         }
     }
-    if (!here) return;
     const float by_k = a.scale / lift.by, by_v = 1.f / Lift<T>::PROBABILITY;
-    auto value = [&](float sum, float by) { return there ? sum * by : 0.f; };
-    const int64_t index = ((int64_t)at.n * a.kv_heads + at.kv) * a.Lk + key, all_rows = (int64_t)a.N * a.kv_heads * a.Lk;
-    auto write = [&](const typename X::acc *sums, float by, T *out, float *part) {
+    auto write = [&](const auto &sums, float by, T *out) {
 #pragma unroll
         for (int d = 0; d < DH / M; ++d)
 #pragma unroll
             for (int r = 0; r < X::C; r += 4) {
-                const float w[4] = {value(sums[d][r], by), value(sums[d][r + 1], by), value(sums[d][r + 2], by), value(sums[d][r + 3], by)};
-                if (part) store_four<float>(part, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
-                else store_four<T>(out, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
+                const float w[4] = {there ? sums[d][r] * by : 0.f, there ? sums[d][r + 1] * by : 0.f, there ? sums[d][r + 2] * by : 0.f, there ? sums[d][r + 3] * by : 0.f};
+                store_four<T>(out, e0 + d * M + X::row_of(r, g), a.D, w[0], w[1], w[2], w[3]);
             }
     };
-    const int64_t part_at = (at.split * all_rows + index) * a.D;
+    if (split.count > 1) {
+        const int64_t slot = attn_slot(a, at);
+        if constexpr (DK)
+            if (a.dk) store_part<M, WAVES>(a.part_k, slot, wave, lane, by_k, dk);
+        if constexpr (DV)
+            if (a.dv) store_part<M, WAVES>(a.part_v, slot, wave, lane, by_v, dv);
+        return;
+    }
+    if (!here) return;
     if constexpr (DK)
-        if (a.dk) write(dk, by_k, (T *)a.dk + at.n * a.k_image + key * a.k_row + at.kv * a.k_head, split.count > 1 ? a.part_k + part_at : nullptr);
+        if (a.dk) write(dk, by_k, (T *)a.dk + at.n * a.k_image + key * a.k_row + at.kv * a.k_head);
     if constexpr (DV)
-        if (a.dv) write(dv, by_v, (T *)a.dv + at.n * a.v_image + key * a.v_row + at.kv * a.v_head, split.count > 1 ? a.part_v + part_at : nullptr);
+        if (a.dv) write(dv, by_v, (T *)a.dv + at.n * a.v_image + key * a.v_row + at.kv * a.v_head);
 }
 
 // ---------------------------------------------------------------- launches

@@ -3,8 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdio>
-#include <cstdlib>
 
 namespace qrm {
 
@@ -49,116 +47,71 @@ __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, co
     }
 }
 
-// Joins the splits of a row: a thread has four elements of some of them; `lanes` threads, a power of two, have the same elements of others.  A row that was
-// written at once is left alone.
-struct JoinCut {
-    int quads, lanes, rows; // threads to a split's row (a power of two), of the same elements, rows of a workgroup
-    uint32_t blocks(int64_t all) const { return (uint32_t)((all + rows - 1) / rows); }
-};
-JoinCut join_cut(int D, int splits)
-{
-    JoinCut c{1, 1, 0};
-    while (c.quads * 4 < D) c.quads *= 2;
-    while (c.lanes < splits && c.lanes * c.quads < kThreads) c.lanes *= 2;
-    c.rows = kThreads / (c.quads * c.lanes);
-    return c;
-}
-
-// Adds f32 sums of `lanes` threads that are `quads` threads apart; the first has them.
-template <int COUNT> __device__ __forceinline__ void add_lanes(float (&v)[COUNT], int quads, int lanes, float (*shared)[COUNT + 1])
-{
-    for (int apart = lanes / 2; apart; apart /= 2) {
-        if (apart * quads < 64 && quads * apart * 2 <= 64) {
-#pragma unroll
-            for (int e = 0; e < COUNT; ++e) v[e] += __shfl_down(v[e], apart * quads);
-        } else {
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < COUNT; ++e) shared[threadIdx.x][e] = v[e];
-            __syncthreads();
-            const int from = threadIdx.x + apart * quads;
-            if (from < kThreads)
-#pragma unroll
-                for (int e = 0; e < COUNT; ++e) v[e] += shared[from][e];
-        }
-    }
-}
-
-// The forward's: results about a power of two, and their sum.
-template <typename T> __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttnArgs a, JoinCut cut, int64_t all)
-{
-    __shared__ float shared[kThreads][6];
-    const int quad = threadIdx.x % cut.quads, lane = threadIdx.x / cut.quads % cut.lanes, d = quad * 4;
-    const int64_t i = (int64_t)blockIdx.x * cut.rows + threadIdx.x / (cut.quads * cut.lanes);
-    const int64_t n = min(i, all - 1) / ((int64_t)a.heads * a.Lq);
-    const int rest = (int)(min(i, all - 1) - n * a.heads * a.Lq), h = rest / a.Lq, pos = rest % a.Lq;
-    const int part = (pos * a.group + h % a.group) / a.columns;
-    const int splits = attn_split(attn_key_tiles(a, attn_length(a.q_len, n, a.Lq), attn_length(a.k_len, n, a.Lk), part), a.per, 0).count;
-    const bool mine = i < all && splits > 1;
-    const float2 *const sums = (const float2 *)a.part_sums;
-    float top = -INFINITY;
-    if (mine)
-        for (int k = 0; k < splits; ++k) top = fmaxf(top, sums[k * all + i].x);
-    float o[5] = {}; // .. and the sum
-    if (mine && d < a.D)
-#pragma unroll 4
-        for (int k = lane; k < splits; k += cut.lanes) {
-            const float2 s = sums[k * all + i];
-            const Pack<float, 4> p = load_pack<float, 4>(a.part + (k * all + i) * a.D + d);
-            const float by = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
-            o[4] += s.y * by;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += by == 0.f ? 0.f : p.e[e] * by;
-        }
-    add_lanes<5>(o, cut.quads, cut.lanes, shared);
-    if (!mine || lane || d >= a.D) return;
-    const bool some = top != -INFINITY;
-    const float inv = some ? 1.f / o[4] : 0.f;
-    Pack<T, 4> out;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) out.e[e] = (T)(o[e] * inv);
-    store_pack<T, 4>((T *)a.o + n * a.o_image + h * a.o_head + pos * a.o_row + d, out);
-    if (d == 0 && a.lse) a.lse[i] = some ? (top + __builtin_amdgcn_logf(o[4])) * kLn2 : -INFINITY;
-}
-
-// Gradients': dq's rows, then those of dk, then those of dv.
-struct AddJob {
+// Joins the splits of a launch: a thread has four results, where the lanes of the splits' workgroups had them (store_part).  What was written at once is left alone.
+struct JoinJob {
     const float *part;
+    const float2 *sums; // forward: (power of two that a row's results are about, their sum)
     void *out;
-    int64_t row, head, image, all;
+    int64_t row, head, image;
+    AttnShape shape;
+    int width;
+    bool keys;      // rows are those of keys
     uint32_t first; // workgroup
-    JoinCut cut;
+    int64_t per;    // threads to a part
 };
-template <typename T> __global__ __launch_bounds__(kThreads) void attention_add_kernel(AttnArgs by_q, AttnArgs by_k, AddJob q, AddJob k, AddJob v)
+template <typename T> __device__ __forceinline__ void join_part(const AttnArgs &a, const JoinJob &j)
 {
-    __shared__ float shared[kThreads][5];
-    const bool is_q = blockIdx.x < k.first;
-    const AttnArgs &a = is_q ? by_q : by_k;
-    const AddJob j = is_q ? q : blockIdx.x < v.first ? k : v;
-    const int quad = threadIdx.x % j.cut.quads, lane = threadIdx.x / j.cut.quads % j.cut.lanes, d = quad * 4;
-    const int64_t i = (int64_t)(blockIdx.x - j.first) * j.cut.rows + threadIdx.x / (j.cut.quads * j.cut.lanes), near = min(i, j.all - 1);
-    const int L = is_q ? a.Lq : a.Lk, heads = is_q ? a.heads : a.kv_heads;
-    const int64_t n = near / ((int64_t)heads * L);
-    const int rest = (int)(near - n * heads * L), h = rest / L, pos = rest % L;
+    const AttnShape &h = j.shape;
+    const int64_t t = (int64_t)(blockIdx.x - j.first) * kThreads + threadIdx.x, which = t / j.per; // (a part is so many workgroups' work)
+    const int group = (int)(which / a.parts), part = (int)(which % a.parts), n = group / a.kv_heads, kv = group % a.kv_heads;
     const int q_len = attn_length(a.q_len, n, a.Lq), k_len = attn_length(a.k_len, n, a.Lk);
     int skip;
-    const int tiles = is_q ? attn_key_tiles(a, q_len, k_len, (pos * a.group + h % a.group) / a.columns) : attn_query_tiles(a, q_len, k_len, pos / a.columns, &skip) * a.group;
+    const int tiles = j.keys ? attn_query_tiles(a, q_len, k_len, part, &skip) * a.group : attn_key_tiles(a, q_len, k_len, part);
     const int splits = attn_split(tiles, a.per, 0).count;
-    const bool mine = i < j.all && splits > 1;
-    float sum[4] = {};
-    if (mine && d < a.D)
-#pragma unroll 4
-        for (int s = lane; s < splits; s += j.cut.lanes) {
-            const Pack<float, 4> p = load_pack<float, 4>(j.part + (s * j.all + i) * a.D + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += p.e[e];
-        }
-    add_lanes<4>(sum, j.cut.quads, j.cut.lanes, shared);
-    if (!mine || lane || d >= a.D) return;
+    if (splits == 1) return;
+    // the lane's columns and elements: as in store_part and Mma::row_of
+    const int item = (int)(t - which * j.per), lane = item % 64, ng = 64 / h.m, quads = h.m * h.m / 256, each = j.width / h.share, blocks = each / h.m * quads;
+    const int wave = item / 64 / blocks, block = item / 64 % blocks, column = wave / h.share * h.m + lane % h.m;
+    const int d = wave % h.share * each + block / quads * h.m + (block % quads * ng + lane / h.m) * 4;
+    const int r = part * a.columns + column, pos = j.keys ? r : r / a.group, head = j.keys ? kv : kv * a.group + r % a.group;
+    if (pos >= (j.keys ? a.Lk : a.Lq) || d >= a.D) return;
+    const int64_t apart = (int64_t)a.N * a.kv_heads * a.parts; // slots from one split to the next
+    const f32x4 *const from = (const f32x4 *)j.part + t;
+    f32x4 o = {};
     Pack<T, 4> out;
+    if (j.sums) {
+        const float2 *const sums = j.sums + which * a.columns + column;
+        float top = -INFINITY, sum = 0.f;
+        for (int k = 0; k < splits; ++k) top = fmaxf(top, sums[k * apart * a.columns].x);
+#pragma unroll 4
+        for (int k = 0; k < splits; ++k) {
+            const float2 s = sums[k * apart * a.columns];
+            const f32x4 p = from[k * apart * j.per];
+            const float by = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
+            sum += s.y * by;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out.e[e] = (T)sum[e];
-    store_pack<T, 4>((T *)j.out + n * j.image + h * j.head + pos * j.row + d, out);
+            for (int e = 0; e < 4; ++e) o[e] += by == 0.f ? 0.f : p[e] * by;
+        }
+        const bool some = top != -INFINITY;
+        const float inv = some ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= inv;
+        if (d == 0 && a.lse) a.lse[((int64_t)n * a.heads + head) * a.Lq + pos] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    } else {
+        if (!j.keys || r < k_len)
+#pragma unroll 4
+            for (int k = 0; k < splits; ++k) o += from[k * apart * j.per];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out.e[e] = (T)o[e];
+    store_pack<T, 4>((T *)j.out + n * j.image + head * j.head + pos * j.row + d, out);
+}
+template <typename T> __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttnArgs a, JoinJob j) { join_part<T>(a, j); }
+template <typename T> __global__ __launch_bounds__(kThreads) void attention_add_kernel(AttnArgs by_q, AttnArgs by_k, JoinJob q, JoinJob k, JoinJob v)
+{
+    if (blockIdx.x < k.first) join_part<T>(by_q, q);
+    else if (blockIdx.x < v.first) join_part<T>(by_k, k);
+    else join_part<T>(by_k, v);
 }
 
 // Rows [N,L,heads,D] from one place to another, element by element on the side that is not aligned: into rows of `wide` elements, zeros behind the D, or
@@ -208,28 +161,37 @@ hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, con
     });
 }
 
-hipError_t launch_attention_join(int type, const AttnArgs &a, hipStream_t s)
+namespace {
+
+// Adds a job's workgroups to those that there are.
+JoinJob join_job(const AttnArgs &a, const AttnCut &cut, const float *part, void *out, int64_t row, int64_t head, int64_t image, uint32_t *blocks)
 {
-    const int64_t all = (int64_t)a.N * a.heads * a.Lq;
-    const JoinCut cut = join_cut(a.D, a.splits);
+    JoinJob j{part, nullptr, out, row, head, image, cut.shape, cut.width, cut.kind == ATTN_DKV, *blocks, (int64_t)cut.shape.rows() * cut.width / 4};
+    if (out && a.splits > 1) *blocks += (uint32_t)(j.per * a.N * a.kv_heads * a.parts / kThreads);
+    return j;
+}
+
+} // namespace
+
+hipError_t launch_attention_join(int type, const AttnArgs &a, const AttnCut &cut, hipStream_t s)
+{
+    uint32_t blocks = 0;
+    JoinJob j = join_job(a, cut, a.part, a.o, a.o_row, a.o_head, a.o_image, &blocks);
+    j.sums = (const float2 *)a.part_sums;
+    if (!blocks) return hipSuccess;
     return with_type(type, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;
-        hipLaunchKernelGGL((attention_join_kernel<T>), dim3(cut.blocks(all)), dim3(kThreads), 0, s, a, cut, all);
+        hipLaunchKernelGGL((attention_join_kernel<T>), dim3(blocks), dim3(kThreads), 0, s, a, j);
         return hipGetLastError();
     });
 }
 
-hipError_t launch_attention_add(int type, const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s)
+hipError_t launch_attention_add(int type, const AttnArgs &by_q, const AttnCut &cut_q, const AttnArgs &by_k, const AttnCut &cut_k, hipStream_t s)
 {
     uint32_t blocks = 0;
-    auto job = [&](const AttnArgs &a, const float *part, void *out, int64_t row, int64_t head, int64_t image, int64_t all) {
-        AddJob j{part, out, row, head, image, all, blocks, join_cut(a.D, a.splits)};
-        if (out && a.splits > 1) blocks += j.cut.blocks(all);
-        return j;
-    };
-    const AddJob q = job(by_q, by_q.part, by_q.dq, by_q.q_row, by_q.q_head, by_q.q_image, (int64_t)by_q.N * by_q.heads * by_q.Lq);
-    const int64_t keys = (int64_t)by_k.N * by_k.kv_heads * by_k.Lk;
-    const AddJob k = job(by_k, by_k.part_k, by_k.dk, by_k.k_row, by_k.k_head, by_k.k_image, keys), v = job(by_k, by_k.part_v, by_k.dv, by_k.v_row, by_k.v_head, by_k.v_image, keys);
+    const JoinJob q = join_job(by_q, cut_q, by_q.part, by_q.dq, by_q.q_row, by_q.q_head, by_q.q_image, &blocks);
+    const JoinJob k = join_job(by_k, cut_k, by_k.part_k, by_k.dk, by_k.k_row, by_k.k_head, by_k.k_image, &blocks);
+    const JoinJob v = join_job(by_k, cut_k, by_k.part_v, by_k.dv, by_k.v_row, by_k.v_head, by_k.v_image, &blocks);
     if (!blocks) return hipSuccess;
     return with_type(type, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;
@@ -251,40 +213,41 @@ hipError_t launch_attention_copy(int type, bool out, const AttnRows &r, void *th
     });
 }
 
-// Splits of the other side are as many as let the busiest compute unit be done first, by a model of times in us: tiles at the rate that the kernels reach
-// (0.4 of the matrix products' peak), a workgroup alone on its compute unit at 0.65 of the time that it takes beside others, 3 us for a workgroup's beginning and
-// end, and the join, a launch that reads what the splits write.
+// Splits of the other side: as many as a model of times says is best.  Tiles take what the matrix products take at the rate that the kernels reach on a full card (1e15
+// operations a second, f32 1.2e14), for few rows what the memory takes (5 TB/s) and 1.6 us at least; a compute unit has its workgroups' tiles one after the other, and 4 us for
+// the beginning and end of those that it has at a time.  Where causal, parts differ: the longest workgroup bounds the launch, and the compute units are not done at one time (0.4 of the longest
+// behind their average).  The join is a launch (5 us) that reads what the splits write (6 TB/s, both).  Measured, us, by number of splits (the rule's in brackets):
+//   one head of 512, bf16, forward, 4 x 1024 rows: 1 66, 2 52, [4 40], 8 43; 4 x 4096 rows: 1 233, [2 169], 3 206, 4 180; backward, dq 4 x 1024: 1 134, 2 110, [4 97], 8 111
+//   (all of the call); dk and dv: 1 152, 2 112, [4 93], 8 116
+//   16 heads of 128, 4 key heads, causal: forward, 2 x 8192 rows [1 511], 2 645; backward, 2 x 4096, dk and dv: 1 831, 2 620, 3 549, [6 530], 12 554
+//   16 single tokens of 32 heads over up to 8191 rows of 4: 2 106, 4 60, 8 41, [12 40], 24 52; f32, 6 heads of 60, 3 x 2257 rows: 1 299, 2 242, [3 228], 4 254
 AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num_cu)
 {
     const int size = type_bytes(d.type), w = attn_width(width);
     const int64_t group = d.heads / d.kv_heads, columns = kind == ATTN_DKV ? d.Lk : d.Lq * group, others = kind == ATTN_DKV ? d.Lq : d.Lk;
     AttnCut c{};
     c.kind = kind;
+    c.width = w;
     if (kind == ATTN_FORWARD && columns <= attn_shape(size, w, ATTN_FEW).rows()) c.kind = ATTN_FEW;
+    const bool few = c.kind == ATTN_FEW;
     const AttnShape h = c.shape = attn_shape(size, w, c.kind);
     c.parts = (int)((columns + h.rows() - 1) / h.rows());
     const int64_t tiles = std::max<int64_t>(1, (others + h.tile - 1) / h.tile * (kind == ATTN_DKV ? group : 1)), blocks = std::max<int64_t>(1, d.N * d.kv_heads * c.parts);
     // the share of the tiles that a part sees on average where causal: of Lq x Lk, all but a triangle
-    const double lq = (double)d.Lq, lk = (double)d.Lk, seen = std::min(lq, lk), share = !d.causal || lq * lk == 0.0 ? 1.0 : seen * (lk - 0.5 * seen) / (lq * lk);
-    const double products = kind == ATTN_FORWARD ? 2.0 : kind == ATTN_DQ ? 3.0 : 4.0, rate = (size == 2 ? 1e15 : 6e13) / num_cu * 1e-6; // operations in a us of a compute unit
-    const double tile_us = products * 2.0 * h.rows() * h.tile * w / rate;
-    const double part_us = (kind == ATTN_DKV ? 2.0 : 1.0) * d.N * d.kv_heads * (double)columns * width * 8.0 / 4e6; // written and read again, a split
+    const double lq = (double)d.Lq, lk = (double)d.Lk, seen = std::min(lq, lk), share = !d.causal || few || lq * lk == 0.0 ? 1.0 : seen * (lk - 0.5 * seen) / (lq * lk);
+    const double products = kind == ATTN_FORWARD ? 2.0 : kind == ATTN_DQ ? 3.0 : 4.0, rate = (size == 2 ? 1e9 : 1.2e8) / num_cu; // operations in a us of a compute unit
+    const double bytes_us = 5e6 / num_cu, tile_us = std::max(products * 2.0 * h.rows() * h.tile * w / rate, few ? 2.0 * h.tile * w * size / bytes_us : 0.0), least_us = few ? 1.6 : 1.1 * tile_us;
+    const double part_us = (kind == ATTN_DKV ? 2.0 : 1.0) * blocks * h.rows() * w * 8.0 / 6e6; // of a split: written, and read again
+    const int at_once = std::max(1, std::min(h.occupancy * 4 / h.waves, (160 << 10) / (h.buffers * 2 * h.tile * w * size + 1024)));
     double best = 0.0;
     for (int64_t n = 1; n <= std::min<int64_t>(tiles, 64); ++n) {
         const int64_t per = (tiles + n - 1) / n;
         if ((tiles + per - 1) / per != n) continue;
-        const double all = std::max(1.0, n * share + (n > 1 && share < 1.0 ? 0.5 : 0.0)) * blocks, on_one = std::ceil(all / num_cu);
-        const double rounds = std::floor(on_one / h.occupancy) + 0.65 * (std::fmod(on_one, h.occupancy) > 0.0 ? 1.0 : 0.0);
-        const double us = rounds * (std::min(per * 1.0, tiles * share) * tile_us * h.occupancy + 3.0) + (n > 1 ? 5.0 + part_us * n * share : 0.0);
+        const double all = blocks * (share < 1.0 ? std::max(1.0, n * share + 0.5) : (double)n), on_one = std::ceil(all / num_cu), longest = per * least_us;
+        const double work = share < 1.0 ? blocks * tiles * share * tile_us / num_cu + 0.4 * longest : on_one * per * tile_us;
+        const double us = std::max(work, longest) + std::ceil(on_one / at_once) * 4.0 + (n > 1 ? 5.0 + part_us * n * share : 0.0);
         if (n == 1 || us < best) best = us, c.splits = (int)n, c.per = (int)per;
     }
-    const char *env = getenv(kind == ATTN_DKV ? "SPL_K" : kind == ATTN_DQ ? "SPL_Q" : "SPL_F");
-    if (env) {
-        const int64_t n = std::min<int64_t>(atoi(env), tiles);
-        c.per = (int)((tiles + n - 1) / n);
-        c.splits = (int)((tiles + c.per - 1) / c.per);
-    }
-    if (getenv("SPL_SAY")) printf("kind %d blocks %ld tiles %ld splits %d per %d tile_us %.2f\n", c.kind, (long)blocks, (long)tiles, c.splits, c.per, tile_us);
     return c;
 }
 

@@ -190,7 +190,7 @@ struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie
     void *o, *dq, *dk, *dv;
     float *lse;                        // [N,heads,Lq]
     const float *row_lse, *row_delta;  // backward, [N,heads,Lq]: minus log-sums over the scale (-inf: the row sees nothing), minus sums of dy o
-    float *part, *part_sums;           // splits > 1: their results, f32 [splits][rows][D], and forward (power of two, sum) of each row
+    float *part, *part_sums;           // splits > 1: their results, and forward (power of two, sum) of each row (store_part)
     float *part_k, *part_v;
     const int32_t *q_len, *k_len;      // [N] or null
     int64_t q_row, q_head, q_image, k_row, k_head, k_image, v_row, v_head, v_image, o_row, o_head, o_image;
@@ -228,8 +228,11 @@ struct AttnRows { // where rows [N,L,heads,D] lie
     int64_t row, head, image;
 };
 struct AttnCut {
-    int kind, parts, splits, per;
+    int kind, parts, splits, per, width; // width: of the kernel
     AttnShape shape;
+    // bytes that wait for the other splits': results, or forward their rows' sums
+    size_t part_bytes(const qrm_attention_desc &d) const { return splits > 1 ? (size_t)splits * d.N * d.kv_heads * parts * shape.rows() * width * 4 : 0; }
+    size_t sums_bytes(const qrm_attention_desc &d) const { return splits > 1 ? (size_t)splits * d.N * d.kv_heads * parts * shape.rows() * 8 : 0; }
 };
 // A part's splits: a workgroup walks down `per` tiles at most; a part of no more is written at once, the results of others are joined.  Both here and there
 // as many as are walked down at all: tiles of an image's length, not of Lk.
@@ -261,10 +264,9 @@ AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num
 hipError_t launch_attention(int type, int kind, const AttnArgs &a, hipStream_t s); // kind ATTN_DKV: dk, dv, whichever is not null
 // Backward, before all else: row_lse and row_delta of lse, o and dy.
 hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, const void *dy, const float *lse, const int32_t *q_len, float *row_lse, float *row_delta, hipStream_t s);
-// Behind launches with splits: the forward's parts into o and lse; the sums of gradient parts, [splits][N,heads,Lq,D] into dq (by_q.splits > 1) and
-// [splits][N,kv_heads,Lk,D] into dk and dv (by_k.splits > 1).
-hipError_t launch_attention_join(int type, const AttnArgs &a, hipStream_t s);
-hipError_t launch_attention_add(int type, const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s);
+// Behind launches with splits: what they have left, into o and lse, or into dq, dk and dv (those that are not null and were split).
+hipError_t launch_attention_join(int type, const AttnArgs &a, const AttnCut &cut, hipStream_t s);
+hipError_t launch_attention_add(int type, const AttnArgs &by_q, const AttnCut &cut_q, const AttnArgs &by_k, const AttnCut &cut_k, hipStream_t s);
 // Rows of any alignment into rows [N,heads,L,wide] that the kernels take, or (out) back.
 hipError_t launch_attention_copy(int type, bool out, const AttnRows &r, void *there, void *here, int64_t N, int64_t L, int heads, int D, int wide, hipStream_t s);
 

@@ -516,8 +516,7 @@ qrm_status qrm_attention(qrm_ctx *c, const qrm_attention_desc *desc, const void 
     Workspace w;
     const AttnTensor q = place(a, a.q, d.Lq, d.heads, {d_q}, 1, &w), k = place(a, a.k, d.Lk, d.kv_heads, {d_k}, 1, &w), v = place(a, a.v, d.Lk, d.kv_heads, {d_v}, 1, &w),
                      o = place(a, a.o, d.Lq, d.heads, {d_o}, 1, &w);
-    const size_t rows = (size_t)d.N * d.heads * d.Lq;
-    const size_t part = cut.splits > 1 ? w.take(cut.splits * rows * a.wide * 4) : 0, sums = cut.splits > 1 ? w.take(cut.splits * rows * 8) : 0;
+    const size_t part = w.take(cut.part_bytes(d)), sums = w.take(cut.sums_bytes(d));
     if ((st = start(c)) != QRM_OK) return st;
     QrmSlot *slot = nullptr;
     const hipStream_t s = (hipStream_t)stream;
@@ -538,7 +537,7 @@ qrm_status qrm_attention(qrm_ctx *c, const qrm_attention_desc *desc, const void 
     g.v = in(v, a.v, d_v, d.Lk, d.kv_heads);
     g.o = o.copied ? ws + o.at : d_o;
     if (e == hipSuccess) e = launch_attention(d.type, cut.kind, g, s);
-    if (e == hipSuccess && cut.splits > 1) e = launch_attention_join(d.type, g, s);
+    if (e == hipSuccess && cut.splits > 1) e = launch_attention_join(d.type, g, cut, s);
     if (e == hipSuccess && o.copied) e = launch_attention_copy(d.type, true, a.o, d_o, g.o, d.N, d.Lq, d.heads, d.D, a.wide, s);
     if (slot) st = slot_done(c, slot, s, true);
     return e == hipSuccess ? st : hip_fail(c, e, "attention launch");
@@ -573,8 +572,7 @@ qrm_status qrm_attention_backward(qrm_ctx *c, const qrm_attention_desc *desc, co
     const AttnTensor q = place(a, a.q, d.Lq, d.heads, {d_q, d_dq}, 2, &w), k = place(a, a.k, d.Lk, d.kv_heads, {d_k, d_dk}, 2, &w),
                      v = place(a, a.v, d.Lk, d.kv_heads, {d_v, d_dv}, 2, &w), y = place(a, a.o, d.Lq, d.heads, {d_do}, 1, &w);
     const size_t row_lse = w.take(q_rows * 4), row_delta = w.take(q_rows * 4);
-    const size_t part_q = d_dq && by_q.splits > 1 ? w.take(by_q.splits * q_rows * a.wide * 4) : 0, part_k = d_dk && by_k.splits > 1 ? w.take(by_k.splits * k_rows * a.wide * 4) : 0,
-                 part_v = d_dv && by_k.splits > 1 ? w.take(by_k.splits * k_rows * a.wide * 4) : 0;
+    const size_t part_q = w.take(d_dq ? by_q.part_bytes(d) : 0), part_k = w.take(d_dk ? by_k.part_bytes(d) : 0), part_v = w.take(d_dv ? by_k.part_bytes(d) : 0);
     if ((st = start(c)) != QRM_OK) return st;
     QrmSlot *slot = nullptr;
     const hipStream_t s = (hipStream_t)stream;
@@ -604,7 +602,7 @@ qrm_status qrm_attention_backward(qrm_ctx *c, const qrm_attention_desc *desc, co
     cut_to(&gk, by_k);
     if (e == hipSuccess && d_dq) e = launch_attention(d.type, ATTN_DQ, gq, s);
     if (e == hipSuccess && (d_dk || d_dv)) e = launch_attention(d.type, ATTN_DKV, gk, s);
-    if (e == hipSuccess) e = launch_attention_add(d.type, gq, gk, s);
+    if (e == hipSuccess) e = launch_attention_add(d.type, gq, by_q, gk, by_k, s);
     back(q, a.q, d_dq, g.dq, d.Lq, d.heads);
     back(k, a.k, d_dk, g.dk, d.Lk, d.kv_heads);
     back(v, a.v, d_dv, g.dv, d.Lk, d.kv_heads);
