@@ -63,6 +63,11 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)"
 // .. of the loads that the compiler knows: said once before a loop, it does not wait for them inside, and for what is under way there.
 __device__ __forceinline__ void wait_known_loads() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
 
+__device__ __forceinline__ uint32_t again_scalar(uint32_t v)
+{
+    asm volatile("" : "+s"(v));
+    return v;
+}
 // A value that what follows is computed from anew, instead of being kept in registers from before.
 __device__ __forceinline__ int again(int v)
 {
@@ -91,14 +96,18 @@ template <typename T, int DP> struct Tile {
         rows = max(0, min(rows, ROWS));
         const int bytes = rows ? (rows - 1) * row_bytes + D * (int)sizeof(T) : 0;
         __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(src), 0, bytes, 0x00020000);
-        // (rows of 1 KB and more: a row to a wavefront, whose offsets take four instructions; they are computed anew, as their registers are needed)
-        const int lane = PIECES >= 64 ? again(tid & 63) : 0;
+        // A lane's loads are APART rows apart; the swizzle of a sum of rows without common bits is that of the one and that of the other.  Offsets are computed anew
+        // each time, two instructions each: kept, they would take a register each.
+        constexpr int APART = WAVES * 64 / PIECES;
+        asm volatile("" : "+s"(row_bytes));
+        const int row = tid / PIECES, piece = (tid % PIECES) ^ swizzle(row), start = __mul24(row, row_bytes);
+        const bool full = D == PB / (int)sizeof(T);
 #pragma unroll
         for (int k = 0; k < COUNT / (WAVES * 64); ++k) {
-            const int first = (k * WAVES + wave) * 64, at = k * (WAVES * 64) + tid;
-            const int row = PIECES >= 64 ? first / PIECES : at / PIECES, piece = (PIECES >= 64 ? first % PIECES + lane : at % PIECES) ^ swizzle(row);
-            const uint32_t off = piece * E < D ? (uint32_t)(row * row_bytes + piece * 16) : 0x80000000u;
-            load_to_lds16(rsrc, off, tile + first * 16);
+            const int p = piece ^ swizzle(k * APART);
+            uint32_t off = start + k * APART * row_bytes + p * 16;
+            if (!full) off = p * E < D ? off : 0x80000000u;
+            load_to_lds16(rsrc, off, tile + (k * WAVES + wave) * 1024);
         }
     }
 
@@ -192,19 +201,34 @@ template <typename T> __device__ __forceinline__ void one_by_one()
     if (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);
 }
 
-// Order of a block of COUNT products with READS LDS reads each (and FIRST reads before them): the reads of AHEAD products are on their way before the first
-// product, and each product is followed by the reads of another.  Left to itself the compiler reads just ahead of the use, and the products wait.
-template <typename T, int COUNT, int READS, int AHEAD, int FIRST = 0> __device__ __forceinline__ void in_turn()
+// Order of a block of COUNT turns of PRODUCTS products with READS LDS reads together (and FIRST reads before them): the reads of AHEAD turns are on their way
+// before the first product, and each turn's products are followed by the reads of another.  Left to itself the compiler reads just ahead of the use, and the products wait.
+template <typename T, int COUNT, int READS, int AHEAD, int FIRST = 0, int PRODUCTS = 1> __device__ __forceinline__ void in_turn()
 {
     if (sizeof(T) == 4) return;
     constexpr int DS = 0x100, MFMA = 0x8, A = AHEAD < COUNT ? AHEAD : COUNT;
     __builtin_amdgcn_sched_group_barrier(DS, FIRST + A * READS, 0);
 #pragma unroll
     for (int i = 0; i < COUNT - A; ++i) {
-        __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(MFMA, PRODUCTS, 0);
         __builtin_amdgcn_sched_group_barrier(DS, READS, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(MFMA, A, 0);
+    __builtin_amdgcn_sched_group_barrier(MFMA, A * PRODUCTS, 0);
+}
+
+// Eight numbers as a column operand: 16-bit types two to an instruction.
+template <typename T> __device__ __forceinline__ auto pack_eight(const float *v)
+{
+    typedef T frag __attribute__((ext_vector_type(8)));
+    if constexpr (sizeof(T) == 4) {
+        return frag{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+    } else {
+        typedef T pair __attribute__((ext_vector_type(2)));
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, (pair){(T)v[2 * i], (T)v[2 * i + 1]});
+        return __builtin_bit_cast(frag, w);
+    }
 }
 
 // Largest and sum over the lanes of a column.
@@ -382,12 +406,14 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
             }
             const float about = top == -INFINITY ? 0.f : top * c;
             typename X::frag p[TK / X::KK];
+            float chance[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score(r), c, -about));
-                sums[r % 4] += e;
-                p[r / 8][r % 8] = (T)e;
+                chance[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(score(r), c, -about));
+                sums[r % 4] += chance[r];
             }
+#pragma unroll
+            for (int u = 0; u < TK / X::KK; ++u) p[u] = pack_eight<T>(chance + 8 * u);
 #pragma unroll
             for (int u = 0; u < TK / X::KK; ++u)
 #pragma unroll
@@ -573,7 +599,9 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
             }
             typename X::frag p[STEP / X::KK];
 #pragma unroll
-            for (int r = 0; r < R; ++r) p[r / 8][r % 8] = (T)(Lift<T>::USED ? ds[r] * lift.by : ds[r]);
+            for (int r = 0; r < R; ++r) ds[r] = Lift<T>::USED ? ds[r] * lift.by : ds[r];
+#pragma unroll
+            for (int u = 0; u < STEP / X::KK; ++u) p[u] = pack_eight<T>(ds + 8 * u);
 #pragma unroll
             for (int u = 0; u < STEP / X::KK; ++u)
 #pragma unroll
@@ -602,7 +630,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
 }
 
 // Columns: key rows.  dv = sum over queries of P do, dk = scale sum of dS q, over all heads that share the keys.  DK, DV: which of the two (both where the
-// registers hold both).
+// registers hold both).  Of the rows of 256 bytes of 16-bit types the values lie in LDS: with them in registers there are none left for operands that are on their way, and every
+// product waits for its own (2 x 4096 causal rows of 16 heads 320 us; from LDS 3 reads for two products instead of 2, TURN).
 template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, int OCC, bool DK, bool DV>
 __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs a)
 {
@@ -610,7 +639,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     typedef Tile<T, DP> L;
     constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE, AHEAD = 4;
     constexpr int BUF = 2 * TQ * L::PB + 512; // queries, gradients, 64 log-sums, 64 deltas
-    constexpr int TILES = NBUF * BUF, SWAP = 2048;
+    constexpr bool FROM_LDS = DK && DV && sizeof(T) == 2 && L::PB == 256;
+    constexpr int TILES = NBUF * BUF + (FROM_LDS ? WAVES * M * L::PB : 0), SWAP = 2048;
     static_assert(TQ <= 64, "a wavefront loads a tile's log-sums at once");
     static_assert(SHARE == 1 || (BLOCKS == SHARE && X::C == 4 && TQ == STEP), "of two wavefronts each finishes the scores of one block, once a tile");
     __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
@@ -629,9 +659,21 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     const int from = split.from, to = split.to;
 
     const int q_bytes = (int)a.q_row * (int)sizeof(T), y_bytes = (int)a.o_row * (int)sizeof(T);
-    auto load = [&](int t) {
-        uint8_t *const tile = lds + (t - from) % NBUF * BUF;
-        const int h = t / each, first = (skip + t - h * each) * TQ, head = at.kv * a.group + h;
+    struct Walk { // tile by tile, head by head
+        int head, tile, buffer;
+        __device__ __forceinline__ void next(int each)
+        {
+            const bool last = tile + 1 == each;
+            head += last ? 1 : 0;
+            tile = last ? 0 : tile + 1;
+            buffer = NBUF - 1 - buffer;
+        }
+    };
+    const int head0 = each ? from / each : 0;
+    Walk now{head0, from - head0 * each, 0}, ahead = now;
+    auto load = [&](const Walk &w) {
+        uint8_t *const tile = lds + w.buffer * BUF;
+        const int first = (skip + w.tile) * TQ, head = at.kv * a.group + w.head;
         const uint8_t *const q = (const uint8_t *)a.q + (at.n * a.q_image + head * a.q_head + (int64_t)first * a.q_row) * (int64_t)sizeof(T);
         const uint8_t *const y = (const uint8_t *)a.dy + (at.n * a.o_image + head * a.o_head + (int64_t)first * a.o_row) * (int64_t)sizeof(T);
         L::template load<TQ, WAVES>(q, q_bytes, q_len - first, a.D, tile, tid, wave);
@@ -641,33 +683,44 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
             const int bytes = min(64, q_len - first) * 4;
             __amdgpu_buffer_rsrc_t l = __builtin_amdgcn_make_buffer_rsrc((void *)(a.row_lse + index), 0, bytes, 0x00020000);
             __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc((void *)(a.row_delta + index), 0, bytes, 0x00020000);
-            load_to_lds4(l, lane * 4, tile + 2 * TQ * L::PB);
-            load_to_lds4(d, lane * 4, tile + 2 * TQ * L::PB + 256);
+            const uint32_t ones = again_scalar(~0u), off = __builtin_amdgcn_mbcnt_hi(ones, __builtin_amdgcn_mbcnt_lo(ones, 0)) * 4;
+            load_to_lds4(l, off, tile + 2 * TQ * L::PB);
+            load_to_lds4(d, off, tile + 2 * TQ * L::PB + 256);
         }
     };
-    if (from < to) load(from);
+    if (from < to) {
+        load(ahead);
+        if (FROM_LDS) {
+            const int base = at.part * (WAVES / SHARE) * M;
+            L::template load<WAVES * M, WAVES>((const uint8_t *)((const T *)a.v + at.n * a.v_image + at.kv * a.v_head + (int64_t)base * a.v_row), (int)a.v_row * (int)sizeof(T), k_len - base,
+                                               a.D, lds + NBUF * BUF, tid, wave);
+        }
+    }
 
-    typename X::frag k[DH / X::KK], v[DK ? DH / X::KK : 1];
+    typename X::frag k[DH / X::KK], v[DK && !FROM_LDS ? DH / X::KK : 1];
     const T *const k_row = (const T *)a.k + at.n * a.k_image + key * a.k_row + at.kv * a.k_head;
     const T *const v_row = (const T *)a.v + at.n * a.v_image + key * a.v_row + at.kv * a.v_head;
 #pragma unroll
     for (int s = 0; s < DH / X::KK; ++s) {
         k[s] = row_piece<T>(k_row, there, e0 + s * X::KK + 8 * g, a.D);
-        if constexpr (DK) v[s] = row_piece<T>(v_row, there, e0 + s * X::KK + 8 * g, a.D);
+        if constexpr (DK && !FROM_LDS) v[s] = row_piece<T>(v_row, there, e0 + s * X::KK + 8 * g, a.D);
     }
 
     wait_known_loads();
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, mine = lds0 + e0 * (int)sizeof(T);
     const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
+    const uint32_t values = lds0 + NBUF * BUF + L::template along_at<M>(wave * M + col, g);
     typename X::acc dk[DK ? DH / M : 1] = {}, dv[DV ? DH / M : 1] = {};
     Lift<T> lift;
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
         wait_loads();
         attn_barrier();
-        if (NBUF > 1 && t + 1 < to) load(t + 1);
-        const uint32_t tile = (t - from) % NBUF * BUF, along = along0 + tile, across = across0 + tile, sums = lds0 + tile + 2 * TQ * L::PB + 16 * g; // queries; gradients behind them
-        const int pos0 = (skip + t % each) * TQ;
+        ahead.next(each);
+        if (NBUF > 1 && t + 1 < to) load(ahead);
+        const uint32_t tile = now.buffer * BUF, along = along0 + tile, across = across0 + tile, sums = lds0 + tile + 2 * TQ * L::PB + 16 * g; // queries; gradients behind them
+        const int pos0 = (skip + now.tile) * TQ;
+        now.next(each);
 #pragma unroll
         for (int h = 0; h < TQ; h += STEP) {
             if (SHARE == 1 && pos0 + h >= q_len) break;
@@ -694,11 +747,14 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
                     s[b] = X::mul(L::template along<M>(along, i, (h + b * M) * L::PB), k[i], s[b]);
                     one_by_one<T>();
                     if constexpr (DK) {
-                        dp[b] = X::mul(L::template along<M>(along, i, (TQ + h + b * M) * L::PB), v[i], dp[b]);
+                        typename X::frag value;
+                        if constexpr (FROM_LDS) value = L::template along<M>(values, i, 0);
+                        else value = v[i];
+                        dp[b] = X::mul(L::template along<M>(along, i, (TQ + h + b * M) * L::PB), value, dp[b]);
                         one_by_one<T>();
                     }
                 }
-            in_turn<T, 2 * BLOCKS * (DH / X::KK), 1, AHEAD, SHARE == 1 ? R / 2 : 0>();
+            in_turn<T, BLOCKS * (DH / X::KK), FROM_LDS ? 3 : 2, AHEAD / 2, SHARE == 1 ? R / 2 : 0, 2>();
             float pr[R], ds[R];
             if constexpr (SHARE == 1) {
 #pragma unroll
@@ -748,7 +804,10 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
             }
             typename X::frag p[STEP / X::KK], z[STEP / X::KK];
 #pragma unroll
-            for (int r = 0; r < R; ++r) p[r / 8][r % 8] = (T)(Lift<T>::USED ? pr[r] * Lift<T>::PROBABILITY : pr[r]), z[r / 8][r % 8] = (T)(Lift<T>::USED ? ds[r] * lift.by : ds[r]);
+            for (int r = 0; r < R; ++r)
+                if (Lift<T>::USED) pr[r] *= Lift<T>::PROBABILITY, ds[r] *= lift.by;
+#pragma unroll
+            for (int u = 0; u < STEP / X::KK; ++u) p[u] = pack_eight<T>(pr + 8 * u), z[u] = pack_eight<T>(ds + 8 * u);
 #pragma unroll
             for (int u = 0; u < STEP / X::KK; ++u)
 #pragma unroll
@@ -761,7 +820,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
         }
         if (NBUF == 1 && t + 1 < to) {
             attn_barrier();
-            load(t + 1);
+            load(ahead);
         }
     }
     const float by_k = a.scale / lift.by, by_v = 1.f / Lift<T>::PROBABILITY;

@@ -219,7 +219,7 @@ constexpr AttnShape attn_shape(int size, int width, int kind)
     case ATTN_DQ:
         return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
     default:
-        return bytes <= 128 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 1, size == 2 ? 64 : 32, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
+        return bytes <= 128 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 256 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
     }
 }
 // The registers hold the sums of dk and dv beside the keys and values, or they are two launches.

@@ -180,8 +180,8 @@ AttnTensor place(const AttnCheck &a, const AttnRows &r, int64_t L, int heads, st
     const int size = type_bytes(a.d.type), e = 16 / size;
     AttnTensor t;
     t.rows = r;
-    // (a tile's rows are less than 2^31 bytes apart)
-    t.copied = a.wide != a.d.D || common_alignment(list) < 16 || r.row % e || r.head % e || r.image % e || r.row * size > (1 << 24);
+    // (the kernels multiply a tile's rows by their distance in 24 bits)
+    t.copied = a.wide != a.d.D || common_alignment(list) < 16 || r.row % e || r.head % e || r.image % e || r.row * size >= (1 << 23);
     if (t.copied) {
         t.at = w->take((size_t)copies * a.d.N * heads * L * a.wide * size);
         t.rows = {a.wide, L * a.wide, heads * L * a.wide};
