@@ -78,8 +78,7 @@ __device__ __forceinline__ int again(int v)
 // A tile in LDS: rows of PB bytes, a power of two, whose pieces of 16 bytes are swapped about within the row (swizzle) so that neither the reads of one
 // piece of 16 neighbouring rows nor those of 4 rows by 4 pieces meet in one of the 64 banks.
 template <typename T, int DP> struct Tile {
-    static constexpr int bytes_of(int n) { return n <= 128 ? 128 : n <= 256 ? 256 : n <= 512 ? 512 : n <= 1024 ? 1024 : 2048; }
-    static constexpr int PB = bytes_of(DP * (int)sizeof(T)), E = 16 / (int)sizeof(T), PIECES = PB / 16;
+    static constexpr int PB = attn_pitch(DP * (int)sizeof(T)), E = 16 / (int)sizeof(T), PIECES = PB / 16;
     static __device__ __forceinline__ int swizzle(int row)
     {
         const int four = (row >> 2 & 3) ^ (row >> 2 & 1) << 1; // 0, 3, 2, 1
@@ -156,7 +155,7 @@ template <typename T, int DP> struct Tile {
         } else {
             frag f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = read<float>(piece_at(at, d0 / 4 ^ (j % 4) << 2 ^ (M == 32 ? j / 4 * 2 : 0), (first + X::row_of(j, 0)) * PB + add));
+            for (int j = 0; j < 8; ++j) f[j] = read<float>(piece_at(at, d0 / 4 ^ swizzle(j % 4) ^ (M == 32 ? j / 4 * 2 : 0), (first + X::row_of(j, 0)) * PB + add));
             return f;
         }
     }
@@ -265,10 +264,10 @@ __device__ __forceinline__ bool attn_place(const AttnArgs &a, int parts, int spl
         group = b / per;
         rest = b % per;
     }
-    p->n = group / a.kv_heads;
-    p->kv = group % a.kv_heads;
-    p->part = rest % parts;
-    p->split = rest / parts;
+    p->n = a.kv_heads == 1 ? group : group / a.kv_heads;
+    p->kv = group - p->n * a.kv_heads;
+    p->split = splits == 1 ? 0 : rest / parts;
+    p->part = rest - p->split * parts;
     return true;
 }
 
@@ -286,6 +285,33 @@ template <int M, int WAVES, typename ACC, int COUNT> __device__ __forceinline__ 
     for (int d = 0; d < COUNT; ++d)
 #pragma unroll
         for (int r = 0; r < QUADS; ++r) to[(d * QUADS + r) * 64] = f32x4{sums[d][4 * r] * by, sums[d][4 * r + 1] * by, sums[d][4 * r + 2] * by, sums[d][4 * r + 3] * by};
+}
+
+// A wavefront's results as rows in memory: through LDS (`rows`, M rows of it, nobody else's any more), so that a row leaves in pieces of 16 bytes side by side instead of
+// 8 bytes a lane.  at(row): where a row's elements begin, or null.
+template <typename T, typename L, int M, typename ACC, int COUNT, typename F>
+__device__ __forceinline__ void store_rows(uint32_t rows, int lane, int D, float by, const ACC (&sums)[COUNT], F &&at)
+{
+    typedef Mma<T, M> X;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef T pair __attribute__((ext_vector_type(2)));
+    constexpr int PIECES = COUNT * M / 8;
+    const int col = lane % M, g = lane / M, sw = L::swizzle(col);
+#pragma unroll
+    for (int d = 0; d < COUNT; ++d)
+#pragma unroll
+        for (int r = 0; r < X::C; r += 4) {
+            const int e = d * M + X::row_of(r, 0) + 4 * g; // (four of a piece's eight)
+            const u32x2 w = {__builtin_bit_cast(uint32_t, (pair){(T)(sums[d][r] * by), (T)(sums[d][r + 1] * by)}),
+                             __builtin_bit_cast(uint32_t, (pair){(T)(sums[d][r + 2] * by), (T)(sums[d][r + 3] * by)})};
+            L::write(rows + col * L::PB + ((e / 8 ^ sw) << 4) + e % 8 * 2, w);
+        }
+#pragma unroll
+    for (int k = 0; k < (M * PIECES + 63) / 64; ++k) {
+        const int item = k * 64 + lane, row = item / PIECES, piece = item % PIECES;
+        T *const to = row < M ? at(row) : nullptr;
+        if (to && piece * 8 < D) *(u32x4 *)(to + piece * 8) = L::template read<u32x4>(rows + row * L::PB + ((piece ^ L::swizzle(row)) << 4));
+    }
 }
 
 // ---------------------------------------------------------------- forward
@@ -310,14 +336,14 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
     const int half = SHARE > 1 ? wave % SHARE : 0, e0 = half * DH; // which elements
     const int row0 = (at.part * (WAVES / SHARE) + wave / SHARE) * M, rows = a.Lq * a.group;
-    int row = row0 + col, pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
+    int row = row0 + col, pos = attn_position(a, row), head = at.kv * a.group + (row - pos * a.group);
     const bool there = row < rows && pos < q_len;
     const int seen = there ? (a.causal ? max(0, min(k_len, pos + off + 1)) : k_len) : 0; // keys that the column sees
     // .. and the most and the least in the wavefront
-    auto last_seen = [&](int last_row) { const int p = min(last_row, rows - 1) / a.group; return a.causal ? max(0, min(k_len, min(p, q_len - 1) + off + 1)) : k_len; };
-    const bool any = row0 < rows && row0 / a.group < q_len;
+    auto last_seen = [&](int last_row) { const int p = attn_position(a, min(last_row, rows - 1)); return a.causal ? max(0, min(k_len, min(p, q_len - 1) + off + 1)) : k_len; };
+    const bool any = row0 < rows && attn_position(a, row0) < q_len;
     const int most = any ? last_seen(row0 + M - 1) : 0;
-    const int least = row0 + M <= rows && (row0 + M - 1) / a.group < q_len ? (a.causal ? max(0, min(k_len, row0 / a.group + off + 1)) : k_len) : 0;
+    const int least = row0 + M <= rows && attn_position(a, row0 + M - 1) < q_len ? (a.causal ? max(0, min(k_len, attn_position(a, row0) + off + 1)) : k_len) : 0;
     const AttnSplit split = attn_split(attn_key_tiles(a, q_len, k_len, at.part), a.per, at.split);
     if (at.split >= split.count) return;
     const int from = split.from, to = split.to;
@@ -425,7 +451,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         }
     }
     const float sum = column_sum<M>(sums[0] + sums[1] + (sums[2] + sums[3]));
-    row = row0 + again(col), pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
+    row = row0 + again(col), pos = attn_position(a, row), head = at.kv * a.group + (row - pos * a.group);
     const float about = top == -INFINITY ? 0.f : top * c;
     if (split.count > 1) { // a part of a row: results, and their sum about 2^about
         const int64_t slot = attn_slot(a, at);
@@ -433,16 +459,24 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         store_part<M, WAVES>(a.part, slot, wave, lane, 1.f, o);
         return;
     }
-    if (row >= rows) return;
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
-    if (g == 0 && half == 0 && a.lse) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
+    if constexpr (sizeof(T) == 2 && SHARE == 1) {
+        attn_barrier(); // (everybody has read the tiles)
+        store_rows<T, L, M>(lds0 + wave * M * L::PB, lane, a.D, inv, o, [&](int r) -> T * {
+            const int at_row = row0 + r, p = attn_position(a, at_row);
+            return at_row < rows ? (T *)a.o + at.n * a.o_image + p * a.o_row + (at.kv * a.group + (at_row - p * a.group)) * a.o_head : nullptr;
+        });
+        return;
+    }
+    if (row >= rows) return;
+    T *const o_rows = (T *)a.o + at.n * a.o_image;
 #pragma unroll
     for (int d = 0; d < DH / M; ++d)
 #pragma unroll
         for (int r = 0; r < X::C; r += 4)
-            store_four<T>(o_row, e0 + d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+            store_four<T>(o_rows + pos * a.o_row + head * a.o_head, e0 + d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
 }
 
 // ---------------------------------------------------------------- backward
@@ -508,13 +542,13 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
     const int half = SHARE > 1 ? wave % SHARE : 0, e0 = half * DH; // which elements
     const int row0 = (at.part * (WAVES / SHARE) + wave / SHARE) * M, rows = a.Lq * a.group;
-    const int row = row0 + col, pos = row / a.group, head = at.kv * a.group + (row - pos * a.group);
+    const int row = row0 + col, pos = attn_position(a, row), head = at.kv * a.group + (row - pos * a.group);
     const bool here = row < rows, there = here && pos < q_len;
     const int seen = there ? (a.causal ? max(0, min(k_len, pos + off + 1)) : k_len) : 0;
-    auto last_seen = [&](int last_row) { const int p = min(last_row, rows - 1) / a.group; return a.causal ? max(0, min(k_len, min(p, q_len - 1) + off + 1)) : k_len; };
-    const bool any = row0 < rows && row0 / a.group < q_len;
+    auto last_seen = [&](int last_row) { const int p = attn_position(a, min(last_row, rows - 1)); return a.causal ? max(0, min(k_len, min(p, q_len - 1) + off + 1)) : k_len; };
+    const bool any = row0 < rows && attn_position(a, row0) < q_len;
     const int most = any ? last_seen(row0 + M - 1) : 0;
-    const int least = row0 + M <= rows && (row0 + M - 1) / a.group < q_len ? (a.causal ? max(0, min(k_len, row0 / a.group + off + 1)) : k_len) : 0;
+    const int least = row0 + M <= rows && attn_position(a, row0 + M - 1) < q_len ? (a.causal ? max(0, min(k_len, attn_position(a, row0) + off + 1)) : k_len) : 0;
     const AttnSplit split = attn_split(attn_key_tiles(a, q_len, k_len, at.part), a.per, at.split);
     if (at.split >= split.count) return;
     const int from = split.from, to = split.to;
@@ -630,7 +664,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
 }
 
 // Columns: key rows.  dv = sum over queries of P do, dk = scale sum of dS q, over all heads that share the keys.  DK, DV: which of the two (both where the
-// registers hold both).  Of the rows of 256 bytes of 16-bit types the values lie in LDS: with them in registers there are none left for operands that are on their way, and every
+// registers hold both).  Of 128 elements of 16 bits the values lie in LDS: with them in registers there are none left for operands that are on their way, and every
 // product waits for its own (2 x 4096 causal rows of 16 heads 320 us; from LDS 3 reads for two products instead of 2, TURN).
 template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, int OCC, bool DK, bool DV>
 __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs a)
@@ -639,7 +673,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     typedef Tile<T, DP> L;
     constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE, AHEAD = 4;
     constexpr int BUF = 2 * TQ * L::PB + 512; // queries, gradients, 64 log-sums, 64 deltas
-    constexpr bool FROM_LDS = DK && DV && sizeof(T) == 2 && L::PB == 256;
+    constexpr bool FROM_LDS = DK && DV && sizeof(T) == 2 && DP == 128;
     constexpr int TILES = NBUF * BUF + (FROM_LDS ? WAVES * M * L::PB : 0), SWAP = 2048;
     static_assert(TQ <= 64, "a wavefront loads a tile's log-sums at once");
     static_assert(SHARE == 1 || (BLOCKS == SHARE && X::C == 4 && TQ == STEP), "of two wavefronts each finishes the scores of one block, once a tile");
@@ -886,9 +920,12 @@ template <typename T, int DP> hipError_t attention_launch_width(int kind, const 
 
 template <typename T> hipError_t attention_launch(int kind, const AttnArgs &a, hipStream_t s)
 {
-    switch (attn_width(a.D)) {
+    switch (attn_width(sizeof(T), a.D)) {
+    case 32: return attention_launch_width<T, 32>(kind, a, s);
     case 64: return attention_launch_width<T, 64>(kind, a, s);
+    case 96: return attention_launch_width<T, 96>(kind, a, s);
     case 128: return attention_launch_width<T, 128>(kind, a, s);
+    case 192: return attention_launch_width<T, sizeof(T) == 2 ? 192 : 256>(kind, a, s);
     case 256: return attention_launch_width<T, 256>(kind, a, s);
     default: return attention_launch_width<T, 512>(kind, a, s);
     }

@@ -223,7 +223,7 @@ hipError_t launch_attention_copy(int type, bool out, const AttnRows &r, void *th
 //   16 single tokens of 32 heads over up to 8191 rows of 4: 2 106, 4 60, 8 41, [12 40], 24 52; f32, 6 heads of 60, 3 x 2257 rows: 1 299, 2 242, [3 228], 4 254
 AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num_cu)
 {
-    const int size = type_bytes(d.type), w = attn_width(width);
+    const int size = type_bytes(d.type), w = attn_width(size, width);
     const int64_t group = d.heads / d.kv_heads, columns = kind == ATTN_DKV ? d.Lk : d.Lq * group, others = kind == ATTN_DKV ? d.Lq : d.Lk;
     AttnCut c{};
     c.kind = kind;
@@ -238,7 +238,7 @@ AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num
     const double products = kind == ATTN_FORWARD ? 2.0 : kind == ATTN_DQ ? 3.0 : 4.0, rate = (size == 2 ? 1e9 : 1.2e8) / num_cu; // operations in a us of a compute unit
     const double bytes_us = 5e6 / num_cu, tile_us = std::max(products * 2.0 * h.rows() * h.tile * w / rate, few ? 2.0 * h.tile * w * size / bytes_us : 0.0), least_us = few ? 1.6 : 1.1 * tile_us;
     const double part_us = (kind == ATTN_DKV ? 2.0 : 1.0) * blocks * h.rows() * w * 8.0 / 6e6; // of a split: written, and read again
-    const int at_once = std::max(1, std::min(h.occupancy * 4 / h.waves, (160 << 10) / (h.buffers * 2 * h.tile * w * size + 1024)));
+    const int at_once = std::max(1, std::min(h.occupancy * 4 / h.waves, (160 << 10) / (h.buffers * 2 * h.tile * attn_pitch(w * size) + 1024)));
     double best = 0.0;
     for (int64_t n = 1; n <= std::min<int64_t>(tiles, 64); ++n) {
         const int64_t per = (tiles + n - 1) / n;

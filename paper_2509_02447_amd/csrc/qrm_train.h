@@ -207,15 +207,17 @@ struct AttnShape {
     constexpr int rows() const { return m * waves / share; }
 };
 enum { ATTN_FORWARD, ATTN_FEW, ATTN_DQ, ATTN_DKV }; // ATTN_FEW: forward with few query rows
-constexpr int attn_width(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 256 ? 256 : 512; }
+// Elements of a row that a kernel is made for.  (Half a row is whole pieces of 256 bytes where two wavefronts share columns: no 192 of f32.)
+constexpr int attn_width(int size, int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 && size == 2 ? 192 : D <= 256 ? 256 : 512; }
+constexpr int attn_pitch(int bytes) { return bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : bytes <= 1024 ? 1024 : 2048; } // of a row in LDS
 constexpr AttnShape attn_shape(int size, int width, int kind)
 {
-    const int bytes = size * width; // of a row
+    const int bytes = attn_pitch(size * width);
     switch (kind) {
     case ATTN_FEW:
         return bytes <= 256 ? AttnShape{32, 1, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 1, 1, 32, 2, 1} : AttnShape{16, 2, 2, 32, 1, 1};
     case ATTN_FORWARD:
-        return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 1024 ? AttnShape{size == 2 ? 16 : 32, 8, size == 2 ? 1 : 2, 32, size == 2 ? 2 : 1, 2} : AttnShape{16, 8, 2, 32, 1, 2};
+        return bytes <= 128 ? AttnShape{32, 4, 1, 64, 2, 4} : bytes == 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 1024 ? AttnShape{size == 2 ? 16 : 32, 8, size == 2 ? 1 : 2, 32, size == 2 ? 2 : 1, 2} : AttnShape{16, 8, 2, 32, 1, 2};
     case ATTN_DQ:
         return bytes <= 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{16, 4, 1, 32, 2, 2} : AttnShape{16, 8, 2, 32, bytes == 1024 ? 2 : 1, 2};
     default:
@@ -223,7 +225,7 @@ constexpr AttnShape attn_shape(int size, int width, int kind)
     }
 }
 // The registers hold the sums of dk and dv beside the keys and values, or they are two launches.
-constexpr bool attn_dk_dv_at_once(int size, int width) { return size * width <= 1024; }
+constexpr bool attn_dk_dv_at_once(int size, int width) { return attn_pitch(size * width) <= 1024; }
 struct AttnRows { // where rows [N,L,heads,D] lie
     int64_t row, head, image;
 };
@@ -241,16 +243,19 @@ struct AttnSplit {
 };
 __device__ __forceinline__ AttnSplit attn_split(int tiles, int per, int which)
 {
-    const int count = tiles <= per ? 1 : (tiles + per - 1) / per, each = (tiles + count - 1) / count;
+    if (tiles <= per) return AttnSplit{1, 0, tiles};
+    const int count = (tiles + per - 1) / per, each = (tiles + count - 1) / count;
     return AttnSplit{count, which * each, min(tiles, (which + 1) * each)};
 }
 __device__ __forceinline__ int attn_length(const int32_t *lens, int n, int all) { return lens ? max(0, min(lens[n], all)) : all; }
+// Query rows are counted position by position, the heads of a group side by side.  (A quotient takes some thirty instructions, a small launch's time.)
+__device__ __forceinline__ int attn_position(const AttnArgs &a, int row) { return a.group == 1 ? row : row / a.group; }
 // Tiles of keys that any of a part's query rows sees; tiles of a head's queries (behind `skip`) that see any of a part's keys.
 __device__ __forceinline__ int attn_key_tiles(const AttnArgs &a, int q_len, int k_len, int part)
 {
-    const int first = part * a.columns / a.group;
+    const int first = attn_position(a, part * a.columns);
     if (first >= q_len) return 0;
-    const int last = min((part * a.columns + a.columns - 1) / a.group, q_len - 1);
+    const int last = min(attn_position(a, part * a.columns + a.columns - 1), q_len - 1);
     return ((a.causal ? max(0, min(k_len, last + k_len - q_len + 1)) : k_len) + a.tile - 1) / a.tile;
 }
 __device__ __forceinline__ int attn_query_tiles(const AttnArgs &a, int q_len, int k_len, int part, int *skip)
