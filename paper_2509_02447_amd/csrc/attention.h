@@ -250,24 +250,25 @@ constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 struct AttnPlace {
     int n, kv, part, split; // image, key head, tile of rows, split of the other side
 };
-__device__ __forceinline__ bool attn_place(const AttnArgs &a, int parts, int splits, int b, AttnPlace *p)
+__device__ __forceinline__ bool attn_place(const AttnArgs &a, int b, AttnPlace *p)
 {
-    const int per = parts * splits, groups = a.N * a.kv_heads;
+    const int per = a.parts * a.splits, groups = a.N * a.kv_heads;
     int group, rest;
-    if (groups < 8 && 8 % groups == 0) {
-        group = b % 8 % groups;
-        rest = b / 8 * (8 / groups) + b % 8 / groups;
+    if (groups < 8 && (groups & (groups - 1)) == 0) {
+        const int bits = groups / 2 - (groups >> 2); // log2 of 1, 2, 4
+        group = b & (groups - 1);
+        rest = (b >> 3 << (3 - bits)) + ((b & 7) >> bits);
         if (rest >= per) return false;
     } else {
-        if (groups >= 8) b = b % 8 * ((groups * per + 7) / 8) + b / 8;
+        if (groups >= 8) b = (b & 7) * ((groups * per + 7) >> 3) + (b >> 3);
         if (b >= groups * per) return false;
-        group = b / per;
-        rest = b % per;
+        group = a.by_blocks.of(b);
+        rest = b - group * per;
     }
-    p->n = a.kv_heads == 1 ? group : group / a.kv_heads;
+    p->n = a.by_kv_heads.of(group);
     p->kv = group - p->n * a.kv_heads;
-    p->split = splits == 1 ? 0 : rest / parts;
-    p->part = rest - p->split * parts;
+    p->split = a.by_parts.of(rest);
+    p->part = rest - p->split * a.parts;
     return true;
 }
 
@@ -287,33 +288,6 @@ template <int M, int WAVES, typename ACC, int COUNT> __device__ __forceinline__ 
         for (int r = 0; r < QUADS; ++r) to[(d * QUADS + r) * 64] = f32x4{sums[d][4 * r] * by, sums[d][4 * r + 1] * by, sums[d][4 * r + 2] * by, sums[d][4 * r + 3] * by};
 }
 
-// A wavefront's results as rows in memory: through LDS (`rows`, M rows of it, nobody else's any more), so that a row leaves in pieces of 16 bytes side by side instead of
-// 8 bytes a lane.  at(row): where a row's elements begin, or null.
-template <typename T, typename L, int M, typename ACC, int COUNT, typename F>
-__device__ __forceinline__ void store_rows(uint32_t rows, int lane, int D, float by, const ACC (&sums)[COUNT], F &&at)
-{
-    typedef Mma<T, M> X;
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    typedef T pair __attribute__((ext_vector_type(2)));
-    constexpr int PIECES = COUNT * M / 8;
-    const int col = lane % M, g = lane / M, sw = L::swizzle(col);
-#pragma unroll
-    for (int d = 0; d < COUNT; ++d)
-#pragma unroll
-        for (int r = 0; r < X::C; r += 4) {
-            const int e = d * M + X::row_of(r, 0) + 4 * g; // (four of a piece's eight)
-            const u32x2 w = {__builtin_bit_cast(uint32_t, (pair){(T)(sums[d][r] * by), (T)(sums[d][r + 1] * by)}),
-                             __builtin_bit_cast(uint32_t, (pair){(T)(sums[d][r + 2] * by), (T)(sums[d][r + 3] * by)})};
-            L::write(rows + col * L::PB + ((e / 8 ^ sw) << 4) + e % 8 * 2, w);
-        }
-#pragma unroll
-    for (int k = 0; k < (M * PIECES + 63) / 64; ++k) {
-        const int item = k * 64 + lane, row = item / PIECES, piece = item % PIECES;
-        T *const to = row < M ? at(row) : nullptr;
-        if (to && piece * 8 < D) *(u32x4 *)(to + piece * 8) = L::template read<u32x4>(rows + row * L::PB + ((piece ^ L::swizzle(row)) << 4));
-    }
-}
-
 // ---------------------------------------------------------------- forward
 
 // Columns: query rows (position, head of the group).  Walks over the keys with a running maximum; the results are scaled down when it has grown by more
@@ -330,7 +304,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     static_assert(SHARE > 1 || !TURNS, "in turns there is a barrier between keys and values");
     __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
     AttnPlace at;
-    if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
+    if (!attn_place(a, blockIdx.x, &at)) return;
     if (a.causal) at.part = a.parts - 1 - at.part; // (the longest first)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
@@ -344,7 +318,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     const bool any = row0 < rows && attn_position(a, row0) < q_len;
     const int most = any ? last_seen(row0 + M - 1) : 0;
     const int least = row0 + M <= rows && attn_position(a, row0 + M - 1) < q_len ? (a.causal ? max(0, min(k_len, attn_position(a, row0) + off + 1)) : k_len) : 0;
-    const AttnSplit split = attn_split(attn_key_tiles(a, q_len, k_len, at.part), a.per, at.split);
+    const AttnSplit split = attn_split(a, attn_key_tiles(a, q_len, k_len, at.part), at.split);
     if (at.split >= split.count) return;
     const int from = split.from, to = split.to;
 
@@ -462,21 +436,13 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
     if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    if constexpr (sizeof(T) == 2 && SHARE == 1) {
-        attn_barrier(); // (everybody has read the tiles)
-        store_rows<T, L, M>(lds0 + wave * M * L::PB, lane, a.D, inv, o, [&](int r) -> T * {
-            const int at_row = row0 + r, p = attn_position(a, at_row);
-            return at_row < rows ? (T *)a.o + at.n * a.o_image + p * a.o_row + (at.kv * a.group + (at_row - p * a.group)) * a.o_head : nullptr;
-        });
-        return;
-    }
     if (row >= rows) return;
-    T *const o_rows = (T *)a.o + at.n * a.o_image;
+    T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
 #pragma unroll
     for (int d = 0; d < DH / M; ++d)
 #pragma unroll
         for (int r = 0; r < X::C; r += 4)
-            store_four<T>(o_rows + pos * a.o_row + head * a.o_head, e0 + d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+            store_four<T>(o_row, e0 + d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
 }
 
 // ---------------------------------------------------------------- backward
@@ -526,17 +492,18 @@ __device__ __forceinline__ f32x4 finish_block(bool second, const ACC (&s)[2], co
 }
 
 // Columns: query rows, as above.  dq = scale sum over keys of dS k, dS = P (do v - delta), P = exp(score - lse).
-template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF, int OCC>
-__global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs a)
+template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF> struct DqShape {
+    static constexpr int LDS = NBUF * 2 * TK * Tile<T, DP>::PB + (SHARE > 1 ? WAVES * 2048 : 0);
+};
+template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF> __device__ __forceinline__ void attention_dq(const AttnArgs &a, int block, uint8_t *lds)
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
     constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE, AHEAD = 6; // keys at a time, elements of a wavefront
     constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = 2048;
     static_assert(SHARE == 1 || (BLOCKS == SHARE && X::C == 4 && TK == STEP), "of two wavefronts each finishes the scores of one block, once a tile");
-    __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
     AttnPlace at;
-    if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
+    if (!attn_place(a, block, &at)) return;
     if (a.causal) at.part = a.parts - 1 - at.part;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
@@ -549,7 +516,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
     const bool any = row0 < rows && attn_position(a, row0) < q_len;
     const int most = any ? last_seen(row0 + M - 1) : 0;
     const int least = row0 + M <= rows && attn_position(a, row0 + M - 1) < q_len ? (a.causal ? max(0, min(k_len, attn_position(a, row0) + off + 1)) : k_len) : 0;
-    const AttnSplit split = attn_split(attn_key_tiles(a, q_len, k_len, at.part), a.per, at.split);
+    const AttnSplit split = attn_split(a, attn_key_tiles(a, q_len, k_len, at.part), at.split);
     if (at.split >= split.count) return;
     const int from = split.from, to = split.to;
 
@@ -666,20 +633,22 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dq_kernel(AttnArgs 
 // Columns: key rows.  dv = sum over queries of P do, dk = scale sum of dS q, over all heads that share the keys.  DK, DV: which of the two (both where the
 // registers hold both).  Of 128 elements of 16 bits the values lie in LDS: with them in registers there are none left for operands that are on their way, and every
 // product waits for its own (2 x 4096 causal rows of 16 heads 320 us; from LDS 3 reads for two products instead of 2, TURN).
-template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, int OCC, bool DK, bool DV>
-__global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs a)
+template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, bool DK, bool DV> struct DkvShape {
+    static constexpr bool FROM_LDS = DK && DV && sizeof(T) == 2 && DP == 128;
+    static constexpr int LDS = NBUF * (2 * TQ * Tile<T, DP>::PB + 512) + (FROM_LDS ? WAVES * M * Tile<T, DP>::PB : 0) + (SHARE > 1 ? WAVES * 2048 : 0);
+};
+template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, bool DK, bool DV> __device__ __forceinline__ void attention_dkv(const AttnArgs &a, int block, uint8_t *lds)
 {
     typedef Mma<T, M> X;
     typedef Tile<T, DP> L;
     constexpr int STEP = M > X::KK ? M : X::KK, BLOCKS = STEP / M, R = STEP / X::NG, DH = DP / SHARE, AHEAD = 4;
     constexpr int BUF = 2 * TQ * L::PB + 512; // queries, gradients, 64 log-sums, 64 deltas
-    constexpr bool FROM_LDS = DK && DV && sizeof(T) == 2 && DP == 128;
+    constexpr bool FROM_LDS = DkvShape<T, DP, M, WAVES, SHARE, TQ, NBUF, DK, DV>::FROM_LDS;
     constexpr int TILES = NBUF * BUF + (FROM_LDS ? WAVES * M * L::PB : 0), SWAP = 2048;
     static_assert(TQ <= 64, "a wavefront loads a tile's log-sums at once");
     static_assert(SHARE == 1 || (BLOCKS == SHARE && X::C == 4 && TQ == STEP), "of two wavefronts each finishes the scores of one block, once a tile");
-    __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
     AttnPlace at;
-    if (!attn_place(a, a.parts, a.splits, blockIdx.x, &at)) return;
+    if (!attn_place(a, block, &at)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % M, g = lane / M;
     const int q_len = attn_length(a.q_len, at.n, a.Lq), k_len = attn_length(a.k_len, at.n, a.Lk), off = k_len - q_len;
     const int half = SHARE > 1 ? wave % SHARE : 0, e0 = half * DH;
@@ -688,7 +657,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
     // all heads' queries one after the other
     int skip;
     const int each = attn_query_tiles(a, q_len, k_len, at.part, &skip);
-    const AttnSplit split = attn_split(each * a.group, a.per, at.split);
+    const AttnSplit split = attn_split(a, each * a.group, at.split);
     if (at.split >= split.count) return;
     const int from = split.from, to = split.to;
 
@@ -703,7 +672,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
             buffer = NBUF - 1 - buffer;
         }
     };
-    const int head0 = each ? from / each : 0;
+    const int head0 = from ? from / each : 0;
     Walk now{head0, from - head0 * each, 0}, ahead = now;
     auto load = [&](const Walk &w) {
         uint8_t *const tile = lds + w.buffer * BUF;
@@ -882,53 +851,71 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_dkv_kernel(AttnArgs
         if (a.dv) write(dv, by_v, (T *)a.dv + at.n * a.v_image + key * a.v_row + at.kv * a.v_head);
 }
 
+// Both in one launch: the first `split` workgroups do keys' gradients, which take longer, the others queries'.  What is short then fills the compute units that the
+// long leave, and a small launch's beginning and end are passed once.
+template <typename T, int DP, bool DK, bool DV>
+__global__ __launch_bounds__(attn_shape(sizeof(T), DP, ATTN_DQ).waves * 64, 2) void attention_backward_kernel(AttnArgs by_q, AttnArgs by_k, int split)
+{
+    constexpr AttnShape q = attn_shape(sizeof(T), DP, ATTN_DQ), k = attn_shape(sizeof(T), DP, ATTN_DKV);
+    static_assert(q.waves == k.waves, "one launch");
+    typedef DqShape<T, DP, q.m, q.waves, q.share, q.tile, q.buffers> Dq;
+    typedef DkvShape<T, DP, k.m, k.waves, k.share, k.tile, k.buffers, DK, DV> Dkv;
+    __shared__ alignas(256) uint8_t lds[Dq::LDS > Dkv::LDS ? Dq::LDS : Dkv::LDS];
+    if ((int)blockIdx.x < split) attention_dkv<T, DP, k.m, k.waves, k.share, k.tile, k.buffers, DK, DV>(by_k, blockIdx.x, lds);
+    else attention_dq<T, DP, q.m, q.waves, q.share, q.tile, q.buffers>(by_q, blockIdx.x - split, lds);
+}
+
 // ---------------------------------------------------------------- launches
 
-template <typename T, int DP> hipError_t attention_launch_width(int kind, const AttnArgs &a, hipStream_t s)
+// Workgroups of a launch's cut, in eights (attn_place).
+inline uint32_t attn_blocks(const AttnArgs &a) { return (uint32_t)(((int64_t)a.N * a.kv_heads * a.parts * a.splits + 7) / 8 * 8); }
+
+template <typename T, int DP> hipError_t attention_forward_width(int kind, const AttnArgs &a, hipStream_t s)
 {
-    constexpr int size = sizeof(T);
-    const int64_t groups = (int64_t)a.N * a.kv_heads, per = (int64_t)a.parts * a.splits;
-    const dim3 grid((uint32_t)((groups * per + 7) / 8 * 8)); // (attn_place)
-    switch (kind) {
-    case ATTN_FORWARD: {
-        constexpr AttnShape h = attn_shape(size, DP, ATTN_FORWARD);
-        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
-        break;
-    }
-    case ATTN_FEW: {
-        constexpr AttnShape h = attn_shape(size, DP, ATTN_FEW);
-        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
-        break;
-    }
-    case ATTN_DQ: {
-        constexpr AttnShape h = attn_shape(size, DP, ATTN_DQ);
-        hipLaunchKernelGGL((attention_dq_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy>), grid, dim3(h.waves * 64), 0, s, a);
-        break;
-    }
-    default: {
-        constexpr AttnShape h = attn_shape(size, DP, ATTN_DKV);
-        if constexpr (attn_dk_dv_at_once(size, DP)) {
-            hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy, true, true>), grid, dim3(h.waves * 64), 0, s, a);
-        } else {
-            if (a.dk) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy, true, false>), grid, dim3(h.waves * 64), 0, s, a);
-            if (a.dv) hipLaunchKernelGGL((attention_dkv_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy, false, true>), grid, dim3(h.waves * 64), 0, s, a);
-        }
-    }
+    const auto launch = [&](auto few) {
+        constexpr AttnShape h = attn_shape(sizeof(T), DP, decltype(few)::value);
+        hipLaunchKernelGGL((attention_kernel<T, DP, h.m, h.waves, h.share, h.tile, h.buffers, h.occupancy>), dim3(attn_blocks(a)), dim3(h.waves * 64), 0, s, a);
+    };
+    kind == ATTN_FEW ? launch(std::integral_constant<int, ATTN_FEW>()) : launch(std::integral_constant<int, ATTN_FORWARD>());
+    return hipGetLastError();
+}
+
+template <typename T, int DP> hipError_t attention_backward_width(const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s)
+{
+    const dim3 threads(attn_shape(sizeof(T), DP, ATTN_DQ).waves * 64);
+    const auto launch = [&](auto dk, auto dv, bool keys, bool queries) {
+        const uint32_t first = keys ? attn_blocks(by_k) : 0, blocks = first + (queries ? attn_blocks(by_q) : 0);
+        if (blocks) hipLaunchKernelGGL((attention_backward_kernel<T, DP, decltype(dk)::value, decltype(dv)::value>), dim3(blocks), threads, 0, s, by_q, by_k, (int)first);
+    };
+    if constexpr (attn_dk_dv_at_once(sizeof(T), DP)) {
+        launch(std::true_type(), std::true_type(), by_k.dk || by_k.dv, by_q.dq);
+    } else {
+        if (by_k.dk || by_q.dq) launch(std::true_type(), std::false_type(), by_k.dk, by_q.dq);
+        if (by_k.dv) launch(std::false_type(), std::true_type(), true, false);
     }
     return hipGetLastError();
 }
 
-template <typename T> hipError_t attention_launch(int kind, const AttnArgs &a, hipStream_t s)
+// Calls f with the width of a kernel for rows of D elements.
+template <typename T, typename F> hipError_t attention_with_width(int D, F &&f)
 {
-    switch (attn_width(sizeof(T), a.D)) {
-    case 32: return attention_launch_width<T, 32>(kind, a, s);
-    case 64: return attention_launch_width<T, 64>(kind, a, s);
-    case 96: return attention_launch_width<T, 96>(kind, a, s);
-    case 128: return attention_launch_width<T, 128>(kind, a, s);
-    case 192: return attention_launch_width<T, sizeof(T) == 2 ? 192 : 256>(kind, a, s);
-    case 256: return attention_launch_width<T, 256>(kind, a, s);
-    default: return attention_launch_width<T, 512>(kind, a, s);
+    switch (attn_width(sizeof(T), D)) {
+    case 32: return f(std::integral_constant<int, 32>());
+    case 64: return f(std::integral_constant<int, 64>());
+    case 96: return f(std::integral_constant<int, 96>());
+    case 128: return f(std::integral_constant<int, 128>());
+    case 192: return f(std::integral_constant<int, sizeof(T) == 2 ? 192 : 256>());
+    case 256: return f(std::integral_constant<int, 256>());
+    default: return f(std::integral_constant<int, 512>());
     }
+}
+template <typename T> hipError_t attention_forward(int kind, const AttnArgs &a, hipStream_t s)
+{
+    return attention_with_width<T>(a.D, [&](auto width) { return attention_forward_width<T, decltype(width)::value>(kind, a, s); });
+}
+template <typename T> hipError_t attention_backward(const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s)
+{
+    return attention_with_width<T>(by_q.D, [&](auto width) { return attention_backward_width<T, decltype(width)::value>(by_q, by_k, s); });
 }
 
 } // namespace qrm

@@ -9,6 +9,9 @@ namespace qrm {
 hipError_t launch_attention_f32(int kind, const AttnArgs &a, hipStream_t s);
 hipError_t launch_attention_bf16(int kind, const AttnArgs &a, hipStream_t s);
 hipError_t launch_attention_f16(int kind, const AttnArgs &a, hipStream_t s);
+hipError_t launch_attention_backward_f32(const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s);
+hipError_t launch_attention_backward_bf16(const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s);
+hipError_t launch_attention_backward_f16(const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s);
 
 namespace {
 
@@ -67,13 +70,13 @@ template <typename T> __device__ __forceinline__ void join_part(const AttnArgs &
     const int q_len = attn_length(a.q_len, n, a.Lq), k_len = attn_length(a.k_len, n, a.Lk);
     int skip;
     const int tiles = j.keys ? attn_query_tiles(a, q_len, k_len, part, &skip) * a.group : attn_key_tiles(a, q_len, k_len, part);
-    const int splits = attn_split(tiles, a.per, 0).count;
+    const int splits = attn_split(a, tiles, 0).count;
     if (splits == 1) return;
     // the lane's columns and elements: as in store_part and Mma::row_of
     const int item = (int)(t - which * j.per), lane = item % 64, ng = 64 / h.m, quads = h.m * h.m / 256, each = j.width / h.share, blocks = each / h.m * quads;
     const int wave = item / 64 / blocks, block = item / 64 % blocks, column = wave / h.share * h.m + lane % h.m;
     const int d = wave % h.share * each + block / quads * h.m + (block % quads * ng + lane / h.m) * 4;
-    const int r = part * a.columns + column, pos = j.keys ? r : r / a.group, head = j.keys ? kv : kv * a.group + r % a.group;
+    const int r = part * a.columns + column, pos = j.keys ? r : attn_position(a, r), head = j.keys ? kv : kv * a.group + (r - pos * a.group);
     if (pos >= (j.keys ? a.Lk : a.Lq) || d >= a.D) return;
     const int64_t apart = (int64_t)a.N * a.kv_heads * a.parts; // slots from one split to the next
     const f32x4 *const from = (const f32x4 *)j.part + t;
@@ -142,6 +145,11 @@ __global__ __launch_bounds__(kThreads) void attention_copy_kernel(AttnRows rows,
 hipError_t launch_attention(int type, int kind, const AttnArgs &a, hipStream_t s)
 {
     return type == QRM_F32 ? launch_attention_f32(kind, a, s) : type == QRM_BF16 ? launch_attention_bf16(kind, a, s) : launch_attention_f16(kind, a, s);
+}
+
+hipError_t launch_attention_backward(int type, const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s)
+{
+    return type == QRM_F32 ? launch_attention_backward_f32(by_q, by_k, s) : type == QRM_BF16 ? launch_attention_backward_bf16(by_q, by_k, s) : launch_attention_backward_f16(by_q, by_k, s);
 }
 
 hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, const void *dy, const float *lse, const int32_t *q_len, float *row_lse, float *row_delta, hipStream_t s)

@@ -185,6 +185,19 @@ hipError_t launch_scale_grads(int type, const AdamwTensor *tensors, const uint2 
 
 // ---- attention
 
+// Quotients by a number that a launch keeps, of numbers below 2^31: the high half of a product with ceil(2^(31 + s) / d), s = ceil(log2 d), which is exact for them; a
+// division takes thirty instructions, and a workgroup begins with a dozen.
+struct Quotient {
+    uint32_t by, factor;
+    int shift;
+    Quotient() = default;
+    explicit Quotient(uint32_t d) : by(d), factor(0), shift(0)
+    {
+        while (((uint64_t)1 << shift) < d) ++shift;
+        if (shift) factor = (uint32_t)((((uint64_t)1 << (31 + shift)) + d - 1) / d);
+    }
+    __device__ __forceinline__ int of(int n) const { return shift ? (int)(__umulhi((uint32_t)n, factor) >> (shift - 1)) : n; }
+};
 struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie on 16 bytes and are a multiple of them (launch_attention_copy)
     const void *q, *k, *v, *dy;
     void *o, *dq, *dk, *dv;
@@ -196,7 +209,8 @@ struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie
     int64_t q_row, q_head, q_image, k_row, k_head, k_image, v_row, v_head, v_image, o_row, o_head, o_image;
     int N, Lq, Lk, heads, kv_heads, group, D;
     int parts, splits, per;            // of the launch: tiles of the columns' rows, the most splits of the other side, and its tiles in one
-    int columns, tile;                 // rows of a part, of a tile of the other side
+    int columns, tile_shift;           // rows of a part, of a tile of the other side (2 to that)
+    Quotient by_group, by_kv_heads, by_parts, by_blocks, by_per; // by_blocks: parts * splits
     float scale;
     bool causal;
 };
@@ -241,32 +255,33 @@ struct AttnCut {
 struct AttnSplit {
     int count, from, to;
 };
-__device__ __forceinline__ AttnSplit attn_split(int tiles, int per, int which)
+__device__ __forceinline__ AttnSplit attn_split(const AttnArgs &a, int tiles, int which)
 {
-    if (tiles <= per) return AttnSplit{1, 0, tiles};
-    const int count = (tiles + per - 1) / per, each = (tiles + count - 1) / count;
+    if (tiles <= a.per) return AttnSplit{1, 0, tiles};
+    const int count = a.by_per.of(tiles + a.per - 1), each = (tiles + count - 1) / count;
     return AttnSplit{count, which * each, min(tiles, (which + 1) * each)};
 }
 __device__ __forceinline__ int attn_length(const int32_t *lens, int n, int all) { return lens ? max(0, min(lens[n], all)) : all; }
-// Query rows are counted position by position, the heads of a group side by side.  (A quotient takes some thirty instructions, a small launch's time.)
-__device__ __forceinline__ int attn_position(const AttnArgs &a, int row) { return a.group == 1 ? row : row / a.group; }
+// Query rows are counted position by position, the heads of a group side by side.
+__device__ __forceinline__ int attn_position(const AttnArgs &a, int row) { return a.by_group.of(row); }
 // Tiles of keys that any of a part's query rows sees; tiles of a head's queries (behind `skip`) that see any of a part's keys.
 __device__ __forceinline__ int attn_key_tiles(const AttnArgs &a, int q_len, int k_len, int part)
 {
     const int first = attn_position(a, part * a.columns);
     if (first >= q_len) return 0;
     const int last = min(attn_position(a, part * a.columns + a.columns - 1), q_len - 1);
-    return ((a.causal ? max(0, min(k_len, last + k_len - q_len + 1)) : k_len) + a.tile - 1) / a.tile;
+    return ((a.causal ? max(0, min(k_len, last + k_len - q_len + 1)) : k_len) + (1 << a.tile_shift) - 1) >> a.tile_shift;
 }
 __device__ __forceinline__ int attn_query_tiles(const AttnArgs &a, int q_len, int k_len, int part, int *skip)
 {
     const int base = part * a.columns;
-    *skip = a.causal ? max(0, base - (k_len - q_len)) / a.tile : 0;
-    return base < k_len ? max(0, (q_len + a.tile - 1) / a.tile - *skip) : 0;
+    *skip = a.causal ? max(0, base - (k_len - q_len)) >> a.tile_shift : 0;
+    return base < k_len ? max(0, ((q_len + (1 << a.tile_shift) - 1) >> a.tile_shift) - *skip) : 0;
 }
 // width: D rounded up to 16 bytes.
 AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num_cu);
-hipError_t launch_attention(int type, int kind, const AttnArgs &a, hipStream_t s); // kind ATTN_DKV: dk, dv, whichever is not null
+hipError_t launch_attention(int type, int kind, const AttnArgs &a, hipStream_t s); // forward
+hipError_t launch_attention_backward(int type, const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s); // dq, dk and dv, those that are not null
 // Backward, before all else: row_lse and row_delta of lse, o and dy.
 hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, const void *dy, const float *lse, const int32_t *q_len, float *row_lse, float *row_delta, hipStream_t s);
 // Behind launches with splits: what they have left, into o and lse, or into dq, dk and dv (those that are not null and were split).

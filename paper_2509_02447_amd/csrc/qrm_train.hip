@@ -206,7 +206,10 @@ AttnArgs attention_args(const AttnCheck &a, const AttnTensor &q, const AttnTenso
 void cut_to(AttnArgs *g, const AttnCut &cut)
 {
     g->parts = cut.parts, g->splits = cut.splits, g->per = cut.per;
-    g->columns = cut.shape.rows(), g->tile = cut.shape.tile;
+    g->columns = cut.shape.rows();
+    for (g->tile_shift = 0; 1 << g->tile_shift < cut.shape.tile;) ++g->tile_shift;
+    g->by_parts = Quotient(std::max(1, cut.parts)), g->by_blocks = Quotient(std::max(1, cut.parts * cut.splits)), g->by_per = Quotient(cut.per);
+    g->by_group = Quotient(g->group), g->by_kv_heads = Quotient(g->kv_heads);
 }
 
 } // namespace
@@ -600,8 +603,7 @@ qrm_status qrm_attention_backward(qrm_ctx *c, const qrm_attention_desc *desc, co
     AttnArgs gq = g, gk = g;
     cut_to(&gq, by_q);
     cut_to(&gk, by_k);
-    if (e == hipSuccess && d_dq) e = launch_attention(d.type, ATTN_DQ, gq, s);
-    if (e == hipSuccess && (d_dk || d_dv)) e = launch_attention(d.type, ATTN_DKV, gk, s);
+    if (e == hipSuccess) e = launch_attention_backward(d.type, gq, gk, s);
     if (e == hipSuccess) e = launch_attention_add(d.type, gq, by_q, gk, by_k, s);
     back(q, a.q, d_dq, g.dq, d.Lq, d.heads);
     back(k, a.k, d_dk, g.dk, d.Lk, d.kv_heads);
