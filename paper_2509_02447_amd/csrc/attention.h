@@ -255,7 +255,7 @@ __device__ __forceinline__ bool attn_place(const AttnArgs &a, int b, AttnPlace *
     const int per = a.parts * a.splits, groups = a.N * a.kv_heads;
     int group, rest;
     if (groups < 8 && (groups & (groups - 1)) == 0) {
-        const int bits = groups / 2 - (groups >> 2); // log2 of 1, 2, 4
+        const int bits = __builtin_ctz(groups);
         group = b & (groups - 1);
         rest = (b >> 3 << (3 - bits)) + ((b & 7) >> bits);
         if (rest >= per) return false;

@@ -221,42 +221,91 @@ hipError_t launch_attention_copy(int type, bool out, const AttnRows &r, void *th
     });
 }
 
-// Splits of the other side: as many as a model of times says is best.  Tiles take what the matrix products take at the rate that the kernels reach on a full card (1e15
-// operations a second, f32 1.2e14), for few rows what the memory takes (5 TB/s) and 1.6 us at least; a compute unit has its workgroups' tiles one after the other, and 4 us for
-// the beginning and end of those that it has at a time.  Where causal, parts differ: the longest workgroup bounds the launch, and the compute units are not done at one time (0.4 of the longest
-// behind their average).  The join is a launch (5 us) that reads what the splits write (6 TB/s, both).  Measured, us, by number of splits (the rule's in brackets):
-//   one head of 512, bf16, forward, 4 x 1024 rows: 1 66, 2 52, [4 40], 8 43; 4 x 4096 rows: 1 233, [2 169], 3 206, 4 180; backward, dq 4 x 1024: 1 134, 2 110, [4 97], 8 111
-//   (all of the call); dk and dv: 1 152, 2 112, [4 93], 8 116
-//   16 heads of 128, 4 key heads, causal: forward, 2 x 8192 rows [1 511], 2 645; backward, 2 x 4096, dk and dv: 1 831, 2 620, 3 549, [6 530], 12 554
-//   16 single tokens of 32 heads over up to 8191 rows of 4: 2 106, 4 60, 8 41, [12 40], 24 52; f32, 6 heads of 60, 3 x 2257 rows: 1 299, 2 242, [3 228], 4 254
-AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num_cu)
-{
-    const int size = type_bytes(d.type), w = attn_width(size, width);
-    const int64_t group = d.heads / d.kv_heads, columns = kind == ATTN_DKV ? d.Lk : d.Lq * group, others = kind == ATTN_DKV ? d.Lq : d.Lk;
-    AttnCut c{};
-    c.kind = kind;
-    c.width = w;
-    if (kind == ATTN_FORWARD && columns <= attn_shape(size, w, ATTN_FEW).rows()) c.kind = ATTN_FEW;
-    const bool few = c.kind == ATTN_FEW;
-    const AttnShape h = c.shape = attn_shape(size, w, c.kind);
-    c.parts = (int)((columns + h.rows() - 1) / h.rows());
-    const int64_t tiles = std::max<int64_t>(1, (others + h.tile - 1) / h.tile * (kind == ATTN_DKV ? group : 1)), blocks = std::max<int64_t>(1, d.N * d.kv_heads * c.parts);
-    // the share of the tiles that a part sees on average where causal: of Lq x Lk, all but a triangle
-    const double lq = (double)d.Lq, lk = (double)d.Lk, seen = std::min(lq, lk), share = !d.causal || few || lq * lk == 0.0 ? 1.0 : seen * (lk - 0.5 * seen) / (lq * lk);
-    const double products = kind == ATTN_FORWARD ? 2.0 : kind == ATTN_DQ ? 3.0 : 4.0, rate = (size == 2 ? 1e9 : 1.2e8) / num_cu; // operations in a us of a compute unit
-    const double bytes_us = 5e6 / num_cu, tile_us = std::max(products * 2.0 * h.rows() * h.tile * w / rate, few ? 2.0 * h.tile * w * size / bytes_us : 0.0), least_us = few ? 1.6 : 1.1 * tile_us;
-    const double part_us = (kind == ATTN_DKV ? 2.0 : 1.0) * blocks * h.rows() * w * 8.0 / 6e6; // of a split: written, and read again
-    const int at_once = std::max(1, std::min(h.occupancy * 4 / h.waves, (160 << 10) / (h.buffers * 2 * h.tile * attn_pitch(w * size) + 1024)));
-    double best = 0.0;
-    for (int64_t n = 1; n <= std::min<int64_t>(tiles, 64); ++n) {
-        const int64_t per = (tiles + n - 1) / n;
-        if ((tiles + per - 1) / per != n) continue;
-        const double all = blocks * (share < 1.0 ? std::max(1.0, n * share + 0.5) : (double)n), on_one = std::ceil(all / num_cu), longest = per * least_us;
-        const double work = share < 1.0 ? blocks * tiles * share * tile_us / num_cu + 0.4 * longest : on_one * per * tile_us;
-        const double us = std::max(work, longest) + std::ceil(on_one / at_once) * 4.0 + (n > 1 ? 5.0 + part_us * n * share : 0.0);
-        if (n == 1 || us < best) best = us, c.splits = (int)n, c.per = (int)per;
+// How a call is cut: a model of times in us.  Tiles take what the matrix products take at the rate that the kernels reach on a full card (1e15 operations a second,
+// f32 1.2e14), for few rows what the memory takes (5 TB/s) and 1.6 us at least; a compute unit has its workgroups' tiles one after the other, and 4 us for the beginning and end
+// of those that it has at a time.  Where parts differ (causal, keys' gradients beside queries'), the longest workgroup bounds the launch, and the compute units are not done at one time:
+// 0.4 of the longest behind their average.  The join is a launch (5 us) that reads what the splits write (6 TB/s, both).
+namespace {
+
+struct CutModel {
+    AttnCut cut;
+    int64_t tiles, blocks;
+    double share;    // of the tiles that a part sees on average where causal: of Lq x Lk, all but a triangle
+    double tile_us, least_us, part_us;
+    int at_once;     // workgroups on a compute unit
+    int num_cu;
+    CutModel(const qrm_attention_desc &d, int width, int kind, int cus) : cut{}, num_cu(cus)
+    {
+        const int size = type_bytes(d.type), w = cut.width = attn_width(size, width);
+        const bool keys = kind == ATTN_DKV;
+        const int64_t group = d.heads / d.kv_heads, columns = keys ? d.Lk : d.Lq * group, others = keys ? d.Lq : d.Lk;
+        cut.kind = kind == ATTN_FORWARD && columns <= attn_shape(size, w, ATTN_FEW).rows() ? ATTN_FEW : kind;
+        const bool few = cut.kind == ATTN_FEW;
+        const AttnShape h = cut.shape = attn_shape(size, w, cut.kind);
+        cut.parts = (int)((columns + h.rows() - 1) / h.rows());
+        tiles = std::max<int64_t>(1, (others + h.tile - 1) / h.tile * (keys ? group : 1));
+        blocks = d.N * d.kv_heads * cut.parts;
+        const double lq = (double)d.Lq, lk = (double)d.Lk, seen = std::min(lq, lk);
+        share = !d.causal || few || seen == 0.0 ? 1.0 : seen * (lk - 0.5 * seen) / (lq * lk);
+        const double products = kind == ATTN_FORWARD ? 2.0 : kind == ATTN_DQ ? 3.0 : 4.0, rate = (size == 2 ? 1e9 : 1.2e8) / num_cu;
+        tile_us = std::max(products * 2.0 * h.rows() * h.tile * w / rate, few ? 2.0 * h.tile * w * size / (5e6 / num_cu) : 0.0);
+        least_us = few ? 1.6 : 1.1 * tile_us;
+        part_us = (keys ? 2.0 : 1.0) * blocks * h.rows() * w * 8.0 / 6e6;
+        at_once = std::max(1, std::min(h.occupancy * 4 / h.waves, (160 << 10) / (h.buffers * 2 * h.tile * attn_pitch(w * size) + 1024)));
+        split(1);
     }
-    return c;
+    // n splits, or as many as its tiles make
+    void split(int64_t n)
+    {
+        n = std::min(n, tiles);
+        cut.per = (int)((tiles + n - 1) / n);
+        cut.splits = (int)((tiles + cut.per - 1) / cut.per);
+    }
+    double workgroups() const { return blocks * (share < 1.0 ? std::max(1.0, cut.splits * share + 0.5) : (double)cut.splits); }
+    double longest() const { return cut.per * least_us; }
+    double work() const { return blocks * tiles * share * tile_us / num_cu; }
+    double join() const { return cut.splits > 1 ? part_us * cut.splits * share : 0.0; }
+};
+constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+
+} // namespace
+
+// Measured, us, by number of splits (the rule's in brackets): one head of 512, bf16, 4 x 1024 rows 1 66, 2 52, [4 40], 8 43; 4 x 4096 rows 1 233, [2 169], 3 206, 4 180; 16 heads of 128, 4
+// key heads, causal, 2 x 8192 rows [1 511], 2 645; 16 single tokens of 32 heads over up to 8191 rows of 4: 2 106, 4 60, [8 41], 12 40, 24 52; f32, 6 heads of 60, 3 x 2257 rows 1 299,
+// 2 242, [3 228], 4 254.
+AttnCut plan_attention(const qrm_attention_desc &d, int width, int num_cu)
+{
+    CutModel m(d, width, ATTN_FORWARD, num_cu), best = m;
+    double least = 0.0;
+    for (int n : kSplits) {
+        if (n > m.tiles) break;
+        m.split(n);
+        const double on_one = std::ceil(m.workgroups() / num_cu), work = m.share < 1.0 ? m.work() + 0.4 * m.longest() : on_one * m.cut.per * m.tile_us;
+        const double us = std::max(work, m.longest()) + std::ceil(on_one / m.at_once) * 4.0 + (m.cut.splits > 1 ? 5.0 + m.join() : 0.0);
+        if (n == 1 || us < least) least = us, best = m;
+    }
+    return best.cut;
+}
+
+// Both sides of a backward launch, whatever of it is wanted: a gradient's bits do not depend on the others.  Measured, us of the call, by splits of queries' / keys' side: 16 heads of 128, 4 key
+// heads, 2 x 4096 causal rows 1/1 667, 1/2 530, [1/3 490], 2/3 517, 1/4 495; one head of 512, 4 x 1024 rows 1/1 115, [1/2 87], 2/2 82, 2/4 99; f16, 5 x 777 rows over 1033, 8 heads of 96, 2 key
+// heads 1/1 123, 1/3 68, [1/4 69], 2/4 65.
+void plan_attention_backward(const qrm_attention_desc &d, int width, int num_cu, AttnCut *by_q, AttnCut *by_k)
+{
+    CutModel q(d, width, ATTN_DQ, num_cu), k(d, width, ATTN_DKV, num_cu);
+    double least = 0.0;
+    bool any = false;
+    for (int n : kSplits) {
+        if (n > q.tiles) break;
+        q.split(n);
+        for (int m : kSplits) {
+            if (m > k.tiles) break;
+            k.split(m);
+            const double work = q.work() + k.work(), longest = std::max(q.longest(), k.longest()), workgroups = q.workgroups() + k.workgroups();
+            const double us = std::max(work + 0.4 * longest, longest) + std::ceil(workgroups / num_cu / std::min(q.at_once, k.at_once)) * 4.0 + (n > 1 || m > 1 ? 5.0 + q.join() + k.join() : 0.0);
+            if (!any || us < least) least = us, any = true, *by_q = q.cut, *by_k = k.cut;
+        }
+    }
 }
 
 } // namespace qrm

@@ -279,7 +279,8 @@ __device__ __forceinline__ int attn_query_tiles(const AttnArgs &a, int q_len, in
     return base < k_len ? max(0, ((q_len + (1 << a.tile_shift) - 1) >> a.tile_shift) - *skip) : 0;
 }
 // width: D rounded up to 16 bytes.
-AttnCut plan_attention(const qrm_attention_desc &d, int width, int kind, int num_cu);
+AttnCut plan_attention(const qrm_attention_desc &d, int width, int num_cu);
+void plan_attention_backward(const qrm_attention_desc &d, int width, int num_cu, AttnCut *by_q, AttnCut *by_k);
 hipError_t launch_attention(int type, int kind, const AttnArgs &a, hipStream_t s); // forward
 hipError_t launch_attention_backward(int type, const AttnArgs &by_q, const AttnArgs &by_k, hipStream_t s); // dq, dk and dv, those that are not null
 // Backward, before all else: row_lse and row_delta of lse, o and dy.

@@ -515,7 +515,7 @@ qrm_status qrm_attention(qrm_ctx *c, const qrm_attention_desc *desc, const void 
     const int size = type_bytes(d.type);
     if (common_alignment({d_q, d_k, d_v, d_o}) < size || !aligned_to(d_lse, 4) || !aligned_to(d_q_len, 4) || !aligned_to(d_k_len, 4))
         return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
-    const AttnCut cut = plan_attention(d, a.wide, ATTN_FORWARD, c->num_cu);
+    const AttnCut cut = plan_attention(d, a.wide, c->num_cu);
     Workspace w;
     const AttnTensor q = place(a, a.q, d.Lq, d.heads, {d_q}, 1, &w), k = place(a, a.k, d.Lk, d.kv_heads, {d_k}, 1, &w), v = place(a, a.v, d.Lk, d.kv_heads, {d_v}, 1, &w),
                      o = place(a, a.o, d.Lq, d.heads, {d_o}, 1, &w);
@@ -568,7 +568,8 @@ qrm_status qrm_attention_backward(qrm_ctx *c, const qrm_attention_desc *desc, co
     const int size = type_bytes(d.type);
     if (common_alignment({d_q, d_k, d_v, d_o, d_do, d_dq, d_dk, d_dv}) < size || !aligned_to(d_lse, 4) || !aligned_to(d_q_len, 4) || !aligned_to(d_k_len, 4))
         return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
-    const AttnCut by_q = plan_attention(d, a.wide, ATTN_DQ, c->num_cu), by_k = plan_attention(d, a.wide, ATTN_DKV, c->num_cu);
+    AttnCut by_q{}, by_k{};
+    plan_attention_backward(d, a.wide, c->num_cu, &by_q, &by_k);
     Workspace w;
     const size_t q_rows = (size_t)d.N * d.heads * d.Lq, k_rows = (size_t)d.N * d.kv_heads * d.Lk;
     // (a copied tensor's gradient is written behind its copy)
