@@ -85,6 +85,7 @@ template <typename T> __device__ __forceinline__ void join_part(const AttnArgs &
     if (j.sums) {
         const float2 *const sums = j.sums + which * a.columns + column;
         float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
         for (int k = 0; k < splits; ++k) top = fmaxf(top, sums[k * apart * a.columns].x);
 #pragma unroll 4
         for (int k = 0; k < splits; ++k) {
@@ -239,7 +240,7 @@ struct CutModel {
         const int size = type_bytes(d.type), w = cut.width = attn_width(size, width);
         const bool keys = kind == ATTN_DKV;
         const int64_t group = d.heads / d.kv_heads, columns = keys ? d.Lk : d.Lq * group, others = keys ? d.Lq : d.Lk;
-        cut.kind = kind == ATTN_FORWARD && columns <= attn_shape(size, w, ATTN_FEW).rows() ? ATTN_FEW : kind;
+        cut.kind = kind == ATTN_FORWARD && columns <= kAttnFew ? ATTN_FEW : kind;
         const bool few = cut.kind == ATTN_FEW;
         const AttnShape h = cut.shape = attn_shape(size, w, cut.kind);
         cut.parts = (int)((columns + h.rows() - 1) / h.rows());

@@ -220,7 +220,9 @@ struct AttnShape {
     int m, waves, share, tile, buffers, occupancy;
     constexpr int rows() const { return m * waves / share; }
 };
-enum { ATTN_FORWARD, ATTN_FEW, ATTN_DQ, ATTN_DKV }; // ATTN_FEW: forward with few query rows
+enum { ATTN_FORWARD, ATTN_FEW, ATTN_DQ, ATTN_DKV }; // ATTN_FEW: forward with up to kAttnFew query rows to a key head
+// (they fill no workgroup of four wavefronts: 16 single tokens of 8 heads to a key head 41 us with 32 columns to a wavefront, 38 with 16)
+constexpr int kAttnFew = 32;
 // Elements of a row that a kernel is made for.  (Half a row is whole pieces of 256 bytes where two wavefronts share columns: no 192 of f32.)
 constexpr int attn_width(int size, int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 && size == 2 ? 192 : D <= 256 ? 256 : 512; }
 constexpr int attn_pitch(int bytes) { return bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : bytes <= 1024 ? 1024 : 2048; } // of a row in LDS
@@ -229,7 +231,7 @@ constexpr AttnShape attn_shape(int size, int width, int kind)
     const int bytes = attn_pitch(size * width);
     switch (kind) {
     case ATTN_FEW:
-        return bytes <= 256 ? AttnShape{32, 1, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 1, 1, 32, 2, 1} : AttnShape{16, 2, 2, 32, 1, 1};
+        return bytes <= 256 ? AttnShape{16, 1, 1, 32, 2, 2} : bytes == 512 ? AttnShape{16, 1, 1, 32, 2, 1} : AttnShape{16, 2, 2, 32, 1, 1};
     case ATTN_FORWARD:
         return bytes <= 128 ? AttnShape{32, 4, 1, 64, 2, 4} : bytes == 256 ? AttnShape{32, 4, 1, 64, 2, 2} : bytes == 512 ? AttnShape{32, 4, 1, 32, 2, 2} : bytes == 1024 ? AttnShape{size == 2 ? 16 : 32, 8, size == 2 ? 1 : 2, 32, size == 2 ? 2 : 1, 2} : AttnShape{16, 8, 2, 32, 1, 2};
     case ATTN_DQ:
