@@ -5,9 +5,10 @@ Reed-Solomon code word, a term that keeps the images near what they were, AdamW 
 any others do: crop, extractor, Reed-Solomon decoding and the comparison with the key.
 
 The group norms, the message loss and the optimiser are the library's (qrm_group_norm, qrm_group_norm_backward, qrm_message_loss, qrm_adamw_step); convolutions are
-plain matrix products of torch, which also differentiates them.
+plain matrix products of torch, which also differentiates them.  With --attention the decoder's pixels also look at each other between the residual blocks
+(qrm_attention, qrm_attention_backward); with --clip the gradients' norm is bounded (qrm_adamw_grad_norm).
 
-    python examples/finetune_decoder.py [--steps 200] [--bits 8]
+    python examples/finetune_decoder.py [--steps 200] [--bits 8] [--attention] [--clip 1.0]
 """
 from __future__ import annotations
 
@@ -65,6 +66,28 @@ class NormAct(torch.autograd.Function):
         return *(Once.apply(g, x, gamma, beta, dy) for g in (dx, dgamma, dbeta)), None, None
 
 
+class Attend(torch.autograd.Function):
+    """Softmax attention of q [N,Lq,H,D] over k, v [N,Lk,KV,D] through the library; lengths i32 [N] of queries and keys, or None."""
+
+    @staticmethod
+    def forward(fn, q, k, v, ctx, causal, q_len, k_len):
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        n, lq, heads, d = q.shape
+        fn.desc = qrm.attention_desc(n, lq, k.shape[1], heads, k.shape[2], d, q.dtype, causal)
+        o, lse = torch.empty_like(q), q.new_empty((n, heads, lq), dtype=torch.float32)
+        ctx.qrm_attention(fn.desc, q, k, v, o, lse, q_len, k_len)
+        fn.ctx, fn.lens = ctx, (q_len, k_len)
+        fn.save_for_backward(q, k, v, o, lse)
+        return o
+
+    @staticmethod
+    def backward(fn, do):
+        q, k, v, o, lse = fn.saved_tensors
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        fn.ctx.qrm_attention_backward(fn.desc, q, k, v, o, do.contiguous(), lse, dq, dk, dv, *fn.lens)
+        return *(Once.apply(g, q, k, v, do) for g in (dq, dk, dv)), None, None, None, None
+
+
 class MessageLoss(torch.autograd.Function):
     """The library's message loss of logits [N,BITS] against one target for all; its gradient comes with it."""
 
@@ -90,9 +113,9 @@ def conv3x3(x, w):
 
 
 class Decoder:
-    """Latents [N,16,16,8] -> images [N,32,32,3] in 0..1: two residual blocks, doubling, one more block."""
+    """Latents [N,16,16,8] -> images [N,32,32,3] in 0..1: two residual blocks, doubling, one more block; with attention between the two of four heads of 16."""
 
-    def __init__(self, gen):
+    def __init__(self, gen, attention=False):
         def conv(cin, cout, gain=1.0):
             return (torch.randn((9 * cin, cout), generator=gen, device="cuda") * (gain * math.sqrt(2.0 / (9 * cin)))).requires_grad_()
 
@@ -102,11 +125,21 @@ class Decoder:
         self.up = (ones(64), zeros(64), conv(64, 32))
         self.last = (ones(32), zeros(32), conv(32, 3, 0.5))
         self.params = [self.first] + [p for b in self.blocks for p in b] + list(self.up) + list(self.last)
+        self.look = None
+        if attention:
+            mix = lambda cout, gain: (torch.randn((64, cout), generator=gen, device="cuda") * (gain / 8.0)).requires_grad_()
+            self.look = (ones(64), zeros(64), mix(192, 1.0), mix(64, 0.5))
+            self.params += list(self.look)
 
     def __call__(self, z, ctx):
         x = conv3x3(z, self.first)
-        for gamma, beta, w in self.blocks:
+        for i, (gamma, beta, w) in enumerate(self.blocks):
             x = x + conv3x3(NormAct.apply(x, gamma, beta, ctx, 16), w)
+            if self.look is not None and i == 0:
+                gamma, beta, into, out = self.look
+                n, h, wd, _ = x.shape
+                q, k, v = (NormAct.apply(x, gamma, beta, ctx, 16).reshape(n, h * wd, 64) @ into).view(n, h * wd, 3, 4, 16).unbind(2)
+                x = x + (Attend.apply(q, k, v, ctx, False, None, None).reshape(n, h * wd, 64) @ out).view(n, h, wd, 64)
         x = NormAct.apply(x, self.up[0], self.up[1], ctx, 16)
         x = conv3x3(x.repeat_interleave(2, dim=1).repeat_interleave(2, dim=2), self.up[2])
         return torch.sigmoid(conv3x3(NormAct.apply(x, self.last[0], self.last[1], ctx, 8), self.last[2]))
@@ -180,10 +213,10 @@ def detect(ctx, images):
     return bits, nerr, matches, found
 
 
-def main(steps=200, batch=4, moment_bits=8, peak_lr=5e-3, rs_weight=0.05, fidelity=10.0, seed=0, report=print):
+def main(steps=200, batch=4, moment_bits=8, peak_lr=5e-3, rs_weight=0.05, fidelity=10.0, seed=0, report=print, attention=False, clip=0.0):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     rng = np.random.default_rng(seed)
-    decoder, weights = Decoder(gen), extractor_weights(rng)
+    decoder, weights = Decoder(gen, attention), extractor_weights(rng)
     code = qrm.Context(rs=CODE)
 
     # the extractor's linear layer is made to whiten what the extractor sees in images of this decoder and in noisy ones: every bit then starts as a fair
@@ -222,6 +255,7 @@ def main(steps=200, batch=4, moment_bits=8, peak_lr=5e-3, rs_weight=0.05, fideli
     before = decoder(held_out, ctx).detach()
     frozen = [p.detach().clone() for p in decoder.params]
     errors, history = torch.empty(batch, dtype=torch.int32, device="cuda"), []
+    norm, scale = torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
     for step in range(1, steps + 1):
         z = torch.randn((batch, 16, 16, 8), generator=gen, device="cuda")
         with torch.no_grad():                                # what the decoder made of these latents before
@@ -236,7 +270,10 @@ def main(steps=200, batch=4, moment_bits=8, peak_lr=5e-3, rs_weight=0.05, fideli
         grads = torch.autograd.grad(loss, decoder.params)
         warm = min(1.0, step / 20)
         lr = warm * (1e-6 + (peak_lr - 1e-6) * 0.5 * (1 + math.cos(math.pi * max(0, step - 20) / max(1, steps - 20))))
-        opt.qrm_adamw_step([g.contiguous() for g in grads], step, lr)
+        grads = [g.contiguous() for g in grads]
+        if clip > 0.0:
+            opt.qrm_adamw_grad_norm(grads, clip, norm, scale)
+        opt.qrm_adamw_step(grads, step, lr, d_grad_scale=scale if clip > 0.0 else None)
         history.append(float(loss.detach()))
         if step % 25 == 0 or step == 1:
             report(f"step {step:4d}  loss {history[-1]:.4f}  wrong bits an image {float(errors.float().mean()):.1f} of {BITS}")
@@ -260,5 +297,7 @@ if __name__ == "__main__":
     a.add_argument("--steps", type=int, default=200)
     a.add_argument("--bits", type=int, default=8, choices=(8, 32), help="of the optimiser's moments")
     a.add_argument("--seed", type=int, default=0)
+    a.add_argument("--attention", action="store_true", help="the decoder's pixels look at each other")
+    a.add_argument("--clip", type=float, default=0.0, help="bound of the gradients' norm, 0 for none")
     args = a.parse_args()
-    main(steps=args.steps, moment_bits=args.bits, seed=args.seed)
+    main(steps=args.steps, moment_bits=args.bits, seed=args.seed, attention=args.attention, clip=args.clip)
