@@ -171,6 +171,39 @@ def test_odd_row_lengths(ctx, qrm, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("d", [32, 40, 96, 104, 128, 192, 200, 256, 264])
+def test_row_lengths_on_both_sides_of_a_kernels(ctx, qrm, d, dtype):
+    check(ctx, qrm, 1, 140, 150, 2, 1, d, dtype, causal=True, seed=d)
+
+
+@pytest.mark.parametrize("n,kv", [(1, 2), (3, 1), (1, 4), (5, 1), (2, 3), (7, 1), (4, 2), (3, 3), (1, 16), (17, 1)])
+def test_numbers_of_key_heads(ctx, qrm, n, kv):
+    """They are dealt to the dies in ways of their own below eight, at eight and above."""
+    check(ctx, qrm, n, 300, 260, 2 * kv, kv, 64, torch.bfloat16, causal=True, seed=n + kv)
+    check(ctx, qrm, n, 2, 700, 2 * kv, kv, 64, torch.float32, seed=n + kv)
+
+
+def test_rows_and_images_more_than_2_31_elements_apart(ctx, qrm):
+    """Keys 2^21 elements apart, and a second image 2^31 behind the first: offsets of 32 bits would meet other rows."""
+    d, lk, lq = 64, 1100, 70
+    g = torch.Generator().manual_seed(0)
+    apart, image = 1 << 21, (1 << 31) + (1 << 28)
+    wide = torch.zeros(image + lk * apart, dtype=torch.bfloat16, device="cuda")
+    c = Case(qrm, 2, lq, lk, 1, 1, d, torch.bfloat16, causal=True, seed=6)
+    k = wide.as_strided((2, lk, 1, d), (image, apart, d, 1), 0)
+    v = wide.as_strided((2, lk, 1, d), (image, apart, d, 1), 4096)
+    dk, dv = wide.as_strided((2, lk, 1, d), (image, apart, d, 1), 8192), wide.as_strided((2, lk, 1, d), (image, apart, d, 1), 12288)
+    k.copy_(c.k), v.copy_(c.v)
+    c.k, c.v, c.dk, c.dv = k, v, dk, dv
+    c.desc = desc_of(qrm, c.q, k, v, c.o, True, c.scale)
+    c.forward(ctx)
+    c.backward(ctx)
+    torch.cuda.synchronize()
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("d", [64, 200])
 def test_lengths_and_rows_that_see_nothing(ctx, qrm, causal, d, dtype):
@@ -265,6 +298,32 @@ def test_the_same_bits_from_call_to_call_and_beside_other_outputs(ctx, qrm, shap
             assert torch.equal(first[name], getattr(c, name)), name
         for name in {"dq", "dk", "dv"} - set(wanted):
             assert bool((getattr(c, name) == 7.0).all()), name
+
+
+def test_a_backward_pass_needs_no_forward_of_this_library(ctx, qrm):
+    """o and lse may come from anywhere: the formulas say what they are."""
+    c = Case(qrm, 2, 50, 60, 2, 2, 32, torch.float32, seed=12)
+    o, lse, _ = at.attention(*c.args, c.scale)
+    c.o.copy_(torch.from_numpy(o).float())
+    c.lse.copy_(torch.from_numpy(lse).float())
+    c.backward(ctx)
+    torch.cuda.synchronize()
+    c.check_backward()
+
+
+def test_more_streams_than_workspaces(ctx, qrm):
+    cases = [Case(qrm, 1, 2, 3000 + 100 * i, 2, 1, 64, torch.bfloat16, seed=i) for i in range(2 * qrm.QRM_MAX_STREAMS)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(2):
+        for c, s in zip(cases, streams):
+            ctx.qrm_attention(c.desc, c.q, c.k, c.v, c.o, c.lse, None, None, s)
+            ctx.qrm_attention_backward(c.desc, c.q, c.k, c.v, c.o, c.do, c.lse, c.dq, c.dk, c.dv, None, None, s)
+    torch.cuda.synchronize()
+    for c, s in zip(cases, streams):
+        c.check_forward()
+        c.check_backward()
+        ctx.qrm_release_stream(s)
 
 
 def test_no_rows(ctx, qrm):
