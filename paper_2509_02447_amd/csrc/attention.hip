@@ -84,17 +84,16 @@ template <typename T> __device__ __forceinline__ void join_part(const AttnArgs &
     Pack<T, 4> out;
     if (j.sums) {
         const float2 *const sums = j.sums + which * a.columns + column;
-        float top = -INFINITY, sum = 0.f;
-#pragma unroll 4
-        for (int k = 0; k < splits; ++k) top = fmaxf(top, sums[k * apart * a.columns].x);
+        float top = -INFINITY, sum = 0.f; // (one pass: a split's sums and its results are on their way together)
 #pragma unroll 4
         for (int k = 0; k < splits; ++k) {
             const float2 s = sums[k * apart * a.columns];
             const f32x4 p = from[k * apart * j.per];
-            const float by = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - top);
-            sum += s.y * by;
+            const float now = fmaxf(top, s.x), less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now), by = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - now);
+            top = now;
+            sum = sum * less + s.y * by;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += by == 0.f ? 0.f : p[e] * by;
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * less + (by == 0.f ? 0.f : p[e] * by);
         }
         const bool some = top != -INFINITY;
         const float inv = some ? 1.f / sum : 0.f;
