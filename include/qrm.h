@@ -382,7 +382,7 @@ QRM_API qrm_status qrm_profile_read_chunks(qrm_ctx *ctx, int32_t max_chunks, dou
  * Fine-tuning (Section 4.2: the image decoder is taught to write the key, with a message loss on the extractor's logits and some hundred
  * AdamW steps).  The calls below are the parts of such a step that are not matrix products; they take any context, whatever it was
  * created with, unless stated.  They can be recorded into a HIP graph on a stream that has run the same calls on the context before (its
- * workspace is there then; a qrm_message_loss that would have to clear counters first is refused, QRM_E_INVALID).
+ * workspace is there then; a qrm_message_loss or a qrm_adamw_grad_norm that would have to clear counters first is refused, QRM_E_INVALID).
  * Types of tensors: */
 typedef enum { QRM_F32 = 0, QRM_BF16 = 1, QRM_F16 = 2 } qrm_type;
 typedef enum { QRM_ACT_NONE = 0, QRM_ACT_RELU = 1, QRM_ACT_SILU = 2 } qrm_act;

@@ -291,8 +291,9 @@ template <int M, int WAVES, typename ACC, int COUNT> __device__ __forceinline__ 
 // ---------------------------------------------------------------- forward
 
 // Columns: query rows (position, head of the group).  Walks over the keys with a running maximum; the results are scaled down when it has grown by more
-// than 2^8, so that most tiles leave them alone.  Sums and results in 32 bits; probabilities are rounded to the type for the second product (16-bit types:
-// half a step relative to each, unsystematic, which is what the output's own rounding is).
+// than 2^GROWS, so that most tiles leave them alone.  Sums and results in 32 bits; probabilities are rounded to the type for the second product (16-bit types:
+// half a step relative to each, unsystematic, which is what the output's own rounding is).  f16: they are taken times 2^11, so that many keys of little weight
+// are not lost under its smallest number: 2^-36 a key (they stay under 2^16, with what the maximum may grow).
 template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF, int OCC>
 __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 {
@@ -300,6 +301,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     typedef Tile<T, DP> L;
     constexpr int R = TK / X::NG, DH = DP / SHARE, AHEAD = 6; // scores of a lane, elements of a wavefront
     constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = R * 256; // exchanged: a wavefront's scores
+    constexpr float GROWS = std::is_same<T, f16_t>::value ? 4.f : 8.f, LIFT = std::is_same<T, f16_t>::value ? 11.f : 0.f;
     constexpr bool TURNS = NBUF == 1; // keys and values take turns: the one is on its way while the other is used
     static_assert(SHARE > 1 || !TURNS, "in turns there is a barrier between keys and values");
     __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
@@ -345,7 +347,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     wait_known_loads();
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, mine = lds0 + e0 * (int)sizeof(T);
     const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
-    float top = -INFINITY, limit = -INFINITY, sums[4] = {}; // of the raw scores; 2^8 above, in powers of two; of this lane's probabilities
+    float top = -INFINITY, limit = -INFINITY, sums[4] = {}; // of the raw scores; 2^GROWS above, in powers of two; of this lane's probabilities
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
         wait_loads();
@@ -398,13 +400,13 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
                 const float now = fmaxf(top, column_max<M>(high));
                 const float less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - now) * c);
                 top = now;
-                limit = __builtin_fmaf(now, c, 8.f);
+                limit = __builtin_fmaf(now, c, GROWS);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sums[e] *= less;
 #pragma unroll
                 for (int d = 0; d < DH / M; ++d) o[d] *= less;
             }
-            const float about = top == -INFINITY ? 0.f : top * c;
+            const float about = top == -INFINITY ? 0.f : __builtin_fmaf(top, c, -LIFT);
             typename X::frag p[TK / X::KK];
             float chance[R];
 #pragma unroll
@@ -426,7 +428,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     }
     const float sum = column_sum<M>(sums[0] + sums[1] + (sums[2] + sums[3]));
     row = row0 + again(col), pos = attn_position(a, row), head = at.kv * a.group + (row - pos * a.group);
-    const float about = top == -INFINITY ? 0.f : top * c;
+    const float about = top == -INFINITY ? 0.f : __builtin_fmaf(top, c, -LIFT);
     if (split.count > 1) { // a part of a row: results, and their sum about 2^about
         const int64_t slot = attn_slot(a, at);
         if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(sum > 0.f || sum != sum ? about : -INFINITY, sum);

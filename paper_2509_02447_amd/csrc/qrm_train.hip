@@ -93,6 +93,9 @@ qrm_status check_grads(qrm_ctx *c, const qrm_adamw *o, const void *const *h_grad
     return QRM_OK;
 }
 
+constexpr double kLaunchThreads = 4294967296.0; // a launch has less
+const char *const kTooManyRows = "the rows of all images need 2^32 threads and more";
+
 // Where a tensor of an attention call lies: dense strides filled in; rows overlap nowhere.
 qrm_status check_rows(qrm_ctx *c, AttnRows *r, int64_t N, int64_t L, int heads, int D)
 {
@@ -136,9 +139,9 @@ qrm_status check_attention(qrm_ctx *c, const qrm_attention_desc *desc, AttnCheck
     if (d.D > QRM_ATTENTION_MAX_D) return fail(c, QRM_E_UNSUPPORTED, "D above 512");
     if (d.N > most || d.Lq > most || d.Lk > most || d.Lq * d.heads > most) return fail(c, QRM_E_UNSUPPORTED, "N, Lk, or query rows of all heads of an image above 2^30");
     if (d.N * d.heads > most / 128) return fail(c, QRM_E_UNSUPPORTED, "heads of all images above 2^23");
-    // (a launch has less than 2^32 threads; a thread has at least four elements, a workgroup of 64 sixteen rows and more)
+    // (of the launches that take rows one by one: a thread has at least four elements, sixteen threads have a row)
     const double rows = (double)d.N * std::max((double)d.Lq * d.heads, (double)d.Lk * d.kv_heads);
-    if (rows * ((d.D + 7) / 4) >= 4294967296.0 || rows * 16 >= 4294967296.0) return fail(c, QRM_E_UNSUPPORTED, "the rows of all images need 2^32 threads and more");
+    if (rows * ((d.D + 7) / 4) >= kLaunchThreads || rows * 16 >= kLaunchThreads) return fail(c, QRM_E_UNSUPPORTED, kTooManyRows);
     const int size = type_bytes(d.type), e = 16 / size;
     out->wide = (d.D + e - 1) / e * e;
     out->q = {d.q_row, d.q_head, d.q_image};
@@ -516,6 +519,7 @@ qrm_status qrm_attention(qrm_ctx *c, const qrm_attention_desc *desc, const void 
     if (common_alignment({d_q, d_k, d_v, d_o}) < size || !aligned_to(d_lse, 4) || !aligned_to(d_q_len, 4) || !aligned_to(d_k_len, 4))
         return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
     const AttnCut cut = plan_attention(d, a.wide, c->num_cu);
+    if (std::max(cut.threads(d), cut.join_threads(d)) >= kLaunchThreads) return fail(c, QRM_E_UNSUPPORTED, kTooManyRows);
     Workspace w;
     const AttnTensor q = place(a, a.q, d.Lq, d.heads, {d_q}, 1, &w), k = place(a, a.k, d.Lk, d.kv_heads, {d_k}, 1, &w), v = place(a, a.v, d.Lk, d.kv_heads, {d_v}, 1, &w),
                      o = place(a, a.o, d.Lq, d.heads, {d_o}, 1, &w);
@@ -570,6 +574,7 @@ qrm_status qrm_attention_backward(qrm_ctx *c, const qrm_attention_desc *desc, co
         return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
     AttnCut by_q{}, by_k{};
     plan_attention_backward(d, a.wide, c->num_cu, &by_q, &by_k);
+    if (std::max(by_q.threads(d) + by_k.threads(d), by_q.join_threads(d) + 2 * by_k.join_threads(d)) >= kLaunchThreads) return fail(c, QRM_E_UNSUPPORTED, kTooManyRows);
     Workspace w;
     const size_t q_rows = (size_t)d.N * d.heads * d.Lq, k_rows = (size_t)d.N * d.kv_heads * d.Lk;
     // (a copied tensor's gradient is written behind its copy)

@@ -257,6 +257,27 @@ def test_small_gradients_in_f16(ctx, qrm):
     assert float(c.dq.float().abs().mean()) > 0
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_many_keys_of_little_weight(ctx, qrm, dtype):
+    """2^17 keys of exp(-18) each beside one of weight 1: together 0.2 %, each less than half of f16's smallest number.  The weights' rounding (f16: to steps of
+    2^-24 / 2^11 at least), 2^17 / 8 additions to a lane's sum, the result's rounding; and the products' sums: an instruction adds the products of two rows (f32) or more
+    to what there is, so 2^17 / 2 roundings of equal summands, which all go the same way."""
+    lq, lk, heads, d = 1024, 1 << 17, 64, 32
+    q = torch.zeros((1, lq, heads, d), dtype=dtype, device="cuda")
+    k, v = (torch.zeros((1, lk, 1, d), dtype=dtype, device="cuda") for _ in range(2))
+    q[..., 0], k[..., 0], v[...] = 4.0, -4.5, 1.0
+    k[0, 77], v[0, 77] = 0.0, 0.0
+    o = torch.empty_like(q)
+    ctx.qrm_attention(desc_of(qrm, q, k, v, o, False, 1.0), q, k, v, o, None, None, None, 0)
+    p = float(np.exp(-18.0))
+    weight = (lk - 1) * p
+    want = weight / (1.0 + weight)
+    half = HALF[dtype]
+    tolerance = (2 * half + lk / 8 * U + lk / 2 * U + 64 * U + (2.0 ** -36 / p if dtype == torch.float16 else 0.0)) * 1.01
+    off = float((o.double() / want - 1.0).abs().max())
+    assert off <= tolerance, (off, tolerance)
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_values_that_are_not_finite_stay_in_their_image_and_key_head(ctx, qrm, dtype, bad):
@@ -394,6 +415,20 @@ def test_refusals(ctx, qrm):
     refused(bad, swap=lambda t: dict(dk=t["dv"]))
     refused(bad, swap=lambda t: dict(dq=None, dk=None, dv=None))
     assert ctx._lib.qrm_attention(ctx._h, None, None, None, None, None, None, None, None, None) == bad
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_single_rows_of_more_heads_than_a_launch_has_workgroups_for(ctx, qrm, dtype):
+    """A workgroup of 512 threads takes the one row of a head and image: 2^23 of them for queries and as many for keys are 2^33 threads.  Said before anything is read."""
+    import ctypes
+    c = Case(qrm, 1, 1, 1, 1, 1, 512, dtype)
+    c.desc.N = 1 << 23
+    for t in "qkvo":
+        for s in ("row", "head", "image"):
+            setattr(c.desc, f"{t}_{s}", 0)
+    p = {k: getattr(c, k).data_ptr() for k in ("q", "k", "v", "o", "do", "lse", "dq", "dk", "dv")}
+    got = ctx._lib.qrm_attention_backward(ctx._h, ctypes.byref(c.desc), p["q"], p["k"], p["v"], p["o"], p["do"], p["lse"], None, None, p["dq"], p["dk"], p["dv"], None)
+    assert got == qrm.QRM_E_UNSUPPORTED and "2^32" in ctx.last_error()
 
 
 def test_the_binding_compares_tensors_with_their_descriptor(ctx, qrm):
