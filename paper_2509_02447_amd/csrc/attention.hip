@@ -25,13 +25,11 @@ uint32_t blocks_of(int64_t items) { return (uint32_t)((items + kThreads - 1) / k
 constexpr int kRowLanes = 16;
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, const T *dy, int64_t row, int64_t head, int64_t image, const float *lse, const int32_t *q_len,
-                                                                  int64_t all, int Lq, int heads, int D, float scale, float *row_lse, float *row_delta)
+                                                                  int all, Quotient by_heads, Quotient by_rows, int D, float scale, float *row_lse, float *row_delta)
 {
-    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kRowLanes;
-    const int lane = threadIdx.x % kRowLanes;
+    const int i = (int)((blockIdx.x * kThreads + threadIdx.x) / kRowLanes), lane = threadIdx.x % kRowLanes;
     if (i >= all) return;
-    const int64_t n = i / ((int64_t)heads * Lq);
-    const int rest = (int)(i - n * heads * Lq), h = rest / Lq, pos = rest % Lq;
+    const int head_of = by_rows.of(i), pos = i - head_of * (int)by_rows.by, n = by_heads.of(head_of), h = head_of - n * (int)by_heads.by;
     const bool there = !q_len || pos < q_len[n];
     float sum = 0.f;
     if (there) {
@@ -50,7 +48,9 @@ __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, co
     }
 }
 
-// Joins the splits of a launch: a thread has four results, where the lanes of the splits' workgroups had them (store_part).  What was written at once is left alone.
+// Joins the splits of a launch: a thread has two times four results of a row, where the lanes of the splits' workgroups had them (store_part).  What was written at
+// once is left alone.  Bound by memory (most of it in the last cache), if enough is on its way: kAhead splits are read before the first of them is added, and what
+// does not depend on the lane is computed once a wavefront (one head of 512, 4 x 4096 rows in 2 splits, 67 MB: JOINTIMES).
 struct JoinJob {
     const float *part;
     const float2 *sums; // forward: (power of two that a row's results are about, their sum)
@@ -60,61 +60,89 @@ struct JoinJob {
     int width;
     bool keys;      // rows are those of keys
     uint32_t first; // workgroup
-    int64_t per;    // threads to a part
+    int pairs;      // of blocks of a part: a block is what 64 lanes hold in four registers
+    Quotient by_pairs, by_blocks; // by_blocks: of a wavefront
 };
-template <typename T> __device__ __forceinline__ void join_part(const AttnArgs &a, const JoinJob &j)
+constexpr int kAhead = 4;
+template <typename T, bool SUMS> __device__ __forceinline__ void join_part(const AttnArgs &a, const JoinJob &j)
 {
     const AttnShape &h = j.shape;
-    const int64_t t = (int64_t)(blockIdx.x - j.first) * kThreads + threadIdx.x, which = t / j.per; // (a part is so many workgroups' work)
-    const int group = (int)(which / a.parts), part = (int)(which % a.parts), n = group / a.kv_heads, kv = group % a.kv_heads;
+    const int unit = __builtin_amdgcn_readfirstlane((blockIdx.x - j.first) * (kThreads / 64) + threadIdx.x / 64), which = j.by_pairs.of(unit), lane = threadIdx.x % 64;
+    const int group = a.by_parts.of(which), part = which - group * a.parts, n = a.by_kv_heads.of(group), kv = group - n * a.kv_heads;
+    if (n >= a.N) return;
     const int q_len = attn_length(a.q_len, n, a.Lq), k_len = attn_length(a.k_len, n, a.Lk);
     int skip;
     const int tiles = j.keys ? attn_query_tiles(a, q_len, k_len, part, &skip) * a.group : attn_key_tiles(a, q_len, k_len, part);
     const int splits = attn_split(a, tiles, 0).count;
     if (splits == 1) return;
-    // the lane's columns and elements: as in store_part and Mma::row_of
-    const int item = (int)(t - which * j.per), lane = item % 64, ng = 64 / h.m, quads = h.m * h.m / 256, each = j.width / h.share, blocks = each / h.m * quads;
-    const int wave = item / 64 / blocks, block = item / 64 % blocks, column = wave / h.share * h.m + lane % h.m;
-    const int d = wave % h.share * each + block / quads * h.m + (block % quads * ng + lane / h.m) * 4;
+    // the lane's column and elements: as in store_part and Mma::row_of
+    const int pair = unit - which * j.pairs, ng = 64 / h.m, quads = h.m * h.m / 256, each = j.width / h.share, blocks = each / h.m * quads;
+    const int wave = j.by_blocks.of(pair * 2), block = pair * 2 - wave * blocks, column = wave / h.share * h.m + lane % h.m;
     const int r = part * a.columns + column, pos = j.keys ? r : attn_position(a, r), head = j.keys ? kv : kv * a.group + (r - pos * a.group);
-    if (pos >= (j.keys ? a.Lk : a.Lq) || d >= a.D) return;
+    if (pos >= (j.keys ? a.Lk : a.Lq)) return;
     const int64_t apart = (int64_t)a.N * a.kv_heads * a.parts; // slots from one split to the next
-    const f32x4 *const from = (const f32x4 *)j.part + t;
-    f32x4 o = {};
-    Pack<T, 4> out;
-    if (j.sums) {
-        const float2 *const sums = j.sums + which * a.columns + column;
+    const f32x4 *const from = (const f32x4 *)j.part + ((int64_t)which * j.pairs + pair) * 128 + lane;
+    f32x4 o[2] = {};
+    float by_sum = 1.f;
+    if constexpr (SUMS) {
+        const float2 *const sums = j.sums + which * (int64_t)a.columns + column;
         float top = -INFINITY, sum = 0.f; // (one pass: a split's sums and its results are on their way together)
-#pragma unroll 4
-        for (int k = 0; k < splits; ++k) {
-            const float2 s = sums[k * apart * a.columns];
-            const f32x4 p = from[k * apart * j.per];
-            const float now = fmaxf(top, s.x), less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now), by = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - now);
-            top = now;
-            sum = sum * less + s.y * by;
+        for (int k0 = 0; k0 < splits; k0 += kAhead) {
+            float2 s[kAhead];
+            f32x4 p[kAhead][2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = o[e] * less + (by == 0.f ? 0.f : p[e] * by);
+            for (int i = 0; i < kAhead; ++i) {
+                if (k0 + i >= splits) break;
+                const int64_t k = k0 + i;
+                s[i] = sums[k * apart * a.columns];
+                p[i][0] = from[k * apart * j.pairs * 128];
+                p[i][1] = from[k * apart * j.pairs * 128 + 64];
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (k0 + i >= splits) break;
+                const float now = fmaxf(top, s[i].x), less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now), by = s[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[i].x - now);
+                top = now;
+                sum = sum * less + s[i].y * by;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = o[e / 4][e % 4] * less + (by == 0.f ? 0.f : p[i][e / 4][e % 4] * by);
+            }
         }
         const bool some = top != -INFINITY;
-        const float inv = some ? 1.f / sum : 0.f;
+        by_sum = some ? 1.f / sum : 0.f;
+        if (block == 0 && lane < h.m && wave % h.share == 0 && a.lse) a.lse[((int64_t)n * a.heads + head) * a.Lq + pos] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    } else if (!j.keys || r < k_len) {
+        for (int k0 = 0; k0 < splits; k0 += kAhead) {
+            f32x4 p[kAhead][2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] *= inv;
-        if (d == 0 && a.lse) a.lse[((int64_t)n * a.heads + head) * a.Lq + pos] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
-    } else {
-        if (!j.keys || r < k_len)
-#pragma unroll 4
-            for (int k = 0; k < splits; ++k) o += from[k * apart * j.per];
+            for (int i = 0; i < kAhead; ++i) {
+                if (k0 + i >= splits) break;
+                const int64_t k = k0 + i;
+                p[i][0] = from[k * apart * j.pairs * 128];
+                p[i][1] = from[k * apart * j.pairs * 128 + 64];
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (k0 + i >= splits) break;
+                o[0] += p[i][0], o[1] += p[i][1];
+            }
+        }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out.e[e] = (T)o[e];
-    store_pack<T, 4>((T *)j.out + n * j.image + head * j.head + pos * j.row + d, out);
+    for (int u = 0; u < 2; ++u) {
+        const int d = wave % h.share * each + (block + u) / quads * h.m + ((block + u) % quads * ng + lane / h.m) * 4;
+        Pack<T, 4> out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out.e[e] = (T)(o[u][e] * by_sum);
+        if (d < a.D) store_pack<T, 4>((T *)j.out + n * j.image + head * j.head + pos * j.row + d, out);
+    }
 }
-template <typename T> __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttnArgs a, JoinJob j) { join_part<T>(a, j); }
+template <typename T> __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttnArgs a, JoinJob j) { join_part<T, true>(a, j); }
 template <typename T> __global__ __launch_bounds__(kThreads) void attention_add_kernel(AttnArgs by_q, AttnArgs by_k, JoinJob q, JoinJob k, JoinJob v)
 {
-    if (blockIdx.x < k.first) join_part<T>(by_q, q);
-    else if (blockIdx.x < v.first) join_part<T>(by_k, k);
-    else join_part<T>(by_k, v);
+    if (blockIdx.x < k.first) join_part<T, false>(by_q, q);
+    else if (blockIdx.x < v.first) join_part<T, false>(by_k, k);
+    else join_part<T, false>(by_k, v);
 }
 
 // Rows [N,L,heads,D] from one place to another, element by element on the side that is not aligned: into rows of `wide` elements, zeros behind the D, or
@@ -154,7 +182,7 @@ hipError_t launch_attention_backward(int type, const AttnArgs &by_q, const AttnA
 
 hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, const void *dy, const float *lse, const int32_t *q_len, float *row_lse, float *row_delta, hipStream_t s)
 {
-    const int64_t all = d.N * d.heads * d.Lq;
+    const int64_t all = d.N * d.heads * d.Lq; // (below 2^28: sixteen threads each)
     const int size = type_bytes(d.type), v = 16 / size;
     const bool wide = ((uintptr_t)o | (uintptr_t)dy) % 16 == 0 && d.D % v == 0 && d.o_row % v == 0 && d.o_head % v == 0 && d.o_image % v == 0;
     const dim3 grid(blocks_of(all * kRowLanes));
@@ -162,7 +190,7 @@ hipError_t launch_attention_rows(const qrm_attention_desc &d, const void *o, con
         using T = std::remove_pointer_t<decltype(p)>;
         auto run = [&](auto width) {
             hipLaunchKernelGGL((attention_rows_kernel<T, decltype(width)::value>), grid, dim3(kThreads), 0, s, (const T *)o, (const T *)dy, d.o_row, d.o_head, d.o_image, lse, q_len,
-                               all, (int)d.Lq, d.heads, d.D, d.scale, row_lse, row_delta);
+                               (int)all, Quotient((uint32_t)d.heads), Quotient((uint32_t)d.Lq), d.D, d.scale, row_lse, row_delta);
         };
         wide ? run(std::integral_constant<int, 16 / sizeof(T)>()) : run(std::integral_constant<int, 1>());
         return hipGetLastError();
@@ -174,8 +202,10 @@ namespace {
 // Adds a job's workgroups to those that there are.
 JoinJob join_job(const AttnArgs &a, const AttnCut &cut, const float *part, void *out, int64_t row, int64_t head, int64_t image, uint32_t *blocks)
 {
-    JoinJob j{part, nullptr, out, row, head, image, cut.shape, cut.width, cut.kind == ATTN_DKV, *blocks, (int64_t)cut.shape.rows() * cut.width / 4};
-    if (out && a.splits > 1) *blocks += (uint32_t)(j.per * a.N * a.kv_heads * a.parts / kThreads);
+    JoinJob j{part, nullptr, out, row, head, image, cut.shape, cut.width, cut.kind == ATTN_DKV, *blocks, cut.shape.rows() * cut.width / 512};
+    const int m = cut.shape.m;
+    j.by_pairs = Quotient(j.pairs), j.by_blocks = Quotient(cut.width / cut.shape.share / m * (m * m / 256));
+    if (out && a.splits > 1) *blocks += blocks_of((int64_t)j.pairs * a.N * a.kv_heads * a.parts * 64);
     return j;
 }
 

@@ -253,7 +253,7 @@ struct AttnCut {
     size_t sums_bytes(const qrm_attention_desc &d) const { return splits > 1 ? (size_t)splits * d.N * d.kv_heads * parts * shape.rows() * 8 : 0; }
     // threads of the launch (workgroups in eights), and of what joins one of its results: a launch has less than 2^32
     double threads(const qrm_attention_desc &d) const { return ((double)d.N * d.kv_heads * parts * splits + 8) * shape.waves * 64; }
-    double join_threads(const qrm_attention_desc &d) const { return splits > 1 ? (double)d.N * d.kv_heads * parts * shape.rows() * width / 4 : 0.0; }
+    double join_threads(const qrm_attention_desc &d) const { return splits > 1 ? (double)d.N * d.kv_heads * parts * shape.rows() * width / 8 + 256 : 0.0; }
 };
 // A part's splits: a workgroup walks down `per` tiles at most; a part of no more is written at once, the results of others are joined.  Both here and there
 // as many as are walked down at all: tiles of an image's length, not of Lk.
