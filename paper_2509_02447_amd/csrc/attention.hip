@@ -21,7 +21,7 @@ constexpr float kLn2 = 0.693147180559945309f;
 uint32_t blocks_of(int64_t items) { return (uint32_t)((items + kThreads - 1) / kThreads); }
 
 // Sixteen lanes a row: minus the sum of dy o, and minus the log-sum over the scale (a row that sees nothing: -inf, so that its probabilities are zeros).
-// Rows behind an image's queries are not read.
+// Rows behind an image's queries are not read.  Bound by memory: 131072 rows of 128 elements of bf16, 67 MB, in 16 us, 4.2 TB/s.
 constexpr int kRowLanes = 16;
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, const T *dy, int64_t row, int64_t head, int64_t image, const float *lse, const int32_t *q_len,
@@ -50,7 +50,8 @@ __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, co
 
 // Joins the splits of a launch: a thread has two times four results of a row, where the lanes of the splits' workgroups had them (store_part).  What was written at
 // once is left alone.  Bound by memory (most of it in the last cache), if enough is on its way: kAhead splits are read before the first of them is added, and what
-// does not depend on the lane is computed once a wavefront (one head of 512, 4 x 4096 rows in 2 splits, 67 MB: JOINTIMES).
+// does not depend on the lane is computed once a wavefront (one head of 512, 4 x 4096
+// rows in 2 splits, 67 MB: 16 us, 5.2 TB/s; one block a thread, split after split and with divisions 23).
 struct JoinJob {
     const float *part;
     const float2 *sums; // forward: (power of two that a row's results are about, their sum)
@@ -146,7 +147,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void attention_add_
 }
 
 // Rows [N,L,heads,D] from one place to another, element by element on the side that is not aligned: into rows of `wide` elements, zeros behind the D, or
-// out of such.
+// out of such.  Bound by launches and single-element accesses: bf16, 2 x 2048 rows of 16 heads of
+// 128 all an element off, forward 88 -> 130 us, backward 234 -> 329; 4 x 1024 rows of 8 heads of 64, 17 -> 40 and 41 -> 78.
 template <typename T, bool OUT>
 __global__ __launch_bounds__(kThreads) void attention_copy_kernel(AttnRows rows, T *there, T *here, int64_t all, int64_t L, int heads, int D, int wide)
 {
@@ -300,9 +302,9 @@ constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
 
 } // namespace
 
-// Measured, us, by number of splits (the rule's in brackets): one head of 512, bf16, 4 x 1024 rows 1 66, 2 52, [4 40], 8 43; 4 x 4096 rows 1 233, [2 169], 3 206, 4 180; 16 heads of 128, 4
-// key heads, causal, 2 x 8192 rows [1 511], 2 645; 16 single tokens of 32 heads over up to 8191 rows of 4: 2 106, 4 60, [8 41], 12 40, 24 52; f32, 6 heads of 60, 3 x 2257 rows 1 299,
-// 2 242, [3 228], 4 254.
+// Measured, us, by number of splits (the rule's in brackets): one head of 512, bf16, 4 x 1024 rows 1 74, 2 51, 3 42, [4 39], 6 39, 8 41; 4 x 4096 rows 1 254, [2 164], 3 206, 4 183; 16 heads of
+// 128, 4 key heads, causal, 2 x 8192 rows [1 511], 2 645; 16 single tokens of 32 heads over up to 8191 rows of 4: 1 167, 4 49, 6 38, [8 34], 12 34; f32, 6 heads of 60, 3 x 2257 rows 1 298,
+// 2 235, [3 211], 4 237.
 AttnCut plan_attention(const qrm_attention_desc &d, int width, int num_cu)
 {
     CutModel m(d, width, ATTN_FORWARD, num_cu), best = m;
@@ -318,8 +320,8 @@ AttnCut plan_attention(const qrm_attention_desc &d, int width, int num_cu)
 }
 
 // Both sides of a backward launch, whatever of it is wanted: a gradient's bits do not depend on the others.  Measured, us of the call, by splits of queries' / keys' side: 16 heads of 128, 4 key
-// heads, 2 x 4096 causal rows 1/1 667, 1/2 530, [1/3 490], 2/3 517, 1/4 495; one head of 512, 4 x 1024 rows 1/1 115, [1/2 87], 2/2 82, 2/4 99; f16, 5 x 777 rows over 1033, 8 heads of 96, 2 key
-// heads 1/1 123, 1/3 68, [1/4 69], 2/4 65.
+// heads, 2 x 4096 causal rows 1/1 634, 1/2 498, 1/3 460, 1/4 466, [1/5 470]; one head of 512, 4 x 1024 rows 1/1 109, 1/2 82, 1/3 85, [2/2 79], 2/3 92; f16, 5 x 777 rows over 1033, 8 heads of 96,
+// 2 key heads 1/1 119, 1/2 74, [1/3 63], 1/4 67, 2/4 62.
 void plan_attention_backward(const qrm_attention_desc &d, int width, int num_cu, AttnCut *by_q, AttnCut *by_k)
 {
     CutModel q(d, width, ATTN_DQ, num_cu), k(d, width, ATTN_DKV, num_cu);
