@@ -52,41 +52,42 @@ __global__ __launch_bounds__(kThreads) void attention_rows_kernel(const T *o, co
 // once is left alone.  Bound by memory (most of it in the last cache), if enough is on its way: kAhead splits are read before the first of them is added, and what
 // does not depend on the lane is computed once a wavefront (one head of 512, 4 x 4096
 // rows in 2 splits, 67 MB: 16 us, 5.2 TB/s; one block a thread, split after split and with divisions 23).
-struct JoinJob {
+struct JoinTo {
     const float *part;
-    const float2 *sums; // forward: (power of two that a row's results are about, their sum)
     void *out;
     int64_t row, head, image;
-    AttnShape shape;
-    int width;
-    bool keys;      // rows are those of keys
     uint32_t first; // workgroup
-    int pairs;      // of blocks of a part: a block is what 64 lanes hold in four registers
+};
+struct JoinJob {
+    JoinTo to;
+    AttnShape shape;
+    int width, pairs;             // pairs of blocks of a part: a block is what 64 lanes hold in four registers
     Quotient by_pairs, by_blocks; // by_blocks: of a wavefront
 };
 constexpr int kAhead = 4;
-template <typename T, bool SUMS> __device__ __forceinline__ void join_part(const AttnArgs &a, const JoinJob &j)
+// KEYS: rows are those of keys.  SUMS: forward, (power of two that a row's results are about, their sum).
+template <typename T, bool KEYS, bool SUMS> __device__ __forceinline__ void join_part(const AttnArgs &a, const JoinJob &j, const JoinTo &to)
 {
     const AttnShape &h = j.shape;
-    const int unit = __builtin_amdgcn_readfirstlane((blockIdx.x - j.first) * (kThreads / 64) + threadIdx.x / 64), which = j.by_pairs.of(unit), lane = threadIdx.x % 64;
+    const int unit = __builtin_amdgcn_readfirstlane((blockIdx.x - to.first) * (kThreads / 64) + threadIdx.x / 64), which = j.by_pairs.of(unit), lane = threadIdx.x % 64;
     const int group = a.by_parts.of(which), part = which - group * a.parts, n = a.by_kv_heads.of(group), kv = group - n * a.kv_heads;
     if (n >= a.N) return;
     const int q_len = attn_length(a.q_len, n, a.Lq), k_len = attn_length(a.k_len, n, a.Lk);
     int skip;
-    const int tiles = j.keys ? attn_query_tiles(a, q_len, k_len, part, &skip) * a.group : attn_key_tiles(a, q_len, k_len, part);
+    const int tiles = KEYS ? attn_query_tiles(a, q_len, k_len, part, &skip) * a.group : attn_key_tiles(a, q_len, k_len, part);
     const int splits = attn_split(a, tiles, 0).count;
     if (splits == 1) return;
     // the lane's column and elements: as in store_part and Mma::row_of
     const int pair = unit - which * j.pairs, ng = 64 / h.m, quads = h.m * h.m / 256, each = j.width / h.share, blocks = each / h.m * quads;
     const int wave = j.by_blocks.of(pair * 2), block = pair * 2 - wave * blocks, column = wave / h.share * h.m + lane % h.m;
-    const int r = part * a.columns + column, pos = j.keys ? r : attn_position(a, r), head = j.keys ? kv : kv * a.group + (r - pos * a.group);
-    if (pos >= (j.keys ? a.Lk : a.Lq)) return;
+    const int r = part * a.columns + column, pos = KEYS ? r : attn_position(a, r), head = KEYS ? kv : kv * a.group + (r - pos * a.group);
+    if (pos >= (KEYS ? a.Lk : a.Lq)) return;
     const int64_t apart = (int64_t)a.N * a.kv_heads * a.parts; // slots from one split to the next
-    const f32x4 *const from = (const f32x4 *)j.part + ((int64_t)which * j.pairs + pair) * 128 + lane;
+    const f32x4 *const from = (const f32x4 *)to.part + ((int64_t)which * j.pairs + pair) * 128 + lane;
     f32x4 o[2] = {};
     float by_sum = 1.f;
     if constexpr (SUMS) {
-        const float2 *const sums = j.sums + which * (int64_t)a.columns + column;
+        const float2 *const sums = (const float2 *)a.part_sums + which * (int64_t)a.columns + column;
         float top = -INFINITY, sum = 0.f; // (one pass: a split's sums and its results are on their way together)
         for (int k0 = 0; k0 < splits; k0 += kAhead) {
             float2 s[kAhead];
@@ -112,7 +113,7 @@ template <typename T, bool SUMS> __device__ __forceinline__ void join_part(const
         const bool some = top != -INFINITY;
         by_sum = some ? 1.f / sum : 0.f;
         if (block == 0 && lane < h.m && wave % h.share == 0 && a.lse) a.lse[((int64_t)n * a.heads + head) * a.Lq + pos] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
-    } else if (!j.keys || r < k_len) {
+    } else if (!KEYS || r < k_len) {
         for (int k0 = 0; k0 < splits; k0 += kAhead) {
             f32x4 p[kAhead][2];
 #pragma unroll
@@ -135,15 +136,17 @@ template <typename T, bool SUMS> __device__ __forceinline__ void join_part(const
         Pack<T, 4> out;
 #pragma unroll
         for (int e = 0; e < 4; ++e) out.e[e] = (T)(o[u][e] * by_sum);
-        if (d < a.D) store_pack<T, 4>((T *)j.out + n * j.image + head * j.head + pos * j.row + d, out);
+        if (d < a.D) store_pack<T, 4>((T *)to.out + n * to.image + head * to.head + pos * to.row + d, out);
     }
 }
-template <typename T> __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttnArgs a, JoinJob j) { join_part<T, true>(a, j); }
-template <typename T> __global__ __launch_bounds__(kThreads) void attention_add_kernel(AttnArgs by_q, AttnArgs by_k, JoinJob q, JoinJob k, JoinJob v)
+template <typename T> __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttnArgs a, JoinJob j) { join_part<T, false, true>(a, j, j.to); }
+// (dk and dv by one copy of the code, and arguments of less than 1 KB: a backward pass of 4 x 256 rows of 4 heads 18.1 -> 17.7 us)
+template <typename T> __global__ __launch_bounds__(kThreads) void attention_add_kernel(AttnArgs by_q, AttnArgs by_k, JoinJob q, JoinJob k, JoinTo v)
 {
-    if (blockIdx.x < k.first) join_part<T, false>(by_q, q);
-    else if (blockIdx.x < v.first) join_part<T, false>(by_k, k);
-    else join_part<T, false>(by_k, v);
+    const bool values = blockIdx.x >= v.first;
+    if (blockIdx.x < k.to.first) join_part<T, false, false>(by_q, q, q.to);
+    else join_part<T, true, false>(by_k, k, JoinTo{values ? v.part : k.to.part, values ? v.out : k.to.out, values ? v.row : k.to.row, values ? v.head : k.to.head,
+                                                   values ? v.image : k.to.image, values ? v.first : k.to.first});
 }
 
 // Rows [N,L,heads,D] from one place to another, element by element on the side that is not aligned: into rows of `wide` elements, zeros behind the D, or
@@ -204,7 +207,7 @@ namespace {
 // Adds a job's workgroups to those that there are.
 JoinJob join_job(const AttnArgs &a, const AttnCut &cut, const float *part, void *out, int64_t row, int64_t head, int64_t image, uint32_t *blocks)
 {
-    JoinJob j{part, nullptr, out, row, head, image, cut.shape, cut.width, cut.kind == ATTN_DKV, *blocks, cut.shape.rows() * cut.width / 512};
+    JoinJob j{{part, out, row, head, image, *blocks}, cut.shape, cut.width, cut.shape.rows() * cut.width / 512, Quotient(), Quotient()};
     const int m = cut.shape.m;
     j.by_pairs = Quotient(j.pairs), j.by_blocks = Quotient(cut.width / cut.shape.share / m * (m * m / 256));
     if (out && a.splits > 1) *blocks += blocks_of((int64_t)j.pairs * a.N * a.kv_heads * a.parts * 64);
@@ -216,8 +219,7 @@ JoinJob join_job(const AttnArgs &a, const AttnCut &cut, const float *part, void 
 hipError_t launch_attention_join(int type, const AttnArgs &a, const AttnCut &cut, hipStream_t s)
 {
     uint32_t blocks = 0;
-    JoinJob j = join_job(a, cut, a.part, a.o, a.o_row, a.o_head, a.o_image, &blocks);
-    j.sums = (const float2 *)a.part_sums;
+    const JoinJob j = join_job(a, cut, a.part, a.o, a.o_row, a.o_head, a.o_image, &blocks);
     if (!blocks) return hipSuccess;
     return with_type(type, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;
@@ -235,7 +237,7 @@ hipError_t launch_attention_add(int type, const AttnArgs &by_q, const AttnCut &c
     if (!blocks) return hipSuccess;
     return with_type(type, [&](auto *p) {
         using T = std::remove_pointer_t<decltype(p)>;
-        hipLaunchKernelGGL((attention_add_kernel<T>), dim3(blocks), dim3(kThreads), 0, s, by_q, by_k, q, k, v);
+        hipLaunchKernelGGL((attention_add_kernel<T>), dim3(blocks), dim3(kThreads), 0, s, by_q, by_k, q, k, v.to);
         return hipGetLastError();
     });
 }
