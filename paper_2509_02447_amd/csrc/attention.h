@@ -431,17 +431,18 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         }
     }
     const float sum = column_sum<M>(sums[0] + sums[1] + (sums[2] + sums[3]));
+    const bool some = top != -INFINITY || sum != sum; // (scores above 32 bits' largest: a sum of 0 about infinity, which is no number in what follows)
     row = row0 + again(col), pos = attn_position(a, row), head = at.kv * a.group + (row - pos * a.group);
     const float about = top == -INFINITY ? 0.f : __builtin_fmaf(top, c, -LIFT);
     if (split.count > 1) { // a part of a row: results, and their sum about 2^about
         const int64_t slot = attn_slot(a, at);
-        if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(sum > 0.f || sum != sum ? about : -INFINITY, sum);
+        if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(some ? about : -INFINITY, sum);
         store_part<M, WAVES>(a.part, slot, wave, lane, 1.f, o);
         return;
     }
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
-    if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = sum > 0.f || sum != sum ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
-    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = some ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    const float inv = some ? 1.f / sum : 0.f;
     if (row >= rows) return;
     T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
 #pragma unroll

@@ -278,6 +278,19 @@ def test_many_keys_of_little_weight(ctx, qrm, dtype):
     assert off <= tolerance, (off, tolerance)
 
 
+@pytest.mark.parametrize("shape", [(1, 3, 5000, 2, 1, 64), (1, 100, 130, 2, 2, 64), (1, 70, 90, 1, 1, 512)])
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=IDS[:2])
+def test_scores_above_32_bits_are_no_rows_that_see_nothing(ctx, qrm, dtype, shape):
+    n, lq, lk, heads, kv, d = shape
+    q = torch.full((n, lq, heads, d), 2.0 ** 40, dtype=dtype, device="cuda")
+    k, v = (torch.full((n, lk, kv, d), 2.0 ** 30, dtype=dtype, device="cuda") for _ in range(2))
+    q[:, -1] = 0.0                                                             # (scores of zero: the mean of the values)
+    o, lse = torch.empty_like(q), torch.empty((n, heads, lq), device="cuda")
+    ctx.qrm_attention(desc_of(qrm, q, k, v, o, False, 2.0 ** 60), q, k, v, o, lse, None, None, 0)
+    assert not bool(torch.isfinite(o[:, :-1]).any()) and not bool(torch.isneginf(lse[..., :-1]).any())
+    assert float((o[:, -1].double() / 2.0 ** 30 - 1.0).abs().max()) <= lk * U + 2 * HALF[dtype]
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_values_that_are_not_finite_stay_in_their_image_and_key_head(ctx, qrm, dtype, bad):
@@ -345,6 +358,25 @@ def test_more_streams_than_workspaces(ctx, qrm):
         c.check_forward()
         c.check_backward()
         ctx.qrm_release_stream(s)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("shape", [(3, 100, 700, 2, 1, 64), (3, 70, 300, 2, 2, 45), (2, 1, 5000, 8, 2, 128), (1, 260, 390, 1, 1, 512)])
+def test_nothing_is_read_from_a_workspace_that_was_not_written(qrm, shape, dtype):
+    """A workspace full of NaNs gives the bits of one of small numbers: splits that short images do not have, rows that are not there, copies of unaligned rows."""
+    got = []
+    for fill in (0x01, 0xFF):
+        other = qrm.Context(rs=dict(m=4, prim_poly=0x13, n=12, k=8, fcr=1))
+        other.qrm_diag_set_flags(qrm.binding.QRM_DIAG_POISON_WORKSPACE | fill << 8)
+        n, lq, lk = shape[:3]
+        c = Case(qrm, *shape, dtype, causal=True, q_len=[lq, max(1, lq // 3), 0][:n], k_len=[lk // 9, lk, lk // 2][:n], seed=8)
+        c.forward(other)
+        c.backward(other)
+        torch.cuda.synchronize()
+        got.append([t.clone() for t in (c.o, c.lse, c.dq, c.dk, c.dv)])
+        other.close()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert all(bool(torch.isfinite(t.float()).all()) for i, t in enumerate(got[0]) if i != 1)
 
 
 def test_no_rows(ctx, qrm):
