@@ -242,7 +242,7 @@ template <int M> __device__ __forceinline__ float column_sum(float v)
     return v + __shfl_xor(v, 32);
 }
 
-constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLog2E = 1.44269504088896341f;
 
 // Where a workgroup is.  Workgroups that walk down the same keys are on one die, whose cache then serves them all, where there are eight groups of heads that
 // share keys and more (consecutive workgroups are dealt to the eight dies in turn), or a number of them that divides eight; of a group's, those of one split
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     typedef Tile<T, DP> L;
     constexpr int R = TK / X::NG, DH = DP / SHARE, AHEAD = 6; // scores of a lane, elements of a wavefront
     constexpr int TILES = NBUF * 2 * TK * L::PB, SWAP = R * 256; // exchanged: a wavefront's scores
-    constexpr float GROWS = std::is_same<T, f16_t>::value ? 4.f : 8.f, LIFT = std::is_same<T, f16_t>::value ? 11.f : 0.f;
+    constexpr float GROWS = std::is_same<T, f16_t>::value ? 4.f : 8.f, LIFT = attn_lift(std::is_same<T, f16_t>::value), FAR = 0x1p14f;
     constexpr bool TURNS = NBUF == 1; // keys and values take turns: the one is on its way while the other is used
     static_assert(SHARE > 1 || !TURNS, "in turns there is a barrier between keys and values");
     __shared__ alignas(256) uint8_t lds[TILES + (SHARE > 1 ? WAVES * SWAP : 0)];
@@ -351,8 +351,9 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
     wait_known_loads();
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)lds, mine = lds0 + e0 * (int)sizeof(T);
     const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
-    float top = -INFINITY, limit = -INFINITY, sums[4] = {}; // of the raw scores; 2^GROWS above, in powers of two; of this lane's probabilities
-    const float c = a.scale * kLog2E;
+    float top = -INFINITY, limit = -INFINITY, sums[4] = {}; // of the raw scores; what is 2^GROWS times as likely; of this lane's probabilities
+    const float c = a.scale * kLog2E, grows = 0.999f * GROWS * __builtin_amdgcn_rcpf(c);
+    bool far = false; // of the wavefront
     for (int t = from; t < to; ++t) {
         wait_loads();
         attn_barrier();
@@ -400,17 +401,27 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
             float high = score(0);
 #pragma unroll
             for (int r = 1; r < R; ++r) high = fmaxf(high, score(r));
-            if (__any(high * c > limit)) {
+            if (__any(high > limit)) {
                 const float now = fmaxf(top, column_max<M>(high));
                 const float less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - now) * c);
                 top = now;
-                limit = __builtin_fmaf(now, c, GROWS);
+                limit = now + grows;
+                if ((limit - now) * c > GROWS) limit = now; // (rounded up, or past 32 bits' largest)
+                far = __any(top != -INFINITY && !(fabsf(top * c) < FAR));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sums[e] *= less;
 #pragma unroll
                 for (int d = 0; d < DH / M; ++d) o[d] *= less;
             }
-            const float about = top == -INFINITY ? 0.f : __builtin_fmaf(top, c, -LIFT);
+            // Where the largest, in powers of two, is FAR and more from zero, it is subtracted from the scores as they are: there the rounding of its product with the scale
+            // is a factor that counts (2^4 at 1e8; f16 leaves room for 2).  Nearer, that is at most 1 + 2^-11, no more than the score's own rounding makes, and the subtraction is
+            // spared (2 x 8192 causal rows: 537 us with it, 524 without).
+            const float base = top == -INFINITY ? 0.f : top;
+            if (far) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) s[r / X::C][r % X::C] -= base;
+            }
+            const float about = far ? -LIFT : __builtin_fmaf(base, c, -LIFT);
             typename X::frag p[TK / X::KK];
             float chance[R];
 #pragma unroll
@@ -431,18 +442,19 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         }
     }
     const float sum = column_sum<M>(sums[0] + sums[1] + (sums[2] + sums[3]));
-    const bool some = top != -INFINITY || sum != sum; // (scores above 32 bits' largest: a sum of 0 about infinity, which is no number in what follows)
+    const bool some = top != -INFINITY || sum != sum;
     row = row0 + again(col), pos = attn_position(a, row), head = at.kv * a.group + (row - pos * a.group);
-    const float about = top == -INFINITY ? 0.f : __builtin_fmaf(top, c, -LIFT);
-    if (split.count > 1) { // a part of a row: results, and their sum about 2^about
+    const float base = top == -INFINITY ? 0.f : top;
+    if (split.count > 1) { // a part of a row: results, and their sum about the largest score
         const int64_t slot = attn_slot(a, at);
-        if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(some ? about : -INFINITY, sum);
+        if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(some ? base : -INFINITY, sum);
         store_part<M, WAVES>(a.part, slot, wave, lane, 1.f, o);
         return;
     }
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
-    if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = some ? (about + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
-    const float inv = some ? 1.f / sum : 0.f;
+    const float lse = some ? attn_log_sum(base, a.scale, sum, LIFT) : -INFINITY;
+    if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = lse;
+    const float inv = some ? lse == lse ? 1.f / sum : lse : 0.f;
     if (row >= rows) return;
     T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
 #pragma unroll

@@ -16,7 +16,7 @@ hipError_t launch_attention_backward_f16(const AttnArgs &by_q, const AttnArgs &b
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kLog2E = 1.44269504088896341f;
 
 uint32_t blocks_of(int64_t items) { return (uint32_t)((items + kThreads - 1) / kThreads); }
 
@@ -65,7 +65,7 @@ struct JoinJob {
     Quotient by_pairs, by_blocks; // by_blocks: of a wavefront
 };
 constexpr int kAhead = 4;
-// KEYS: rows are those of keys.  SUMS: forward, (power of two that a row's results are about, their sum).
+// KEYS: rows are those of keys.  SUMS: forward, (raw score that a row's results are about, their sum).
 template <typename T, bool KEYS, bool SUMS> __device__ __forceinline__ void join_part(const AttnArgs &a, const JoinJob &j, const JoinTo &to)
 {
     const AttnShape &h = j.shape;
@@ -88,6 +88,7 @@ template <typename T, bool KEYS, bool SUMS> __device__ __forceinline__ void join
     float by_sum = 1.f;
     if constexpr (SUMS) {
         const float2 *const sums = (const float2 *)a.part_sums + which * (int64_t)a.columns + column;
+        const float c = a.scale * kLog2E, lift = attn_lift(std::is_same<T, f16_t>::value);
         float top = -INFINITY, sum = 0.f; // (one pass: a split's sums and its results are on their way together)
         for (int k0 = 0; k0 < splits; k0 += kAhead) {
             float2 s[kAhead];
@@ -103,7 +104,7 @@ template <typename T, bool KEYS, bool SUMS> __device__ __forceinline__ void join
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (k0 + i >= splits) break;
-                const float now = fmaxf(top, s[i].x), less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now), by = s[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[i].x - now);
+                const float now = fmaxf(top, s[i].x), less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - now) * c), by = s[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s[i].x - now) * c);
                 top = now;
                 sum = sum * less + s[i].y * by;
 #pragma unroll
@@ -111,8 +112,9 @@ template <typename T, bool KEYS, bool SUMS> __device__ __forceinline__ void join
             }
         }
         const bool some = top != -INFINITY;
-        by_sum = some ? 1.f / sum : 0.f;
-        if (block == 0 && lane < h.m && wave % h.share == 0 && a.lse) a.lse[((int64_t)n * a.heads + head) * a.Lq + pos] = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+        const float lse = some ? attn_log_sum(top, a.scale, sum, lift) : -INFINITY;
+        by_sum = some ? lse == lse ? 1.f / sum : lse : 0.f;
+        if (block == 0 && lane < h.m && wave % h.share == 0 && a.lse) a.lse[((int64_t)n * a.heads + head) * a.Lq + pos] = lse;
     } else if (!KEYS || r < k_len) {
         for (int k0 = 0; k0 < splits; k0 += kAhead) {
             f32x4 p[kAhead][2];

@@ -203,7 +203,7 @@ struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie
     void *o, *dq, *dk, *dv;
     float *lse;                        // [N,heads,Lq]
     const float *row_lse, *row_delta;  // backward, [N,heads,Lq]: minus log-sums over the scale (-inf: the row sees nothing), minus sums of dy o
-    float *part, *part_sums;           // splits > 1: their results, and forward (power of two, sum) of each row (store_part)
+    float *part, *part_sums;           // splits > 1: their results, and forward (raw score, sum about it) of each row (store_part)
     float *part_k, *part_v;
     const int32_t *q_len, *k_len;      // [N] or null
     int64_t q_row, q_head, q_image, k_row, k_head, k_image, v_row, v_head, v_image, o_row, o_head, o_image;
@@ -269,6 +269,14 @@ __device__ __forceinline__ AttnSplit attn_split(const AttnArgs &a, int tiles, in
     return AttnSplit{count, which * each, min(tiles, (which + 1) * each)};
 }
 __device__ __forceinline__ int attn_length(const int32_t *lens, int n, int all) { return lens ? max(0, min(lens[n], all)) : all; }
+// Forward, probabilities of f16 are taken times two to that (attention_kernel).
+constexpr float attn_lift(bool f16) { return f16 ? 11.f : 0.f; }
+// The log-sum of a row whose probabilities about the raw score `top`, lifted, have the sum `sum`; above 32 bits' largest it is no number.
+__device__ __forceinline__ float attn_log_sum(float top, float scale, float sum, float lift)
+{
+    const float lse = __builtin_fmaf(top, scale, (__builtin_amdgcn_logf(sum) - lift) * 0.693147180559945309f);
+    return lse < INFINITY ? lse : NAN;
+}
 // Query rows are counted position by position, the heads of a group side by side.
 __device__ __forceinline__ int attn_position(const AttnArgs &a, int row) { return a.by_group.of(row); }
 // Tiles of keys that any of a part's query rows sees; tiles of a head's queries (behind `skip`) that see any of a part's keys.

@@ -1,0 +1,44 @@
+"""Attention at the edges of its numbers, on the GPU through the C ABI: large scores, values that are not finite, weights near a type's smallest.
+
+u = 2^-24 is half a unit in the last place of 32 bits.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as at
+from tests.test_gpu_attention import HALF, IDS, TYPES, U, Case, ctx, desc_of, f64, qrm  # noqa: F401 (fixtures)
+
+pytestmark = pytest.mark.gpu
+
+# (queries, keys, query heads, key heads, elements): one tile, many tiles, splits that are joined, few rows, rows of two wavefronts
+LARGE = [(1, 1, 1, 1, 64), (40, 3, 2, 2, 64), (3, 5000, 2, 1, 64), (100, 700, 2, 2, 128), (70, 90, 1, 1, 512), (40, 3000, 1, 1, 512), (1, 900, 4, 1, 512)]
+
+
+@pytest.mark.parametrize("power", [-3, 4, 37, 80])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_large_scores(ctx, qrm, dtype, shape, sign, power):
+    """Scores of 1e8 and more, up to 1e33: three keys (first, middle and last) have the largest, all others half of it or twice (where negative).  Each of the three has
+    a third of the weight: differences of 0 are exact in any format, those of the others leave nothing.  o: a few roundings of the mean and half a step of the type; lse: the
+    sums of powers of two are exact, so the product with the scale and the sum with log 3 are all that is rounded."""
+    lq, lk, heads, kv, d = shape
+    top = 1.25 * 2.0 ** (11 if dtype == torch.float16 or power < 80 else 20)
+    scale = 2.0 ** min(power, 60)
+    g = torch.Generator().manual_seed(lk + d)
+    winners = sorted({0, lk // 2, lk - 1})
+    q = torch.full((2, lq, heads, d), sign * top, dtype=dtype, device="cuda")
+    k = torch.full((2, lk, kv, d), top / 2 if sign > 0 else top, dtype=dtype, device="cuda")
+    k[:, winners] = top if sign > 0 else top / 2
+    v = (torch.randn((2, lk, kv, d), generator=g) + 0.5).to(dtype).cuda()
+    o, lse = torch.empty_like(q), torch.empty((2, heads, lq), device="cuda")
+    ctx.qrm_attention(desc_of(qrm, q, k, v, o, False, scale), q, k, v, o, lse, None, None, 0)
+    mean = f64(v)[:, winners].mean(axis=1)                                     # [2, kv, d]
+    want = np.repeat(mean, heads // kv, axis=1)[:, None]
+    size = np.repeat(np.abs(f64(v)[:, winners]).mean(axis=1), heads // kv, axis=1)[:, None]
+    assert (np.abs(f64(o) - want) <= 8 * U * size + HALF[dtype] * np.abs(want) * 1.01).all()
+    want_lse = scale * sign * d * top * (top if sign > 0 else top / 2) + math.log(len(winners))
+    assert float((lse.double() - want_lse).abs().max()) <= 4 * U * abs(want_lse)
