@@ -443,8 +443,8 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
  * do has o's strides, dq, dk and dv those of q, k and v; each of the three may be NULL (not wanted).  16-bit types: P and dS are rounded to the type (f16:
  * with a factor that keeps a row's largest in range) for the second products.  Rows that are not there have gradients of zero, also where do is not finite.
  * P of the backward pass is off by about 2^-22 |lse| of itself, for an lse of 32 bits says no more: where |lse| is above 2^20 gradients mean nothing.
- * The same bits from call to call.  A value that is not finite in a row that is there reaches the outputs of its image and key head, no others. Scores above
- * 32 bits' largest make their row's o and lse no numbers.
+ * The same bits from call to call.  A value that is not finite in a row that is there reaches the outputs of its image and key head, no others.  A row
+ * that sees keys and whose largest score is past what 32 bits hold, up or down, before the scale or after it, has an o and lse that are no numbers.
  * Errors: QRM_E_INVALID (NULL pointer, N, Lq or Lk < 0, kv_heads that do not divide heads, D < 1, an unknown type, causal not 0 or 1, scale not above
  * zero, strides with which rows overlap, an output that is an input, two outputs that are one, no output, a pointer not aligned to its elements),
  * QRM_E_UNSUPPORTED (D above QRM_ATTENTION_MAX_D; scale outside 2^-64 .. 2^64; N, Lk or Lq * heads above 2^30, N * heads above 2^23, 2^32 threads and more for the rows of

@@ -442,19 +442,18 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         }
     }
     const float sum = column_sum<M>(sums[0] + sums[1] + (sums[2] + sums[3]));
-    const bool some = top != -INFINITY || sum != sum;
     row = row0 + again(col), pos = attn_position(a, row), head = at.kv * a.group + (row - pos * a.group);
     const float base = top == -INFINITY ? 0.f : top;
     if (split.count > 1) { // a part of a row: results, and their sum about the largest score
         const int64_t slot = attn_slot(a, at);
-        if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(some ? base : -INFINITY, sum);
+        if (g == 0 && half == 0) ((float2 *)a.part_sums)[slot * a.columns + row - at.part * a.columns] = make_float2(top != -INFINITY || sum != sum ? base : -INFINITY, sum);
         store_part<M, WAVES>(a.part, slot, wave, lane, 1.f, o);
         return;
     }
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
-    const float lse = some ? attn_log_sum(base, a.scale, sum, LIFT) : -INFINITY;
+    const float lse = seen ? attn_log_sum(base, a.scale, sum, LIFT) : -INFINITY;
     if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = lse;
-    const float inv = some ? lse == lse ? 1.f / sum : lse : 0.f;
+    const float inv = seen ? lse == lse ? 1.f / sum : lse : 0.f;
     if (row >= rows) return;
     T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
 #pragma unroll

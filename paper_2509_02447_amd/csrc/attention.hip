@@ -111,9 +111,9 @@ template <typename T, bool KEYS, bool SUMS> __device__ __forceinline__ void join
                 for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = o[e / 4][e % 4] * less + (by == 0.f ? 0.f : p[i][e / 4][e % 4] * by);
             }
         }
-        const bool some = top != -INFINITY;
-        const float lse = some ? attn_log_sum(top, a.scale, sum, lift) : -INFINITY;
-        by_sum = some ? lse == lse ? 1.f / sum : lse : 0.f;
+        const bool sees = pos < q_len && (a.causal ? min(k_len, pos + k_len - q_len + 1) : k_len) > 0;
+        const float lse = sees ? attn_log_sum(top, a.scale, sum, lift) : -INFINITY;
+        by_sum = sees ? lse == lse ? 1.f / sum : lse : 0.f;
         if (block == 0 && lane < h.m && wave % h.share == 0 && a.lse) a.lse[((int64_t)n * a.heads + head) * a.Lq + pos] = lse;
     } else if (!KEYS || r < k_len) {
         for (int k0 = 0; k0 < splits; k0 += kAhead) {

@@ -271,11 +271,12 @@ __device__ __forceinline__ AttnSplit attn_split(const AttnArgs &a, int tiles, in
 __device__ __forceinline__ int attn_length(const int32_t *lens, int n, int all) { return lens ? max(0, min(lens[n], all)) : all; }
 // Forward, probabilities of f16 are taken times two to that (attention_kernel).
 constexpr float attn_lift(bool f16) { return f16 ? 11.f : 0.f; }
-// The log-sum of a row whose probabilities about the raw score `top`, lifted, have the sum `sum`; above 32 bits' largest it is no number.
+// The log-sum of a row whose probabilities about the raw score `top`, lifted, have the sum `sum`.  Past 32 bits' largest, up or down, it is no number: -inf is the
+// log-sum of a row that sees nothing.
 __device__ __forceinline__ float attn_log_sum(float top, float scale, float sum, float lift)
 {
     const float lse = __builtin_fmaf(top, scale, (__builtin_amdgcn_logf(sum) - lift) * 0.693147180559945309f);
-    return lse < INFINITY ? lse : NAN;
+    return fabsf(lse) < INFINITY ? lse : NAN;
 }
 // Query rows are counted position by position, the heads of a group side by side.
 __device__ __forceinline__ int attn_position(const AttnArgs &a, int row) { return a.by_group.of(row); }

@@ -42,3 +42,43 @@ def test_large_scores(ctx, qrm, dtype, shape, sign, power):
     assert (np.abs(f64(o) - want) <= 8 * U * size + HALF[dtype] * np.abs(want) * 1.01).all()
     want_lse = scale * sign * d * top * (top if sign > 0 else top / 2) + math.log(len(winners))
     assert float((lse.double() - want_lse).abs().max()) <= 4 * U * abs(want_lse)
+
+
+@pytest.mark.parametrize("shape", [(3, 5000, 2, 1, 64), (100, 130, 2, 2, 64), (70, 90, 1, 1, 512), (40, 3000, 1, 1, 512)], ids=str)
+@pytest.mark.parametrize("powers", [(40, 30, 60), (100, 100, 0)], ids=["scaled", "raw"])
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=IDS[:2])
+def test_scores_below_32_bits_are_no_rows_that_see_nothing(ctx, qrm, dtype, powers, shape):
+    """Scores of -2^136 after the scale, or -2^206 before it: no numbers, whatever the rows beside them see."""
+    lq, lk, heads, kv, d = shape
+    q = torch.full((2, lq, heads, d), -2.0 ** powers[0], dtype=dtype, device="cuda")
+    k, v = torch.full((2, lk, kv, d), 2.0 ** powers[1], dtype=dtype, device="cuda"), torch.ones((2, lk, kv, d), dtype=dtype, device="cuda")
+    q[1, -1] = 0.0                                                             # (scores of zero: the mean of the values)
+    o, lse = torch.empty_like(q), torch.empty((2, heads, lq), device="cuda")
+    desc = desc_of(qrm, q, k, v, o, False, 2.0 ** powers[2])
+    ctx.qrm_attention(desc, q, k, v, o, lse, None, None, 0)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(o[0]).all()) and bool(torch.isnan(lse[0]).all()) and bool(torch.isnan(o[1, :-1]).all()) and bool(torch.isnan(lse[1, :, :-1]).all())
+    # lk equal weights and values of one: a rounding a key in the sums on either side, and half a step
+    assert float((o[1, -1].double() - 1.0).abs().max()) <= 2 * lk * U + HALF[dtype]
+    assert float((lse[1, :, -1].double() - math.log(lk)).abs().max()) <= (lk + 16) * U * 1.01
+    # one key of score 0 among them has all of the weight
+    k[:, lk // 2] = 0.0
+    v[:, lk // 2] = 3.0
+    ctx.qrm_attention(desc, q, k, v, o, lse, None, None, 0)
+    torch.cuda.synchronize()
+    assert bool((o[0] == 3.0).all()) and bool((lse[0] == 0.0).all())
+
+
+@pytest.mark.parametrize("shape", [(3, 5000, 2, 1, 64), (100, 130, 2, 2, 64), (40, 3000, 1, 1, 512)], ids=str)
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=IDS[:2])
+def test_raw_scores_above_32_bits(ctx, qrm, dtype, shape):
+    """One key whose products pass 32 bits' largest: the rows that see it are no numbers, the others are as if it were not there."""
+    lq, lk, heads, kv, d = shape
+    q = torch.full((1, lq, heads, d), 2.0 ** 70, dtype=dtype, device="cuda")
+    k, v = torch.zeros((1, lk, kv, d), dtype=dtype, device="cuda"), torch.ones((1, lk, kv, d), dtype=dtype, device="cuda")
+    q[:, -1], k[:, lk // 3] = 0.0, 2.0 ** 70
+    o, lse = torch.empty_like(q), torch.empty((1, heads, lq), device="cuda")
+    ctx.qrm_attention(desc_of(qrm, q, k, v, o, False, 1.0), q, k, v, o, lse, None, None, 0)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(o[0, :-1]).all()) and bool(torch.isnan(lse[..., :-1]).all())
+    assert float((o[0, -1].double() - 1.0).abs().max()) <= 2 * lk * U + HALF[dtype]
