@@ -107,8 +107,10 @@ template <typename T, bool KEYS, bool SUMS> __device__ __forceinline__ void join
                 const float now = fmaxf(top, s[i].x), less = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - now) * c), by = s[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s[i].x - now) * c);
                 top = now;
                 sum = sum * less + s[i].y * by;
+                // (a split of which the row sees nothing adds nothing; one of no weight beside the others adds zeros, and what is not finite stays so)
+                const bool none = s[i].x == -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = o[e / 4][e % 4] * less + (by == 0.f ? 0.f : p[i][e / 4][e % 4] * by);
+                for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = o[e / 4][e % 4] * less + (none ? 0.f : p[i][e / 4][e % 4] * by);
             }
         }
         const bool sees = pos < q_len && (a.causal ? min(k_len, pos + k_len - q_len + 1) : k_len) > 0;

@@ -82,3 +82,21 @@ def test_raw_scores_above_32_bits(ctx, qrm, dtype, shape):
     torch.cuda.synchronize()
     assert bool(torch.isnan(o[0, :-1]).all()) and bool(torch.isnan(lse[..., :-1]).all())
     assert float((o[0, -1].double() - 1.0).abs().max()) <= 2 * lk * U + HALF[dtype]
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("shape", [(1, 5, 2, 1, 64), (3, 5000, 2, 1, 64), (40, 3000, 1, 1, 512), (100, 3000, 1, 1, 128)], ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_a_value_that_is_not_finite_reaches_rows_in_which_it_has_no_weight(ctx, qrm, dtype, shape, bad):
+    """Keys of the second half have scores 200 under those of the first, weights that 32 bits do not hold: 0 times such a value is no number, however the keys are split."""
+    lq, lk, heads, kv, d = shape
+    q = torch.full((1, lq, heads, d), 1.0, dtype=dtype, device="cuda")
+    k, v = torch.zeros((1, lk, kv, d), dtype=dtype, device="cuda"), torch.ones((1, lk, kv, d), dtype=dtype, device="cuda")
+    k[:, lk // 2:, :, 0] = -200.0
+    v[0, lk - 1, 0, 3] = bad
+    o = torch.empty_like(q)
+    ctx.qrm_attention(desc_of(qrm, q, k, v, o, False, 1.0), q, k, v, o, None, None, None, 0)
+    torch.cuda.synchronize()
+    assert not bool(torch.isfinite(o[..., 3]).any())
+    o[..., 3] = 1.0
+    assert float((o.double() - 1.0).abs().max()) <= 2 * lk * U + HALF[dtype]
