@@ -450,6 +450,10 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         store_part<M, WAVES>(a.part, slot, wave, lane, 1.f, o);
         return;
     }
+    if (!seen) { // (its weights are zeros, which times values that are not finite are not)
+#pragma unroll
+        for (int d = 0; d < DH / M; ++d) o[d] = typename X::acc{};
+    }
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
     const float lse = seen ? attn_log_sum(base, a.scale, sum, LIFT) : -INFINITY;
     if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = lse;
@@ -634,6 +638,10 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF> __d
             attn_barrier();
             load(t + 1);
         }
+    }
+    if (!seen) { // (as forward)
+#pragma unroll
+        for (int d = 0; d < DH / M; ++d) dq[d] = typename X::acc{};
     }
     const float by = a.scale / lift.by;
     if (split.count > 1) {

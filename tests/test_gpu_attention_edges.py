@@ -100,3 +100,26 @@ def test_a_value_that_is_not_finite_reaches_rows_in_which_it_has_no_weight(ctx, 
     assert not bool(torch.isfinite(o[..., 3]).any())
     o[..., 3] = 1.0
     assert float((o.double() - 1.0).abs().max()) <= 2 * lk * U + HALF[dtype]
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(100, 130, 4, 2, 64), (90, 40, 2, 1, 512), (3, 5000, 2, 1, 64), (300, 2000, 1, 1, 128), (70, 90, 2, 2, 45)], ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_rows_that_see_nothing_stay_zeros_beside_values_that_are_not_finite(ctx, qrm, dtype, shape, causal, bad):
+    """Keys and values that are there hold NaNs or infinities: rows that are not there, and the first rows of more queries than keys, have nothing of them."""
+    lq, lk, heads, kv, d = shape
+    q_len, k_len = [2 * lq // 3, lq, 1], [lk, max(1, min(lk, lq) // 2), lk // 2]
+    c = Case(qrm, 3, lq, lk, heads, kv, d, dtype, causal=causal, q_len=q_len, k_len=k_len, seed=3)
+    for i, m in enumerate(k_len):
+        c.v[i, m - 1] = bad
+        c.k[i, m // 2] = bad
+    c.forward(ctx)
+    c.backward(ctx)
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(q_len, k_len)):
+        first = max(0, a - b) if causal else 0                                 # rows that see nothing
+        for rows in (slice(0, first), slice(a, lq)):
+            assert bool((c.o[i, rows] == 0).all()) and bool((c.dq[i, rows] == 0).all()) and bool(torch.isneginf(c.lse[i, :, rows]).all())
+        assert bool((c.dk[i, b:] == 0).all()) and bool((c.dv[i, b:] == 0).all())
+        assert not bool(torch.isfinite(c.o[i, a - 1]).any())                   # (the last one sees all keys)
