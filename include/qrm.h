@@ -441,7 +441,7 @@ QRM_API qrm_status qrm_group_norm_backward(qrm_ctx *ctx, const qrm_group_norm_de
  * Backward: with dP_ij = do_i . v_j, delta_i = do_i . o_i, dS_ij = P_ij (dP_ij - delta_i), P from S and the given lse
  *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij do_i   (dk, dv over all heads that share the key head).
  * do has o's strides, dq, dk and dv those of q, k and v; each of the three may be NULL (not wanted).  16-bit types: P and dS are rounded to the type (f16:
- * with a factor that keeps a row's largest in range) for the second products.  Rows that are not there have gradients of zero, also where do is not finite;
+ * with a factor that keeps the largest of a query or key in range) for the second products.  Rows that are not there have gradients of zero, also where do is not finite;
  * dq of a row that sees nothing is zero.
  * P of the backward pass is off by about 2^-22 |lse| of itself, for an lse of 32 bits says no more: where |lse| is above 2^20 gradients mean nothing.
  * The same bits from call to call.  A value that is not finite in a row that is there reaches the outputs of its image and key head, no others.  A row

@@ -469,21 +469,28 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 
 // ---------------------------------------------------------------- backward
 
-// f16 numbers reach from 2^-24 to 2^16 only.  A column's numbers are multiplied by a power of two that brings the largest so far to 2^14 .. 2^15 before
-// they are rounded; when a larger one comes, what has been summed is scaled down with the factor.  (bf16 and f32 need none.)  Probabilities, which are
-// not above one, are multiplied by 2^14.
+// f16 numbers reach from 2^-24 to 2^16 only.  A column's numbers are multiplied by a power of two that brings the largest so far to 2^11 .. 2^12 before
+// they are rounded; when one of 2^15 comes, what has been summed is scaled down with the factor, which that room makes rare (f16, 2 x 4096 causal rows of 16
+// heads of 128: 543 us, brought to 2^14 558).  Probabilities of a key too: it may have little weight in all rows, whose gradients may be large.  (bf16 and f32 need none.)
 template <typename T> struct Lift {
     static constexpr bool USED = std::is_same<T, f16_t>::value;
-    static constexpr float PROBABILITY = USED ? 0x1p14f : 1.f;
     float by = USED ? 0x1p100f : 1.f;
     __device__ __forceinline__ bool over(float high) const { return high * by > 0x1p15f; }
     // For numbers of a column whose largest magnitude is `high`; returns what to multiply the column's sums by.
     __device__ __forceinline__ float fit(float high)
     {
         if (!over(high)) return 1.f;
-        const float now = __builtin_ldexpf(1.f, 14 + 127 - (int)(__float_as_uint(high) >> 23)), less = now / by;
+        const float now = __builtin_ldexpf(1.f, 11 + 127 - (int)(__float_as_uint(high) >> 23)), less = now / by;
         by = now;
         return less;
+    }
+    // The same of the lanes' own largest numbers; they ask each other only where one is over.
+    template <int M, typename ACC, int COUNT> __device__ __forceinline__ void follow(float high, ACC (&sums)[COUNT])
+    {
+        if (!__any(over(high))) return;
+        const float less = fit(column_max<M>(high));
+#pragma unroll
+        for (int d = 0; d < COUNT; ++d) sums[d] *= less;
     }
 };
 
@@ -613,12 +620,7 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF> __d
             if constexpr (Lift<T>::USED) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) high = fmaxf(high, fabsf(ds[r]));
-                high = column_max<M>(high);
-                if (__any(lift.over(high))) {
-                    const float less = lift.fit(high);
-#pragma unroll
-                    for (int d = 0; d < DH / M; ++d) dq[d] *= less;
-                }
+                lift.template follow<M>(high, dq);
             }
             typename X::frag p[STEP / X::KK];
 #pragma unroll
@@ -741,7 +743,7 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, boo
     const uint32_t along0 = mine + L::template along_at<M>(col, g), across0 = mine + L::template across_at<M>(lane);
     const uint32_t values = lds0 + NBUF * BUF + L::template along_at<M>(wave * M + col, g);
     typename X::acc dk[DK ? DH / M : 1] = {}, dv[DV ? DH / M : 1] = {};
-    Lift<T> lift;
+    Lift<T> lift, lift_p; // of score gradients, of probabilities
     const float c = a.scale * kLog2E;
     for (int t = from; t < to; ++t) {
         wait_loads();
@@ -825,17 +827,18 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, boo
                 float high = 0.f;
 #pragma unroll
                 for (int r = 0; r < R; ++r) high = fmaxf(high, fabsf(ds[r]));
-                high = column_max<M>(high);
-                if (__any(lift.over(high))) {
-                    const float less = lift.fit(high);
+                lift.template follow<M>(high, dk);
+            }
+            if constexpr (Lift<T>::USED && DV) {
+                float high = 0.f;
 #pragma unroll
-                    for (int d = 0; d < DH / M; ++d) dk[d] *= less;
-                }
+                for (int r = 0; r < R; ++r) high = fmaxf(high, pr[r]);
+                lift_p.template follow<M>(high, dv);
             }
             typename X::frag p[STEP / X::KK], z[STEP / X::KK];
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                if (Lift<T>::USED) pr[r] *= Lift<T>::PROBABILITY, ds[r] *= lift.by;
+                if (Lift<T>::USED) pr[r] *= lift_p.by, ds[r] *= lift.by;
 #pragma unroll
             for (int u = 0; u < STEP / X::KK; ++u) p[u] = pack_eight<T>(pr + 8 * u), z[u] = pack_eight<T>(ds + 8 * u);
 #pragma unroll
@@ -853,7 +856,7 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, boo
             load(ahead);
         }
     }
-    const float by_k = a.scale / lift.by, by_v = 1.f / Lift<T>::PROBABILITY;
+    const float by_k = a.scale / lift.by, by_v = 1.f / lift_p.by;
     auto write = [&](const auto &sums, float by, T *out) {
 #pragma unroll
         for (int d = 0; d < DH / M; ++d)

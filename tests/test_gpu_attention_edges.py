@@ -123,3 +123,30 @@ def test_rows_that_see_nothing_stay_zeros_beside_values_that_are_not_finite(ctx,
             assert bool((c.o[i, rows] == 0).all()) and bool((c.dq[i, rows] == 0).all()) and bool(torch.isneginf(c.lse[i, :, rows]).all())
         assert bool((c.dk[i, b:] == 0).all()) and bool((c.dv[i, b:] == 0).all())
         assert not bool(torch.isfinite(c.o[i, a - 1]).any())                   # (the last one sees all keys)
+
+
+@pytest.mark.parametrize("score", [-18.0, -24.0, -28.0, -32.0])
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_gradients_of_values_of_little_weight(ctx, qrm, dtype, score):
+    """Keys of weight exp(-18) .. exp(-32) in each of 2^15 rows, whose gradients are 2^10: exp(-28) is under 2^-40, the sums are not small.  Half a step each for weights and
+    results (f16: 2^-25 at least); a rounding of equal summands for every two rows; a score's 32 + 8 roundings."""
+    lq, heads, lk, d = 4096, 8, 256, 32
+    q = torch.zeros((1, lq, heads, d), dtype=dtype, device="cuda")
+    k, v = (torch.zeros((1, lk, 1, d), dtype=dtype, device="cuda") for _ in range(2))
+    q[..., 0], k[..., 0] = 4.0, score / 4.0
+    k[0, 77] = 0.0
+    do = torch.full_like(q, 2.0 ** 10)
+    o, lse, dv = torch.empty_like(q), torch.empty((1, heads, lq), device="cuda"), torch.empty_like(v)
+    desc = desc_of(qrm, q, k, v, o, False, 1.0)
+    ctx.qrm_attention(desc, q, k, v, o, lse, None, None, 0)
+    ctx.qrm_attention_backward(desc, q, k, v, o, do, lse, None, None, dv, None, None, 0)
+    torch.cuda.synchronize()
+    rows, half, p = lq * heads, HALF[dtype], math.exp(score)
+    want = torch.full((lk, d), rows * 2.0 ** 10 * p / (1.0 + (lk - 1) * p), dtype=torch.float64)
+    want[77] /= p
+    tolerance = (2 * half + rows / 2 * U + (d + 8) * U * (1.0 - 2.0 * score)) * 1.01 * want + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    if dtype == torch.float16:
+        want[77] = math.inf                                                    # (2^25: more than the type holds)
+    err = (dv[0, :, 0].double().cpu() - want).abs()
+    err[77] = 0.0 if dtype == torch.float16 and bool(torch.isinf(dv[0, 77]).all()) else err[77]
+    assert bool((err <= tolerance).all()), float((err / tolerance).max())
