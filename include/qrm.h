@@ -503,7 +503,8 @@ QRM_API qrm_status qrm_attention_backward(qrm_ctx *ctx, const qrm_attention_desc
  * A gradient that is not finite makes the norm inf or NaN and the scale u * 0 or NaN; without any gradient the norm is 0 and the scale u.  The same bits from call to call.
  * qrm_adamw_scale_grads: out = grad * *d_scale, rounded once to grad_type, for other optimisers: h_outs HOST [n_tensors] of device pointers, each its
  * gradient's own (in place) or a buffer that overlaps nothing; NULL where the gradient is NULL, and only there.
- * Errors: as qrm_adamw_step where they apply, QRM_E_INVALID (max_norm not above zero (inf is: no clipping), d_norm and d_scale both NULL, an output at d_unscale, a missing output).
+ * Errors: as qrm_adamw_step where they apply, QRM_E_INVALID (max_norm not above zero (inf is: no clipping), d_norm and d_scale both NULL, an output at d_unscale, a missing output,
+ * one output for two gradients that have elements).
  */
 #define QRM_MOMENT_BLOCK 256
 typedef struct qrm_adamw qrm_adamw; /* opaque, library-owned */

@@ -5,6 +5,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <functional>
 #include <new>
 #include <vector>
 
@@ -90,6 +91,29 @@ qrm_status check_grads(qrm_ctx *c, const qrm_adamw *o, const void *const *h_grad
     const size_t bytes = type_bytes(o->types.grad);
     for (int i = 0; i < n; ++i)
         if (!aligned_to(h_grads[i], bytes)) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
+    return QRM_OK;
+}
+
+// Each output of its own (an output's elements are written once: a gradient that two tensors share, scaled in place, would be scaled once or twice).
+qrm_status check_outs(qrm_ctx *c, const qrm_adamw *o, void *const *h_outs)
+{
+    const int n = (int)o->first_piece.size() - 1;
+    auto there = [&](int i) { return h_outs[i] && o->first_piece[i + 1] != o->first_piece[i]; };
+    const void *last = nullptr;
+    bool rising = true; // (one behind the other, as tensors mostly are: nothing to sort)
+    for (int i = 0; i < n && rising; ++i)
+        if (there(i)) rising = std::less<const void *>()(last, h_outs[i]), last = h_outs[i];
+    if (rising) return QRM_OK;
+    try {
+        std::vector<const void *> all;
+        all.reserve(n);
+        for (int i = 0; i < n; ++i)
+            if (there(i)) all.push_back(h_outs[i]);
+        std::sort(all.begin(), all.end(), std::less<const void *>());
+        if (std::adjacent_find(all.begin(), all.end()) != all.end()) return fail(c, QRM_E_INVALID, "two outputs are one");
+    } catch (const std::bad_alloc &) {
+        return fail(c, QRM_E_NOMEM, "no host memory for the outputs");
+    }
     return QRM_OK;
 }
 
@@ -446,7 +470,7 @@ qrm_status qrm_adamw_scale_grads(qrm_ctx *c, qrm_adamw *o, const void *const *h_
         if (!h_grads[i] != !h_outs[i]) return fail(c, QRM_E_INVALID, "a gradient without an output, or the reverse");
         if (!aligned_to(h_outs[i], type_bytes(o->types.grad))) return fail(c, QRM_E_INVALID, "a pointer is not aligned to its elements");
     }
-    if ((st = start(c)) != QRM_OK) return st;
+    if ((st = check_outs(c, o, h_outs)) != QRM_OK || (st = start(c)) != QRM_OK) return st;
     for (int i = 0; i < n; i += kScaleGrads) {
         const int count = std::min(n - i, kScaleGrads);
         const uint32_t from = o->first_piece[i], to = o->first_piece[i + count];
