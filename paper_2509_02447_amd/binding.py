@@ -4,15 +4,12 @@ Tensors are torch CUDA(ROCm) tensors used purely as device memory; streams are t
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
 import os
-from operator import attrgetter
 from typing import Optional
 
 import numpy as np
 
-_DTYPE, _IS_CUDA = attrgetter("dtype"), attrgetter("is_cuda")
 QRM_OK, QRM_E_INVALID, QRM_E_UNSUPPORTED, QRM_E_NOMEM, QRM_E_DEVICE = 0, 1, 2, 3, 4
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -379,6 +376,16 @@ def attention_desc(N: int, Lq: int, Lk: int, heads: int, kv_heads: int, D: int, 
                           *[int(x) for lie in (q, k, v, o) for x in lie])
 
 
+def _tensor_addresses():
+    """The binding's own module for lists of tensors (csrc/tensors.cpp), which takes what torch's libraries have: torch is imported before it."""
+    import torch  # noqa: F401
+    try:
+        from . import _tensors
+    except ImportError as e:
+        raise ImportError("_tensors.so is missing or was built for another torch: run `python -m paper_2509_02447_amd.build`") from e
+    return _tensors.pointers
+
+
 def _hptr(t) -> Optional[int]:
     """Host pointer of a CPU torch tensor or a numpy array (or None)."""
     if t is None:
@@ -646,8 +653,8 @@ class AdamW:
         desc = _AdamwDesc(n, type_code(param), type_code(grad_type), QRM_BF16 if copy is None else type_code(copy),
                           {torch.float32: 32, torch.int8: 8}[moment])
         ctx._check(self._lib.qrm_adamw_create(ctx._h, C.byref(desc), rows, C.byref(self._h)))
-        self._n, self._grad_type, self._sizes = n, grad_type, [t["param"].numel() for t in self._keep]
-        self._array, self._tensor = C.c_void_p * max(1, n), torch.Tensor
+        self._grad_type, self._sizes = grad_type, (C.c_int64 * n)(*[t["param"].numel() for t in self._keep])
+        self._array, self._addresses = C.c_void_p * max(1, n), _tensor_addresses()
 
     @staticmethod
     def _check_sizes(t):
@@ -665,17 +672,7 @@ class AdamW:
         raise ValueError(f"all {what} of a plan have one type")
 
     def _pointers(self, grads):
-        assert len(grads) == self._n, "one gradient (or None) for each tensor"
-        some, sizes = grads, self._sizes
-        if any([g is None for g in grads]):
-            some, sizes = zip(*[(g, n) for g, n in zip(grads, sizes) if g is not None]) if any([g is not None for g in grads]) else ((), ())
-        tensor = self._tensor
-        # (attributes one by one over all tensors: a third of the time of a loop over tensors)
-        assert list(map(tensor.numel, some)) == list(sizes) and set(map(_DTYPE, some)) <= {self._grad_type} and all(map(_IS_CUDA, some)) and all(map(tensor.is_contiguous, some)), \
-            "gradients must have the plan's type and sizes, be contiguous and on the GPU"
-        if some is not grads:
-            return self._array(*[None if g is None else g.data_ptr() for g in grads])
-        return self._array.from_buffer(array.array("Q", map(tensor.data_ptr, grads)) if grads else bytearray(8))
+        return self._array.from_buffer(self._addresses(grads, self._sizes, self._grad_type))
 
     def qrm_adamw_grad_norm(self, grads, max_norm: float, d_norm, d_scale, d_unscale=None, stream=None):
         """grads as in qrm_adamw_step; d_norm, d_scale, d_unscale: f32 [1] on the device (or None)."""

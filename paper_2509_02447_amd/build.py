@@ -1,14 +1,16 @@
-"""Builds libqrm.so (hand-written HIP, gfx950 only) in-tree with hipcc."""
+"""Builds libqrm.so (hand-written HIP, gfx950 only) in-tree with hipcc, and the binding's module of host code (_tensors.so) beside it."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqrm.so")
+MODULE, MODULE_SOURCE = os.path.join(HERE, "_tensors.so"), "tensors.cpp"
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["qrm_api.hip", "extractor.hip", "rs_decode.hip", "tiles.hip", "qrm_noalloc.hip", "qrm_diag.hip", "qrm_plan.hip",
            "qrm_train.hip", "group_norm.hip", "group_norm_f32.hip", "group_norm_bf16.hip",
@@ -31,11 +33,17 @@ def hipcc() -> str:
 
 
 def stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS]
-    return any(os.path.getmtime(d) > t for d in deps)
+    newer = lambda out, deps: not os.path.exists(out) or any(os.path.getmtime(os.path.join(CSRC, d)) > os.path.getmtime(out) for d in deps)
+    return newer(LIB, SOURCES + HEADERS) or newer(MODULE, [MODULE_SOURCE])
+
+
+def build_module() -> str:
+    """Compile the CPython module against the torch that is installed."""
+    from torch.utils import cpp_extension
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden"] +
+                          ["-I" + p for p in [sysconfig.get_paths()["include"]] + cpp_extension.include_paths()] + [os.path.join(CSRC, MODULE_SOURCE), "-o", MODULE] +
+                          ["-L" + p for p in cpp_extension.library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10"])
+    return MODULE
 
 
 def build(force: bool = True, verbose: bool = False) -> str:
@@ -54,7 +62,9 @@ def build(force: bool = True, verbose: bool = False) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as pool:
+        module = pool.submit(build_module)
         objs = list(pool.map(compile_one, SOURCES))
+        module.result()
     subprocess.check_call([cc] + FLAGS + ["-shared"] + objs + ["-o", LIB])
     return LIB
 
