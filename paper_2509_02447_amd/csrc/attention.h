@@ -450,21 +450,18 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
         store_part<M, WAVES>(a.part, slot, wave, lane, 1.f, o);
         return;
     }
-    if (!seen) { // (its weights are zeros, which times values that are not finite are not)
-#pragma unroll
-        for (int d = 0; d < DH / M; ++d) o[d] = typename X::acc{};
-    }
     const int64_t index = ((int64_t)at.n * a.heads + head) * a.Lq + pos;
     const float lse = seen ? attn_log_sum(base, a.scale, sum, LIFT) : -INFINITY;
     if (g == 0 && half == 0 && a.lse && row < rows) a.lse[index] = lse;
     const float inv = seen ? lse == lse ? 1.f / sum : lse : 0.f;
     if (row >= rows) return;
     T *const o_row = (T *)a.o + at.n * a.o_image + pos * a.o_row + head * a.o_head;
+    auto result = [&](float sum) { return seen ? sum * inv : 0.f; }; // (a row that sees nothing: weights of zero, which times values that are not finite are not)
 #pragma unroll
     for (int d = 0; d < DH / M; ++d)
 #pragma unroll
         for (int r = 0; r < X::C; r += 4)
-            store_four<T>(o_row, e0 + d * M + X::row_of(r, g), a.D, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+            store_four<T>(o_row, e0 + d * M + X::row_of(r, g), a.D, result(o[d][r]), result(o[d][r + 1]), result(o[d][r + 2]), result(o[d][r + 3]));
 }
 
 // ---------------------------------------------------------------- backward
