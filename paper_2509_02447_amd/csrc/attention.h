@@ -578,7 +578,7 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF> __d
         wait_loads();
         attn_barrier();
         if (NBUF > 1 && t + 1 < to) load(t + 1);
-        const uint32_t tile = (t - from) % NBUF * (2 * TK * L::PB), along = along0 + tile, across = across0 + tile;
+        const uint32_t tile = (t - from) % NBUF * (2 * TK * L::PB), along = NBUF == 1 ? again(along0) : along0 + tile, across = NBUF == 1 ? again(across0) : across0 + tile;
 #pragma unroll
         for (int h = 0; h < TK; h += STEP) {
             const int first = t * TK + h;
@@ -747,7 +747,8 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, boo
         attn_barrier();
         ahead.next(each);
         if (NBUF > 1 && t + 1 < to) load(ahead);
-        const uint32_t tile = now.buffer * BUF, along = along0 + tile, across = across0 + tile, sums = lds0 + tile + 2 * TQ * L::PB + 16 * g; // queries; gradients behind them
+        // queries; gradients behind them (where they lie in one place tile after tile, their addresses are computed anew all the same: kept, they take the registers)
+        const uint32_t tile = now.buffer * BUF, along = NBUF == 1 ? again(along0) : along0 + tile, across = NBUF == 1 ? again(across0) : across0 + tile, sums = lds0 + tile + 2 * TQ * L::PB + 16 * g;
         const int pos0 = (skip + now.tile) * TQ;
         now.next(each);
 #pragma unroll
@@ -889,7 +890,7 @@ __global__ __launch_bounds__(attn_shape(sizeof(T), DP, ATTN_DQ).waves * 64, 2) v
     typedef DkvShape<T, DP, k.m, k.waves, k.share, k.tile, k.buffers, DK, DV> Dkv;
     __shared__ alignas(256) uint8_t lds[Dq::LDS > Dkv::LDS ? Dq::LDS : Dkv::LDS];
     if ((int)blockIdx.x < split) attention_dkv<T, DP, k.m, k.waves, k.share, k.tile, k.buffers, DK, DV>(by_k, blockIdx.x, lds);
-    else attention_dq<T, DP, q.m, q.waves, q.share, q.tile, q.buffers>(by_q, blockIdx.x - split, lds);
+    else if constexpr (DK) attention_dq<T, DP, q.m, q.waves, q.share, q.tile, q.buffers>(by_q, blockIdx.x - split, lds); // (dv alone: no launch for queries)
 }
 
 // ---------------------------------------------------------------- launches
