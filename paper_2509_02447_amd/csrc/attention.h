@@ -294,10 +294,11 @@ template <int M, int WAVES, typename ACC, int COUNT> __device__ __forceinline__ 
 // than 2^GROWS, so that most tiles leave them alone.  Sums and results in 32 bits; probabilities are rounded to the type for the second product (16-bit types:
 // half a step relative to each, unsystematic, which is what the output's own rounding is).  f16: they are taken times 2^11, so that many keys of little weight
 // are not lost under its smallest number: 2^-36 a key (they stay under 2^16, with what the maximum may grow).
-// Bound: rows of 128 and less, bf16, by the matrix pipe at the clock that the card's power allows (2 x 8192 causal rows of 16 heads of 128: 515 .. 545 us, 1.03 .. 1.07 PFLOP/s, where a
-// large library product reaches 1.12); f32 by its products (3 x 2257 rows of 6 heads of 60: 200 us, 120 TFLOP/s); one head of 512 by LDS reads, which sixteen columns to a wavefront make
-// twice what the products take (4 x 4096 rows: 150 us, 0.92 PFLOP/s; two wavefronts that share 32 columns halve the reads and wait for each other: 184 with the join, against 164);
-// single tokens by memory (4.5 TB/s of the keys and values that are there).
+// Bound (kernels by a trace's medians; calls in a row without the profiler take less): rows of 128 and less, bf16, by the matrix pipe at the clock that the card's power allows (2 x 8192
+// causal rows of 16 heads of 128: 545 us, 1.01 PFLOP/s, the call in a row 519, 1.06, where a large library product reaches 1.12); f32 by its products (3 x 2257 rows of 6 heads of 60: 225 us,
+// 104 TFLOP/s counting the 64 elements that are computed); one head of 512 by LDS reads, which sixteen columns to a wavefront make twice what the products take (4 x 4096 rows: 179 us,
+// 0.77 PFLOP/s, the call with its join 168 in a row; when two wavefronts shared 32 columns, which halves the reads, they waited for each other: calls of 184 against 164); single tokens by memory
+// (16 over up to 8191 rows: 38 us, 4.3 TB/s of the keys and values that are there).
 template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF, int OCC>
 __global__ __launch_bounds__(WAVES * 64, OCC) void attention_kernel(AttnArgs a)
 {
@@ -658,7 +659,7 @@ template <typename T, int DP, int M, int WAVES, int SHARE, int TK, int NBUF> __d
 // Columns: key rows.  dv = sum over queries of P do, dk = scale sum of dS q, over all heads that share the keys.  DK, DV: which of the two (both where the
 // registers hold both).  Of 128 elements of 16 bits the values lie in LDS: with them in registers there are none left for operands that are on their way
 // (2 x 4096 causal rows of 16 heads, the whole call: 480 us, from LDS 471, with three reads for two products instead of two).  Bound: rows of 128 and less by the matrix pipe, with seven
-// products in both halves (that call: 445 us in the kernel, 1.08 PFLOP/s); one head of 512 by the three barriers of a tile and LDS, which hold one workgroup to a compute unit (4 x 1024 rows: 62 us).
+// products in both halves (that call: 448 us in the kernel, 1.07 PFLOP/s); one head of 512 by the three barriers of a tile and LDS, which hold one workgroup to a compute unit (4 x 1024 rows: 63 us).
 template <typename T, int DP, int M, int WAVES, int SHARE, int TQ, int NBUF, bool DK, bool DV> struct DkvShape {
     static constexpr bool FROM_LDS = DK && DV && sizeof(T) == 2 && DP == 128;
     static constexpr int LDS = NBUF * (2 * TQ * Tile<T, DP>::PB + 512) + (FROM_LDS ? WAVES * M * Tile<T, DP>::PB : 0) + (SHARE > 1 ? WAVES * 2048 : 0);

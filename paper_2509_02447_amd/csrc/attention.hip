@@ -326,7 +326,7 @@ AttnCut plan_attention(const qrm_attention_desc &d, int width, int num_cu)
 }
 
 // Both sides of a backward launch, whatever of it is wanted: a gradient's bits do not depend on the others.  Measured, us of the call, by splits of queries' / keys' side: 16 heads of 128, 4 key
-// heads, 2 x 4096 causal rows 1/1 634, 1/2 498, 1/3 460, 1/4 466, [1/5 470]; one head of 512, 4 x 1024 rows 1/1 109, 1/2 82, 1/3 85, [2/2 79], 2/3 92; f16, 5 x 777 rows over 1033, 8 heads of 96,
+// heads, 2 x 4096 causal rows 1/1 634, 1/2 498, 1/3 460, 1/4 466, [1/5 470], 2 % from the best; one head of 512, 4 x 1024 rows 1/1 109, 1/2 82, 1/3 85, [2/2 79], 2/3 92; f16, 5 x 777 rows over 1033, 8 heads of 96,
 // 2 key heads 1/1 119, 1/2 74, [1/3 63], 1/4 67, 2/4 62.
 void plan_attention_backward(const qrm_attention_desc &d, int width, int num_cu, AttnCut *by_q, AttnCut *by_k)
 {

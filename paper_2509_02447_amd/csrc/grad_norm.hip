@@ -1,8 +1,9 @@
 // The norm of all gradients of a step with the factor that clips it (qrm_adamw_grad_norm), and gradients times a factor (qrm_adamw_scale_grads).
 //
 // A wavefront takes pieces of 4096 elements from the optimiser's table; squares and sums are taken in 64 bits, as wide as no square of a gradient
-// overflows.  One launch: the workgroup that is done last adds the others' sums up, in their order.  Bound by memory: a gradient is read once, 16 KB a
-// wavefront under way before the first is used (50 M elements of bf16, 100 MB: 28 us, 3.6 TB/s; 60 thousand of f32 in one workgroup: 5.6 us); the factor is applied in 31 us (200 MB, 6.4 TB/s).
+// overflows.  One launch: the workgroup that is done last adds the others' sums up, in their order.  Bound by memory: a gradient is read once, a
+// piece a wavefront (16 KB of f32, 8 KB of 16 bits) under way before the first is used (50 M elements of bf16, 100 MB: 28 us, 3.5 TB/s; 60 thousand of f32 in one workgroup: 5.7 us); the factor is
+// applied in 32 us (200 MB, 6.2 TB/s).
 #include "qrm_train.h"
 
 #include <algorithm>

@@ -217,7 +217,8 @@ struct AttnArgs { // of the kernels; strides in elements; rows of D elements lie
 // How a kernel cuts its work: columns of a wavefront (the matrix products' side), wavefronts of a workgroup, how many of them share a set of columns, rows of
 // the other side in a tile, tiles in LDS, wavefronts to a SIMD that the registers are kept for.
 // Tiles and wavefronts as measured, us (forward, bf16): one head of 512, 4 x 4096 rows, 16 columns in each of eight wavefronts with two tiles in LDS 164, two wavefronts to 32 columns 184 (two
-// tiles) and 200 (one); rows of 64 and less in tiles of 64 keys or 32: f32 or bf16 over 4096 keys 170 and 179, over 77 keys 21 and 19.6.
+// tiles) and 200 (one); rows of 64 and less in tiles of 64 keys or 32: f32 or bf16 over 4096 keys 170 and 179, over 77 keys 21 and 19.6: 64 for all
+// lengths, for the long ones' sake.
 struct AttnShape {
     int m, waves, share, tile, buffers, occupancy;
     constexpr int rows() const { return m * waves / share; }
