@@ -1,5 +1,6 @@
 """The binding's module for lists of tensors, and that a call's host work in Python does not grow with the number of tensors."""
 import ctypes
+import gc
 import sys
 
 import pytest
@@ -68,11 +69,13 @@ def test_the_calls_of_a_step_do_not_grow_with_its_tensors():
             opt.qrm_adamw_step(zeros[3], 1, 1e-3, d_grad_scale=scale, stream=stream)
 
         call()
+        gc.disable()                                               # (what it collects has calls of its own)
         sys.setprofile(lambda frame, event, arg: seen.append(event) if event in ("call", "c_call") else None)
         try:
             call()
         finally:
             sys.setprofile(None)
+            gc.enable()
         counts.append(len(seen))
         torch.cuda.synchronize()
         opt.close()
